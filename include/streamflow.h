@@ -311,6 +311,90 @@ int sf_context_cache_stats(const sf_model* m, long* calls, long* projected);
 int sf_timing_enable(sf_model* m, int kc, int enable);
 int sf_timing_read(sf_model* m, int kc, double* total_ms, long* launches);
 
+/* ---- Operators on the caller's own tensors -------------------------------------------
+ *
+ * The calls below need no model. They enqueue on hip_stream of the current device, keep
+ * no state and no workspace, allocate nothing (so they may be captured into a graph) and
+ * give the same bits on every call. Device pointers; strides and row lengths count
+ * elements. An empty tensor (a count of 0) is no work and returns SF_OK. */
+
+/* Rows of x to 8-bit codes with one scale per row (a token's activations, or an output
+ * channel's weights):
+ *   a_m = max_k |x[m][k]|, codes[m][k] = rint(127 x[m][k] / a_m), scale[m] = a_m / 127,
+ * rint of the exact quotient, ties to even, the scale rounded to fp32. A row of zeros has
+ * codes and scale 0. A row that holds a NaN or an infinity has codes 0 and scale NaN, so
+ * whatever is computed from it is NaN.
+ * x: [rows][cols], row length ldx, element type SF_PREC_BF16 or SF_PREC_FP32; codes:
+ * [rows][cols], row length ldc, a multiple of 16 at an address that is one (the bytes past
+ * cols stay as they are); scale: [rows]. cols 1..1048576. SF_E_INVAL otherwise. */
+int sf_quantize_rows(const void* x, int type, long long rows, int cols, long long ldx, signed char* codes,
+                     long long ldc, float* scale, void* hip_stream);
+
+/* The product of two matrices of 8-bit codes, each row with its scale (a linear layer in
+ * 8 bits: tokens A, weights B stored [out][in]):
+ *   out[m][n] = (sum_k A[m][k] B[n][k]) a_scale[m] b_scale[n] + bias[n]
+ * The sum is exact (32-bit integers); its conversion to fp32, the two products and the sum
+ * with the bias are rounded to fp32 one after the other, and to the output's type last.
+ * a: [M][K], row length lda; b: [N][K], row length ldb; both row lengths multiples of 16
+ * and at least K rounded up to one, at addresses that are multiples of 16, every row
+ * readable to that length (what stands past K is not used). bias: fp32 [N] or NULL. out:
+ * [M][N], row length ldo >= N, element type out_type (SF_PREC_*), any alignment of its
+ * elements. K 1..131071 (a longer sum could pass 32 bits); row lengths below 2^23. */
+int sf_matmul_i8(const signed char* a, long long lda, const float* a_scale, const signed char* b, long long ldb,
+                 const float* b_scale, const float* bias, int M, int N, int K, void* out, long long ldo, int out_type,
+                 void* hip_stream);
+
+/* Rotary positions with several axes (row and column of a picture; time, row and column
+ * of a video). Each pair (x, y) of a head's dims belongs to one axis and turns by the angle
+ * u = p f of its token's position p on that axis: (x cos u - y sin u, x sin u + y cos u).
+ *   dims[a]: head dims turned by axis a, even, 0 for none; the pairs are numbered axis by
+ *            axis, and the dims past sum(dims) stay as they are.
+ *   layout:  SF_ROPE_ADJACENT      pair j is dims (2j, 2j + 1);
+ *            SF_ROPE_HALVES        pair j is dims (j, j + P), P pairs in all;
+ *            SF_ROPE_AXIS_HALVES   pair i of an axis whose dims start at s is dims
+ *                                  (s + i, s + dims[a] / 2 + i).
+ *   spread:  0: f = theta^(-2 i / dims[a]) for pair i of axis a (every axis has the whole
+ *            range of frequencies); 1: f = theta^(-j / P) for pair j of all P (one
+ *            range, shared out over the axes).
+ * Angles are formed and reduced in fp64, so far positions keep their digits. */
+enum { SF_ROPE_ADJACENT = 0, SF_ROPE_HALVES = 1, SF_ROPE_AXIS_HALVES = 2 };
+#define SF_ROPE_AXES 4
+typedef struct sf_rope {
+  int axes;                /* values per position, 1..SF_ROPE_AXES */
+  int dims[SF_ROPE_AXES];
+  int layout;
+  int spread;
+  double theta;            /* finite, > 1 (10000) */
+} sf_rope;
+
+/* A tensor of heads [rows][tokens][heads][dh], read from `in` and written to `out`, which is
+ * `in` itself with the same strides or does not overlap it. The dims of a head are adjacent;
+ * the strides (in elements) are free, and those of `in` may be 0. */
+typedef struct sf_heads {
+  const void* in;
+  void* out;
+  int heads;
+  long long in_row, in_token, in_head;
+  long long out_row, out_token, out_head;
+} sf_heads;
+
+/* Turns every head of x by its token's position (inverse: by minus the angles).
+ * type: SF_PREC_*; dh even, 2..256; pos: fp32 [rows][tokens][axes], pos_row elements from
+ * one row to the next (0: one table for all rows). Products and sums in fp32, one
+ * rounding to the element type. SF_E_INVAL for a rope whose dims pass dh, null pointers, an
+ * output stride of 0 over more than one entry, or rows x tokens of 2^31 and more. */
+int sf_rotate(const sf_heads* x, int type, int rows, int tokens, int dh, const sf_rope* rope, const float* pos,
+              long long pos_row, int inverse, void* hip_stream);
+
+/* The norm of queries and keys for each head, and their rotation, in one pass:
+ *   y = x / sqrt(mean_d x^2 + eps) * gain[d], then y turned as by sf_rotate.
+ * k may be NULL (q alone), and may have other strides and fewer heads than q. q_gain, k_gain:
+ * fp32 [dh] or NULL (1). rope NULL: the norm alone (pos is not read). eps >= 0. Statistics
+ * and products in fp32, one rounding to the element type. Otherwise as sf_rotate. */
+int sf_qk_norm_rotate(const sf_heads* q, const sf_heads* k, const float* q_gain, const float* k_gain, float eps, int type,
+                      int rows, int tokens, int dh, const sf_rope* rope, const float* pos, long long pos_row,
+                      void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

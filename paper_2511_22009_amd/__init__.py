@@ -4,5 +4,16 @@ marshals arguments (torch tensors provide device memory and streams)."""
 from .binding import (Buffer, Cond, KernelClass, Model, SFError, Precision, lib_path, load_library,
                       library_symbols)
 
+# the operators on torch tensors; importing the package itself needs no torch
+_OPERATORS = ("Rotary", "matmul_i8", "qk_norm_rotate", "quantize_rows", "rotate")
+
 __all__ = ["Buffer", "Cond", "KernelClass", "Model", "SFError", "Precision", "lib_path", "load_library",
-           "library_symbols"]
+           "library_symbols", *_OPERATORS]
+
+
+def __getattr__(name):
+    if name in _OPERATORS:
+        from . import operators
+        globals().update({n: getattr(operators, n) for n in _OPERATORS})
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -14,6 +14,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libstreamflow.so"
 
 SF_MAX_ROWS = 64
+SF_ROPE_AXES = 4
 
 
 class Precision(enum.IntEnum):
@@ -70,9 +71,20 @@ class _Info(ctypes.Structure):
                 ("vt_ld", ctypes.c_int), ("vt_key_perm", ctypes.c_int)]
 
 
+class _Rope(ctypes.Structure):
+    _fields_ = [("axes", ctypes.c_int), ("dims", ctypes.c_int * SF_ROPE_AXES), ("layout", ctypes.c_int),
+                ("spread", ctypes.c_int), ("theta", ctypes.c_double)]
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("heads", ctypes.c_int)] + \
+               [(n, ctypes.c_longlong) for n in ("in_row", "in_token", "in_head", "out_row", "out_token", "out_head")]
+
+
 _LIB = None
 _P = ctypes.c_void_p
 _I = ctypes.c_int
+_J = ctypes.c_longlong
 _SIGS = {
     "sf_load_weights": (_I, [ctypes.c_void_p, ctypes.c_size_t, _I, _I, ctypes.POINTER(_P)]),
     "sf_free": (None, [_P]),
@@ -97,6 +109,10 @@ _SIGS = {
     "sf_modulation_cache_stats": (_I, [_P, ctypes.POINTER(ctypes.c_long)]),
     "sf_context_cache": (_I, [_P, _I]),
     "sf_context_cache_stats": (_I, [_P, ctypes.POINTER(ctypes.c_long), ctypes.POINTER(ctypes.c_long)]),
+    "sf_quantize_rows": (_I, [_P, _I, _J, _I, _J, _P, _J, _P, _P]),
+    "sf_matmul_i8": (_I, [_P, _J, _P, _P, _J, _P, _P, _I, _I, _I, _P, _J, _I, _P]),
+    "sf_rotate": (_I, [_P, _I, _I, _I, _I, _P, _P, _J, _I, _P]),
+    "sf_qk_norm_rotate": (_I, [_P, _P, _P, _P, ctypes.c_float, _I, _I, _I, _I, _P, _P, _J, _P]),
 }
 
 

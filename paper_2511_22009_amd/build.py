@@ -15,7 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OUT = os.path.join(HERE, "libstreamflow.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
-SOURCES = ["k_cond.hip", "k_norm.hip", "k_gemm.hip", "k_attn.hip", "k_euler.hip", "streamflow.cpp"]
+SOURCES = ["k_cond.hip", "k_norm.hip", "k_gemm.hip", "k_attn.hip", "k_euler.hip", "k_quant.hip",
+           "k_gemm_i8.hip", "k_rope.hip", "streamflow.cpp", "operators.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",

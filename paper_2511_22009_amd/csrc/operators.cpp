@@ -1,0 +1,117 @@
+// C ABI of the operators on the caller's own tensors: argument checks and one launch each.
+#include "streamflow.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "sf_launch.h"
+
+namespace {
+
+static_assert(sf::kRopeAxes == SF_ROPE_AXES, "axes of a rotation");
+
+bool is_type(int t) { return t == SF_PREC_BF16 || t == SF_PREC_FP32; }
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+int status(hipError_t e) { return e == hipSuccess ? SF_OK : SF_E_HIP; }
+
+// True when the plan fits heads of dh dims; fills the kernel's form of it.
+bool take_rope(const sf_rope& r, int dh, sf::RopeArgs& a) {
+  if (r.axes < 1 || r.axes > SF_ROPE_AXES || r.layout < SF_ROPE_ADJACENT || r.layout > SF_ROPE_AXIS_HALVES ||
+      (r.spread != 0 && r.spread != 1) || !std::isfinite(r.theta) || !(r.theta > 1.0))
+    return false;
+  int pairs = 0;
+  for (int i = 0; i < r.axes; ++i) {
+    if (r.dims[i] < 0 || r.dims[i] % 2 || r.dims[i] > dh) return false;
+    a.first[i] = pairs;
+    pairs += r.dims[i] / 2;
+  }
+  if (2 * pairs > dh) return false;
+  for (int i = r.axes; i <= SF_ROPE_AXES; ++i) a.first[i] = pairs;
+  a.axes = r.axes;
+  a.pairs = pairs;
+  a.layout = r.layout;
+  a.spread = r.spread;
+  a.log2_theta = std::log2(r.theta);
+  return true;
+}
+
+// Whether every entry of the output has a place of its own as far as a stride of 0 tells.
+bool own_places(const sf_heads& t, int rows, int tokens) {
+  return !((rows > 1 && t.out_row == 0) || (tokens > 1 && t.out_token == 0) || (t.heads > 1 && t.out_head == 0));
+}
+
+sf::RopeHeads take_heads(const sf_heads& t, const float* gain) {
+  return sf::RopeHeads{(const char*)t.in, (char*)t.out, gain,       t.in_row,  t.in_token,
+                       t.in_head,         t.out_row,    t.out_token, t.out_head};
+}
+
+int rope_call(const sf_heads* q, const sf_heads* k, const float* q_gain, const float* k_gain, bool norm, float eps, int type,
+              int rows, int tokens, int dh, const sf_rope* rope, const float* pos, long long pos_row, int inverse,
+              void* stream) {
+  if (!q || !is_type(type) || rows < 0 || tokens < 0 || (int64_t)rows * tokens > 0x7fffffff || dh < 2 || dh > 256 || dh % 2 ||
+      q->heads < 0 || (k && k->heads < 0) || (int64_t)q->heads + (k ? k->heads : 0) > 65535 || !(eps >= 0.0f) ||
+      !std::isfinite(eps))
+    return SF_E_INVAL;
+  sf::RopeArgs a{};
+  if (rope && !take_rope(*rope, dh, a)) return SF_E_INVAL;
+  a.heads0 = q->heads;
+  a.heads = q->heads + (k ? k->heads : 0);
+  if (rows == 0 || tokens == 0 || a.heads == 0) return SF_OK;
+  if (rope && !pos) return SF_E_INVAL;
+  if (q->heads > 0 && (!q->in || !q->out || !own_places(*q, rows, tokens))) return SF_E_INVAL;
+  if (k && k->heads > 0 && (!k->in || !k->out || !own_places(*k, rows, tokens))) return SF_E_INVAL;
+  a.t[0] = take_heads(*q, q_gain);
+  if (k) a.t[1] = take_heads(*k, k_gain);
+  a.rows = rows;
+  a.tokens = tokens;
+  a.dh = dh;
+  a.div_tok = sf::make_fastdiv((uint32_t)tokens);
+  a.eps = eps;
+  a.inverse = inverse != 0;
+  a.pos = pos;
+  a.pos_row = pos_row;
+  return status(sf::launch_rope(type == SF_PREC_BF16, norm, rope != nullptr, a, (hipStream_t)stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+int sf_quantize_rows(const void* x, int type, long long rows, int cols, long long ldx, signed char* codes, long long ldc,
+                     float* scale, void* stream) {
+  if (!is_type(type) || rows < 0 || rows > 0x7fffffff || cols < 1 || cols > (1 << 20)) return SF_E_INVAL;
+  if (rows == 0) return SF_OK;
+  if (!x || !codes || !scale || ldx < 0 || ldc % 16 || ldc < cols || !aligned16(codes)) return SF_E_INVAL;
+  const sf::QuantArgs a{x, ldx, (int)rows, cols, (int8_t*)codes, ldc, scale};
+  return status(sf::launch_quantize_rows(type == SF_PREC_BF16, a, (hipStream_t)stream));
+}
+
+int sf_matmul_i8(const signed char* a, long long lda, const float* a_scale, const signed char* b, long long ldb,
+                 const float* b_scale, const float* bias, int M, int N, int K, void* out, long long ldo, int out_type,
+                 void* stream) {
+  if (!is_type(out_type) || M < 0 || N < 0 || K < 1 || K > 131071) return SF_E_INVAL;
+  if (M == 0 || N == 0) return SF_OK;
+  const long long need = ((long long)K + 15) / 16 * 16;
+  constexpr long long kMostLd = 1ll << 23;  // a tile's rows stay within 32-bit offsets
+  if (!a || !b || !a_scale || !b_scale || !out || !aligned16(a) || !aligned16(b) || lda % 16 || ldb % 16 || lda < need ||
+      ldb < need || lda >= kMostLd || ldb >= kMostLd || ldo < N)
+    return SF_E_INVAL;
+  const sf::GemmI8Args g{(const int8_t*)a, (const int8_t*)b, (int)lda, (int)ldb, M, N, K, a_scale, b_scale, bias, out, ldo};
+  return status(sf::launch_gemm_i8(out_type == SF_PREC_BF16, g, (hipStream_t)stream));
+}
+
+int sf_rotate(const sf_heads* x, int type, int rows, int tokens, int dh, const sf_rope* rope, const float* pos,
+              long long pos_row, int inverse, void* stream) {
+  if (!rope) return SF_E_INVAL;
+  return rope_call(x, nullptr, nullptr, nullptr, false, 0.0f, type, rows, tokens, dh, rope, pos, pos_row, inverse, stream);
+}
+
+int sf_qk_norm_rotate(const sf_heads* q, const sf_heads* k, const float* q_gain, const float* k_gain, float eps, int type,
+                      int rows, int tokens, int dh, const sf_rope* rope, const float* pos, long long pos_row,
+                      void* stream) {
+  return rope_call(q, k, q_gain, k_gain, true, eps, type, rows, tokens, dh, rope, pos, pos_row, 0, stream);
+}
+
+}  // extern "C"

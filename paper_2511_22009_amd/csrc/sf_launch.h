@@ -234,4 +234,60 @@ hipError_t launch_cfg_combine(const float* v, int B, int E, float w, float* v_ou
 // out = (1 - t0) x_ref + t0 z, each product and the sum rounded separately
 hipError_t launch_noise_latent(const float* x_ref, const float* z, float t0, int E, float* out, hipStream_t s);
 
+// ---- rows to 8-bit codes -------------------------------------------------------------
+struct QuantArgs {
+  const void* x;        // [M][K], row length ldx, bf16 or fp32
+  int64_t ldx;
+  int M, K;
+  int8_t* q;            // [M][K], row length ldq (a multiple of 16, 16-byte aligned)
+  int64_t ldq;
+  float* scale;         // [M]
+};
+hipError_t launch_quantize_rows(bool x_bf16, const QuantArgs& a, hipStream_t s);
+
+// ---- products of 8-bit codes: out = (A . B^T) sa[m] sb[n] + bias[n] ------------------
+struct GemmI8Args {
+  const int8_t* A;      // [M][K], row length lda (a multiple of 16, 16-byte aligned)
+  const int8_t* B;      // [N][K], row length ldb
+  int lda, ldb;
+  int M, N, K;
+  const float* sa;      // [M]
+  const float* sb;      // [N]
+  const float* bias;    // [N] or nullptr
+  void* out;            // [M][N], row length ldo
+  int64_t ldo;
+};
+hipError_t launch_gemm_i8(bool out_bf16, const GemmI8Args& a, hipStream_t s);
+
+// ---- per-head norm and rotation of heads ---------------------------------------------
+constexpr int kRopeAxes = 4;  // equals SF_ROPE_AXES
+struct RopeHeads {
+  const char* in;
+  char* out;
+  const float* gain;    // [dh] or nullptr
+  int64_t in_row, in_tok, in_head;     // strides in elements
+  int64_t out_row, out_tok, out_head;
+};
+struct RopeArgs {
+  RopeHeads t[2];       // q and k (heads0 and heads - heads0 heads)
+  int heads0, heads;
+  int rows, tokens, dh;
+  FastDiv div_tok;
+  float eps;
+  int pairs;            // rotated pairs
+  int axes;
+  int first[kRopeAxes + 1];  // first pair of each axis; past the last one, `pairs`
+  int layout;           // SF_ROPE_*
+  int spread;
+  double log2_theta;
+  int inverse;
+  const float* pos;     // [rows][tokens][axes]
+  int64_t pos_row;
+  int head_step;        // heads of a wavefront
+  int group_log2;       // lanes that share a head: 2^group_log2
+};
+// norm: divide by the root mean square and multiply by the gain; rotate: turn the pairs.
+// Fills in heads per wavefront and lanes per head.
+hipError_t launch_rope(bool is_bf16, bool norm, bool rotate, RopeArgs a, hipStream_t s);
+
 }  // namespace sf
