@@ -1,75 +1,300 @@
 // Products of 8-bit codes on the matrix cores, out[m][n] = (sum_k A[m][k] B[n][k]) sa[m] sb[n]
 // + bias[n]: v_mfma_i32_32x32x32_i8, whose 32-bit sums are exact for every K the entry point
-// allows, on 64 x 64 tiles over 128-wide slices of K.
+// allows, so no choice of tile changes a bit of a result. The weights are the first operand, so
+// a lane ends up with four adjacent output columns of one row.
+//
+// What bounds it: the matrix cores at the clock that their power leaves, and what a tile costs
+// besides its slices. 8192 x 8192 x 8192 takes 444 us (2470 TOP/s; a 256 x 256 tile reaches 398
+// us there, 2760, but loses below K = 4096 or so), 16384 x 4608 x 1152 takes 98 us. Of those 98,
+// 65 go with K (every further 1152 columns cost them again) and 33 do not: the 151 MB of
+// outputs, 23 us at the rate of a plain fill, and the first slices' latency. Outputs that are
+// written while the next tile is under way, by workgroups that stay and fetch across tiles,
+// took the second part to 26 us at K = 128, but the larger kernel's loop lost as much.
 #include "sf_device.h"
 
 namespace sf {
 
-template <typename OT>
-__global__ __launch_bounds__(256) void gemm_i8_kernel(GemmI8Args a) {
-  constexpr int BM = 64, BN = 64, BK = 128, LD = BK + 16;
-  __shared__ __attribute__((aligned(16))) char As[BM * LD];
-  __shared__ __attribute__((aligned(16))) char Bs[BN * LD];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int wm = wave >> 1, wn = wave & 1, l32 = lane & 31, g = lane >> 5;
-  const int nbn = (a.N + BN - 1) / BN;
-  const int m0 = (int)(blockIdx.x / nbn) * BM, n0 = (int)(blockIdx.x % nbn) * BN;
-  i32x16 acc;
+// Workgroup -> tile: each of the eight XCDs (workgroup b goes to XCD b % 8) takes a contiguous
+// range of tiles, in groups of eight tile rows with M fastest, so that the rows and columns
+// that a group touches are read from one L2 (groups of 2, 4 and 16 rows: level or up to 5 %
+// slower).
+__device__ __forceinline__ void i8_tile(int nbm, int nbn, int& mt, int& nt) {
+  const int T = nbm * nbn, b = blockIdx.x;
+  const int xcd = b % 8, local = b / 8, base = T / 8, rem = T % 8;
+  const int logical = xcd * base + min(xcd, rem) + local;
+  const int per_group = 8 * nbn;
+  const int group = logical / per_group;
+  const int first_m = group * 8, gsize = min(8, nbm - first_m);
+  const int in = logical - group * per_group;
+  mt = first_m + in % gsize;
+  nt = in / gsize;
+}
+
+// 128-wide slices of K go global -> LDS directly into a ring of STAGES buffers (rows of eight
+// 16-byte chunks, swizzled by dma_swz); every wavefront owns a sub-tile of 32 x 32 blocks over
+// the whole slice and reads its fragments one K step of 32 ahead, across the slice boundary
+// too. The last K step of a slice has its operands in registers when the workgroup meets at
+// the slice's one barrier, so that barrier frees the stage just read: its refill and the reads
+// of the next slice's first fragments go out under that step's MFMAs.
+//
+// Codes past K: whole chunks read as zeros (an offset past the resource); in a chunk that K
+// ends in, A's bytes past K are cleared in LDS before the last slice is read (a code times 0
+// is 0, whatever B holds there).
+template <int BM, int BN, int WM, int WN, int STAGES, int MINW, typename OT>
+__global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_i8_kernel(GemmI8Args a) {
+  constexpr int NT = WM * WN * 64, BK = 128, CPR = 8, KS = 4;
+  constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+  static_assert(TM * WM * 32 == BM && TN * WN * 32 == BN, "wave grid must tile the block");
+  constexpr int ATOT = BM * CPR, BTOT = BN * CPR;
+  static_assert(ATOT % NT == 0 && BTOT % NT == 0, "whole rounds of chunks per slice");
+  constexpr int ACH = ATOT / NT, BCH = BTOT / NT, LPT = ACH + BCH;
+  static_assert(STAGES >= 2 && STAGES <= 4, "two to four stages");
+  constexpr int SLICE = (ATOT + BTOT) * 16;
+  static_assert(STAGES * SLICE <= 160 * 1024, "stages do not fit in LDS");
+  __shared__ __attribute__((aligned(16))) char st0[SLICE];
+  __shared__ __attribute__((aligned(16))) char st1[SLICE];
+  __shared__ __attribute__((aligned(16))) char st2[STAGES > 2 ? SLICE : 16];
+  __shared__ __attribute__((aligned(16))) char st3[STAGES > 3 ? SLICE : 16];
+  auto stage = [&](auto s) -> char* {
+    constexpr int S = decltype(s)::value % STAGES;
+    if constexpr (S == 0) return st0;
+    else if constexpr (S == 1) return st1;
+    else if constexpr (S == 2) return st2;
+    else return st3;
+  };
+  const int tid = threadIdx.x;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  const int l32 = lane & 31, g = lane >> 5;
+  int mt, nt;
+  const int nbm = (a.M + BM - 1) / BM, nbn = (a.N + BN - 1) / BN;
+  i8_tile(nbm, nbn, mt, nt);
+  const int m0 = mt * BM, n0 = nt * BN;
+  // the epilogue's scales and bias are fetched now: lane l holds those of column l % 32 of each
+  // block column and of row l % 32 of each block row
+  float sa_v[TM], sb_v[TN], bias_v[TN];
 #pragma unroll
-  for (int r = 0; r < 16; ++r) acc[r] = 0;
-  // 16 bytes of row `row` of X at column k; bytes of rows and columns that do not exist are 0
-  auto chunk = [&](const int8_t* X, int ld, int rows, int row, int k) {
-    i32x4 v = {0, 0, 0, 0};
-    if (row < rows && k < a.K) {
-      v = *(const i32x4*)(X + (int64_t)row * ld + k);
-      const int left = a.K - k;
-      if (left < 16) {
+  for (int i = 0; i < TM; ++i) sa_v[i] = a.sa[min(m0 + (wm * TM + i) * 32 + l32, a.M - 1)];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const int n = left - 4 * w;
-          if (n < 4) v[w] = n > 0 ? (int)((uint32_t)v[w] & ((1u << (8 * n)) - 1u)) : 0;
+  for (int j = 0; j < TN; ++j) {
+    const int n = min(n0 + (wn * TN + j) * 32 + l32, a.N - 1);
+    sb_v[j] = a.sb[n];
+    bias_v[j] = a.bias ? a.bias[n] : 0.0f;
+  }
+  int a_off[ACH], b_off[BCH], a_kc[ACH], b_kc[BCH];
+#pragma unroll
+  for (int i = 0; i < ACH; ++i) {
+    const int p = tid + i * NT, row = p / CPR;
+    a_kc[i] = ((p % CPR) ^ dma_swz<CPR>(row)) * 16;
+    a_off[i] = m0 + row < a.M ? row * a.lda + a_kc[i] : kOffOOB;
+  }
+#pragma unroll
+  for (int i = 0; i < BCH; ++i) {
+    const int p = tid + i * NT, row = p / CPR;
+    b_kc[i] = ((p % CPR) ^ dma_swz<CPR>(row)) * 16;
+    b_off[i] = n0 + row < a.N ? row * a.ldb + b_kc[i] : kOffOOB;
+  }
+  // resources based at the tile's first row and the slice's first column, as long as the
+  // tile's rows (each to the end of the chunk that K ends in)
+  const int8_t* const A0 = a.A + (int64_t)m0 * a.lda;
+  const int8_t* const B0 = a.B + (int64_t)n0 * a.ldb;
+  const int kend = (a.K + 15) & ~15;
+  const uint32_t a_bytes = (uint32_t)(min(a.M - m0, BM) - 1) * a.lda + kend;
+  const uint32_t b_bytes = (uint32_t)(min(a.N - n0, BN) - 1) * a.ldb + kend;
+  auto issue = [&](auto fast, char* sb, int kt) __attribute__((always_inline)) {
+    const int k0 = kt * BK;
+    const bool live = k0 < a.K;
+    const __amdgpu_buffer_rsrc_t ra = buffer_rsrc(A0 + k0, live ? a_bytes - k0 : 0u);
+    const __amdgpu_buffer_rsrc_t rb = buffer_rsrc(B0 + k0, live ? b_bytes - k0 : 0u);
+    constexpr bool F = decltype(fast)::value;
+#pragma unroll
+    for (int i = 0; i < ACH; ++i)
+      buffer_load16_lds(ra, sb + (i * NT + wave * 64) * 16, F || k0 + a_kc[i] < a.K ? a_off[i] : kOffOOB);
+#pragma unroll
+    for (int i = 0; i < BCH; ++i)
+      buffer_load16_lds(rb, sb + (ATOT + i * NT + wave * 64) * 16, F || k0 + b_kc[i] < a.K ? b_off[i] : kOffOOB);
+  };
+  // clears A's bytes past K in the last slice
+  auto clear_tail = [&](char* sb) {
+    const int c = (a.K % BK) / 16;
+    for (int r = tid; r < BM; r += NT) {
+      char* p = sb + (r * CPR + (c ^ dma_swz<CPR>(r))) * 16;
+      i32x4 v = *(i32x4*)p;
+      const int left = a.K % 16;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int n = left - 4 * w;
+        if (n < 4) v[w] = n > 0 ? (int)((uint32_t)v[w] & ((1u << (8 * n)) - 1u)) : 0;
+      }
+      *(i32x4*)p = v;
+    }
+    __syncthreads();
+  };
+
+  i32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0;
+  const int sw = dma_swz<CPR>(l32);  // row blocks are 32 apart: every row of a lane shares it
+  const int a_row = (wm * TM * 32 + l32) * CPR;
+  const int b_row = ATOT + (wn * TN * 32 + l32) * CPR;
+  i32x4 af[2][TM], bfr[2][TN];
+  auto frags = [&](const char* cur, int buf, int kk) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) af[buf][i] = *(const i32x4*)(cur + (a_row + i * 32 * CPR + ((g + 2 * kk) ^ sw)) * 16);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) bfr[buf][j] = *(const i32x4*)(cur + (b_row + j * 32 * CPR + ((g + 2 * kk) ^ sw)) * 16);
+  };
+  auto mfmas = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bfr[buf][j], af[buf][i], acc[i][j], 0, 0, 0);
+  };
+  constexpr int NM = TM * TN, ND = TM + TN;
+  const int nk = (a.K + BK - 1) / BK;
+  auto step = [&](auto fast, auto s, int kt) __attribute__((always_inline)) {
+    constexpr int S = decltype(s)::value;
+    const char* cur = stage(std::integral_constant<int, S>{});
+#pragma unroll
+    for (int kk = 0; kk + 1 < KS; ++kk) {
+      frags(cur, (kk + 1) & 1, kk + 1);
+      mfmas(kk & 1);
+    }
+    // reads spread ahead of the MFMAs of their step
+#pragma unroll
+    for (int i = 0; i < (KS - 1) * ND; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, NM >= ND ? NM / ND : 1, 0);
+    }
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0<(STAGES - 2) * LPT>());
+    bare_barrier();
+    if constexpr (!decltype(fast)::value)
+      if (a.K % 16 != 0 && kt + 2 == nk) clear_tail(stage(std::integral_constant<int, S + 1>{}));
+    issue(fast, stage(std::integral_constant<int, S>{}), kt + STAGES);
+    frags(stage(std::integral_constant<int, S + 1>{}), 0, 0);
+    mfmas((KS - 1) & 1);
+#pragma unroll
+    for (int i = 0; i < NM; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, (ND + NM - 1) / NM, 0);
+      __builtin_amdgcn_sched_group_barrier(0x020, (LPT + NM - 1) / NM, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    }
+  };
+  auto main_loop = [&](auto fast) __attribute__((always_inline)) {
+    issue(fast, stage(std::integral_constant<int, 0>{}), 0);
+    issue(fast, stage(std::integral_constant<int, 1>{}), 1);
+    if constexpr (STAGES > 2) issue(fast, stage(std::integral_constant<int, 2>{}), 2);
+    if constexpr (STAGES > 3) issue(fast, stage(std::integral_constant<int, 3>{}), 3);
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0<(STAGES - 1) * LPT>());
+    bare_barrier();
+    if constexpr (!decltype(fast)::value)
+      if (a.K % 16 != 0 && nk == 1) clear_tail(st0);
+    frags(st0, 0, 0);
+    int kt = 0;
+    for (; kt + STAGES <= nk; kt += STAGES) {
+      step(fast, std::integral_constant<int, 0>{}, kt);
+      step(fast, std::integral_constant<int, 1>{}, kt + 1);
+      if constexpr (STAGES > 2) step(fast, std::integral_constant<int, 2>{}, kt + 2);
+      if constexpr (STAGES > 3) step(fast, std::integral_constant<int, 3>{}, kt + 3);
+    }
+    if (kt < nk) step(fast, std::integral_constant<int, 0>{}, kt);
+    if constexpr (STAGES > 2)
+      if (kt + 1 < nk) step(fast, std::integral_constant<int, 1>{}, kt + 1);
+    if constexpr (STAGES > 3)
+      if (kt + 2 < nk) step(fast, std::integral_constant<int, 2>{}, kt + 2);
+  };
+  if (a.K % BK == 0)
+    main_loop(std::true_type{});
+  else
+    main_loop(std::false_type{});
+  __builtin_amdgcn_s_waitcnt(0);  // the loads past K land before the LDS is given up
+
+  // lane (l32, g) holds row l32 of each block and the columns 8 q + 4 g + 0..3, and stores
+  // straight from its registers (through LDS, in whole rows of a wavefront's part, the
+  // launches took as long or up to 10 % longer)
+  typedef uint32_t out16 __attribute__((ext_vector_type(4), aligned(2)));
+  constexpr int QS = sizeof(OT) == 2 ? 2 : 1;  // groups of four columns to a store
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int q = 0; q < 4; q += QS) {
+      float sb[4 * QS], bias[4 * QS];
+#pragma unroll
+      for (int r = 0; r < 4 * QS; ++r) {
+        const int from = 8 * (q + (r >> 2)) + 4 * g + (r & 3);
+        sb[r] = __shfl(sb_v[j], from);
+        bias[r] = __shfl(bias_v[j], from);
+      }
+      const int n = n0 + (wn * TN + j) * 32 + 8 * q + (sizeof(OT) == 2 ? 8 * g : 4 * g);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        float v[4 * QS];
+#pragma unroll
+        for (int r = 0; r < 4 * QS; ++r) v[r] = (float)acc[i][j][4 * q + r] * sa_v[i] * sb[r] + bias[r];
+        u32x4 o;
+        if constexpr (sizeof(OT) == 2) {
+          // the lanes l and l + 32 exchange halves: then the first has the eight columns of
+          // group q, the second those of group q + 1
+          auto pack = [&](int r) {
+            return (uint32_t)__builtin_bit_cast(uint16_t, (bf16)v[r]) |
+                   ((uint32_t)__builtin_bit_cast(uint16_t, (bf16)v[r + 1]) << 16);
+          };
+          const auto x = __builtin_amdgcn_permlane32_swap(pack(0), pack(4), false, false);
+          const auto y = __builtin_amdgcn_permlane32_swap(pack(2), pack(6), false, false);
+          o = u32x4{x[0], y[0], x[1], y[1]};
+        } else {
+          o = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        }
+        const int m = m0 + (wm * TM + i) * 32 + l32;
+        OT* const p = (OT*)a.out + (int64_t)m * a.ldo + n;
+        constexpr int E = 16 / (int)sizeof(OT);
+        if (m < a.M && n + E <= a.N) {
+          *(out16*)p = o;
+        } else if (m < a.M) {
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (n + e < a.N) {
+              if constexpr (sizeof(OT) == 2)
+                ((uint16_t*)p)[e] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
+              else
+                ((uint32_t*)p)[e] = o[e];
+            }
         }
       }
     }
-    return v;
-  };
-  for (int k0 = 0; k0 < a.K; k0 += BK) {
-    __syncthreads();
-    for (int c = tid; c < BM * 8; c += 256)
-      *(i32x4*)&As[(c >> 3) * LD + (c & 7) * 16] = chunk(a.A, a.lda, a.M, m0 + (c >> 3), k0 + (c & 7) * 16);
-    for (int c = tid; c < BN * 8; c += 256)
-      *(i32x4*)&Bs[(c >> 3) * LD + (c & 7) * 16] = chunk(a.B, a.ldb, a.N, n0 + (c >> 3), k0 + (c & 7) * 16);
-    __syncthreads();
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      const i32x4 x = *(const i32x4*)&As[(wm * 32 + l32) * LD + kk * 32 + g * 16];
-      const i32x4 y = *(const i32x4*)&Bs[(wn * 32 + l32) * LD + kk * 32 + g * 16];
-      acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(y, x, acc, 0, 0, 0);
-    }
+}
+
+// Tiles: BM x BN, wave grid, LDS stages, wavefronts per SIMD.
+#define SF_I8_TILES(X)               \
+  X(kI8Deep64, 64, 64, 2, 2, 4, 2)   \
+  X(kI8Tile64, 64, 64, 2, 2, 2, 4)   \
+  X(kI8Tile128, 128, 128, 2, 2, 2, 2) \
+  X(kI8Tile128x192, 128, 192, 2, 2, 2, 2) \
+  X(kI8Tile256x192, 256, 192, 4, 2, 2, 2)
+
+template <typename OT>
+static hipError_t launch_i8(const GemmI8Args& a, hipStream_t s) {
+  switch (choose_gemm_i8_tile(a.M, a.N, a.K)) {
+#define SF_I8_CASE(id, bm, bn, wm, wn, st, mw)                                                               \
+  case id: {                                                                                                 \
+    const int64_t tiles = (((int64_t)a.M + bm - 1) / bm) * (((int64_t)a.N + bn - 1) / bn);                   \
+    if (tiles > 0x7fffffff) return hipErrorInvalidValue;                                                     \
+    launch(gemm_i8_kernel<bm, bn, wm, wn, st, mw, OT>, dim3((uint32_t)tiles), dim3(wm * wn * 64), 0, s, a);  \
+    break;                                                                                                   \
   }
-  // lane (l32, g) holds row l32 and the columns 8 q + 4 g + e
-  const int m = m0 + wm * 32 + l32;
-  if (m >= a.M) return;
-  const float sa = a.sa[m];
-#pragma unroll
-  for (int q = 0; q < 4; ++q)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int n = n0 + wn * 32 + q * 8 + g * 4 + e;
-      if (n >= a.N) continue;
-      const float p = (float)acc[4 * q + e] * sa * a.sb[n];
-      ((OT*)a.out)[(int64_t)m * a.ldo + n] = from_f32<OT>(a.bias ? p + a.bias[n] : p);
-    }
+    SF_I8_TILES(SF_I8_CASE)
+#undef SF_I8_CASE
+  }
+  return hipGetLastError();
 }
 
 hipError_t launch_gemm_i8(bool out_bf16, const GemmI8Args& a, hipStream_t s) {
-  const int64_t tiles = (((int64_t)a.M + 63) / 64) * (((int64_t)a.N + 63) / 64);
-  if (tiles > 0x7fffffff) return hipErrorInvalidValue;
-  if (out_bf16)
-    launch(gemm_i8_kernel<bf16>, dim3((uint32_t)tiles), dim3(256), 0, s, a);
-  else
-    launch(gemm_i8_kernel<float>, dim3((uint32_t)tiles), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return out_bf16 ? launch_i8<bf16>(a, s) : launch_i8<float>(a, s);
 }
 
 }  // namespace sf

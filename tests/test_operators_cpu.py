@@ -1,5 +1,7 @@
 """The operators without a model, on the host: what they refuse, before any HIP call."""
 import ctypes
+import os
+import subprocess
 
 import pytest
 
@@ -123,3 +125,44 @@ def test_python_refusals_without_a_gpu():
             Rotary(dims)
     with pytest.raises(ValueError):
         Rotary([8], layout="quarters")
+
+
+TILES = r"""
+#include <cstdio>
+#include "sf_rules.h"
+int main() {
+  const long sizes[] = {1, 2, 31, 64, 65, 129, 777, 1023, 4096, 16384, 70000, 1 << 20, 2147483647L};
+  const long Ks[] = {1, 16, 100, 768, 4321, 131071};
+  int seen[5] = {0, 0, 0, 0, 0};
+  for (long M : sizes)
+    for (long N : sizes)
+      for (long K : Ks) {
+        const int t = (int)sf::choose_gemm_i8_tile(M, N, K);
+        if (t < 0 || t > 4) return std::printf("%ld %ld %ld: %d\n", M, N, K, t), 1;
+        ++seen[t];
+        // one per CU: never more than one round of them
+        if (t == sf::kI8Tile256x192 && ((M + 255) / 256) * ((N + 191) / 192) > 256) return 2;
+        if (M > 60000 && N > 60000 && t != sf::kI8Tile128x192) return std::printf("%ld %ld %ld\n", M, N, K), 3;
+        if (M <= 64 && N <= 4096 && t > sf::kI8Tile64) return std::printf("%ld %ld %ld\n", M, N, K), 4;
+      }
+  const auto at = [](long M, long N, long K) { return (int)sf::choose_gemm_i8_tile(M, N, K); };
+  if (at(4096, 2304, 768) != sf::kI8Tile256x192 || at(16384, 4608, 1152) != sf::kI8Tile128x192 ||
+      at(2048, 2048, 2048) != sf::kI8Tile128 || at(1023, 777, 4321) != sf::kI8Deep64)
+    return 5;
+  std::printf("ok\n");
+  return 0;
+}
+"""
+
+
+def test_choice_of_8_bit_tiles(tmp_path):
+    """Every size gets a tile without an overflow, the largest ones the largest pairs, few rows
+    a small one."""
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2511_22009_amd", "csrc")
+    src, exe = str(tmp_path / "t.cpp"), str(tmp_path / "t")
+    with open(src, "w") as f:
+        f.write(TILES)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover", "-I", csrc, src,
+                    "-o", exe], check=True)
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=60)
+    assert r.returncode == 0, (r.returncode, r.stdout, r.stderr)
