@@ -171,16 +171,16 @@ inline I8Tile choose_gemm_i8_tile(long M, long N, long K) {
                                {kI8Tile128x192, 128, 192, 2, 1204, 6197, 57},
                                {kI8Tile256x192, 256, 192, 1, 915, 6000, 100}};
   const int64_t slices = ((int64_t)K + 127) / 128;
-  int64_t least = -1;
+  double least = -1.0;  // the largest sizes pass 64-bit integers
   I8Tile best = kI8Tile128;
   for (const I8Cost& t : kTiles) {
     const int64_t tiles = (((int64_t)M + t.bm - 1) / t.bm) * (((int64_t)N + t.bn - 1) / t.bn);
     const int64_t k = (tiles + 255) / 256;
     if (t.per == 1 && k > 1) continue;
-    const int64_t all = t.slice * slices + t.once, rest = k % t.per;
+    const int64_t rest = k % t.per;
     const int64_t part = rest ? t.alone + (100 - t.alone) * (rest - 1) / (t.per > 1 ? t.per - 1 : 1) : 0;
-    const int64_t cost = k / t.per * all * 100 + all * part;
-    if (least < 0 || cost < least) {
+    const double cost = (double)(t.slice * slices + t.once) * ((double)(k / t.per) + 0.01 * (double)part);
+    if (least < 0.0 || cost < least) {
       best = t.tile;
       least = cost;
     }
