@@ -6,8 +6,9 @@
 // a wavefront takes 64 / G tokens (G lanes to a head, each with the same E pairs of every
 // head), forms its lanes' angles once and runs over heads with the cosines and sines in
 // registers. The sum of squares of a head is a butterfly over its G lanes.
-#include "sf_device.h"
+#include <cmath>
 
+#include "sf_device.h"
 #include "streamflow.h"
 
 namespace sf {
@@ -28,6 +29,10 @@ __device__ __forceinline__ void turn_angle(double turns, float& c, float& s) {
   s = quarter >= 2.0 ? -b : b;
 }
 
+#ifndef ROPE_WAVES
+#define ROPE_WAVES 8192
+#endif
+
 // Vectors of E adjacent elements at any element's address.
 template <typename T, int E> struct Piece;
 template <> struct Piece<bf16, 8> { typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2))); };
@@ -40,7 +45,6 @@ template <> struct Piece<float, 1> { typedef uint32_t V; };
 // bf16 pairs, the 8 elements at lo at once).
 template <typename T, int E>
 struct Pairs {
-  static constexpr bool kAdj8 = false;
   typename Piece<T, E>::V lo, hi;
   __device__ __forceinline__ void load(const T* p, int l, int h) {
     lo = *(const typename Piece<T, E>::V*)(p + l);
@@ -89,10 +93,10 @@ __device__ __forceinline__ void store(T* p, const float (&f)[E]) {
 }
 
 // E pairs per unit, U units per lane. E = 4 where a unit's elements are adjacent in memory,
-// else 1. ADJ: the layout of adjacent pairs.
+// else 1. ADJ: the layout of adjacent pairs. blockIdx.y picks heads of q or of k, never of both.
 template <typename T, int E, int U, bool ADJ, bool NORM, bool ROT>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
-  constexpr int HB = 2;  // heads whose loads are in flight together
+  constexpr int HB = 4;  // heads whose loads are in flight together
   const int lane = threadIdx.x & 63;
   const int G = 1 << a.group_log2, li = lane & (G - 1);
   const int per_wave = 64 >> a.group_log2;
@@ -103,12 +107,17 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   const bool here = want < total;
   const uint32_t tt = here ? want : total - 1;
   const uint32_t row = fdiv(tt, a.div_tok), tok = tt - row * (uint32_t)a.tokens;
+  const int which = (int)blockIdx.y >= a.splits0;
+  const RopeHeads& t = a.t[which];
+  const int h0 = ((int)blockIdx.y - (which ? a.splits0 : 0)) * a.head_step;
+  const int h1 = min(h0 + a.head_step, which ? a.heads - a.heads0 : a.heads0);
 
-  // this lane's units: where their elements are, and their angles
+  // this lane's units: where their elements are, and what takes a pair (x, y) of the head to
+  // (x xx + y xy, x yx + y yy): the gains and the turn
   const int units = a.dh / (2 * E);
   int lo[U], hi[U];
   bool on[U], turns[U];
-  float cs[U][E], sn[U][E];
+  float xx[U][E], xy[U][E], yx[U][E], yy[U][E];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int unit = li + u * G;
@@ -118,42 +127,64 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     lo[u] = 2 * j0;  // adjacent pairs, and the dims that stay
     hi[u] = lo[u] + E;
 #pragma unroll
-    for (int e = 0; e < E; ++e) cs[u][e] = 1.0f, sn[u][e] = 0.0f;
+    for (int e = 0; e < E; ++e) xx[u][e] = yy[u][e] = 1.0f, xy[u][e] = yx[u][e] = 0.0f;
     if (turns[u]) {
       const float* p = a.pos + (int64_t)row * a.pos_row + (int64_t)tok * a.axes;
+      int was = -1;
+      double f = 0.0, step = 0.0, at = 0.0;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const int j = j0 + e;
         int ax = 0;
 #pragma unroll
         for (int i = 1; i < kRopeAxes; ++i) ax += i < a.axes && j >= a.first[i];
-        // a.first by a dynamic index would go through memory
-        int s0 = a.first[0], s1 = a.first[1];
+        if (ax == was) {
+          f *= step;  // the next pair of the axis
+        } else {
+          // the arrays by a dynamic index would go through memory
+          int s0 = a.first[0], s1 = a.first[1];
+          double rate = a.rate[0];
+          step = a.step[0];
 #pragma unroll
-        for (int i = 1; i < kRopeAxes; ++i)
-          if (ax == i) s0 = a.first[i], s1 = a.first[i + 1];
-        // 2 i / dims = i / (dims / 2)
-        const double x = a.spread ? (double)j / (double)a.pairs : (double)(j - s0) / (double)(s1 - s0);
-        const double f = exp2(-x * a.log2_theta) * 0.15915494309189534;  // turns per position
-        turn_angle((double)p[ax] * f, cs[u][e], sn[u][e]);
-        if (a.inverse) sn[u][e] = -sn[u][e];
-        if (e == 0 && !ADJ) {
-          if (a.layout == SF_ROPE_HALVES) lo[u] = j0, hi[u] = j0 + a.pairs;
-          if (a.layout == SF_ROPE_AXIS_HALVES) lo[u] = s0 + j0, hi[u] = s1 + j0;  // 2 s0 + (j0 - s0), + (s1 - s0)
+          for (int i = 1; i < kRopeAxes; ++i)
+            if (ax == i) s0 = a.first[i], s1 = a.first[i + 1], rate = a.rate[i], step = a.step[i];
+          f = exp2(-rate * (double)(a.spread ? j : j - s0)) * 0.15915494309189534;  // turns per position
+          at = (double)p[ax];
+          was = ax;
+          if (e == 0 && !ADJ) {
+            if (a.layout == SF_ROPE_HALVES) lo[u] = j0, hi[u] = j0 + a.pairs;
+            if (a.layout == SF_ROPE_AXIS_HALVES) lo[u] = s0 + j0, hi[u] = s1 + j0;  // 2 s0 + (j0 - s0), + (s1 - s0)
+          }
+        }
+        float c, s;
+        turn_angle(at * f, c, s);
+        xx[u][e] = yy[u][e] = c;
+        xy[u][e] = a.inverse ? s : -s;
+        yx[u][e] = -xy[u][e];
+      }
+    }
+    if constexpr (NORM) {
+      if (t.gain) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float gx = t.gain[ADJ && E == 4 ? lo[u] + 2 * e : lo[u] + e];
+          const float gy = t.gain[ADJ && E == 4 ? lo[u] + 2 * e + 1 : hi[u] + e];
+          xx[u][e] *= gx;
+          yx[u][e] *= gx;
+          xy[u][e] *= gy;
+          yy[u][e] *= gy;
         }
       }
     }
   }
-  const int h0 = (int)blockIdx.y * a.head_step, h1 = min(h0 + a.head_step, a.heads);
   const float inv_dh = 1.0f / (float)a.dh;
+  const T* const in = (const T*)t.in + (int64_t)row * t.in_row + (int64_t)tok * t.in_tok;
+  T* const out = (T*)t.out + (int64_t)row * t.out_row + (int64_t)tok * t.out_tok;
   for (int hb = h0; hb < h1; hb += HB) {
     Pairs<T, E> raw[HB][U];
 #pragma unroll
     for (int b = 0; b < HB; ++b) {
-      const int h = min(hb + b, h1 - 1);
-      const RopeHeads& t = a.t[h >= a.heads0];
-      const T* p = (const T*)t.in + (int64_t)row * t.in_row + (int64_t)tok * t.in_tok +
-                   (int64_t)(h >= a.heads0 ? h - a.heads0 : h) * t.in_head;
+      const T* p = in + (int64_t)min(hb + b, h1 - 1) * t.in_head;
 #pragma unroll
       for (int u = 0; u < U; ++u) raw[b][u].load(p, lo[u], hi[u]);
     }
@@ -161,7 +192,6 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     for (int b = 0; b < HB; ++b) {
       const int h = hb + b;
       if (h >= h1) break;
-      const RopeHeads& t = a.t[h >= a.heads0];
       float x[U][E], y[U][E];
       float ss = 0.0f;
 #pragma unroll
@@ -177,12 +207,13 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
           for (int e = 0; e < E; ++e) x[u][e] = p[e], y[u][e] = q[e];
         }
         if constexpr (NORM) {
-          if (on[u]) {
+          float mine = 0.0f;
 #pragma unroll
-            for (int e = 0; e < E; ++e) ss += x[u][e] * x[u][e] + y[u][e] * y[u][e];
-          }
+          for (int e = 0; e < E; ++e) mine += x[u][e] * x[u][e] + y[u][e] * y[u][e];
+          ss += on[u] ? mine : 0.0f;
         }
       }
+      float r = 1.0f;
       if constexpr (NORM) {
         if (G > 1) ss += lane_xor<1>(ss);
         if (G > 2) ss += lane_xor<2>(ss);
@@ -190,32 +221,18 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
         if (G > 8) ss += lane_xor<8>(ss);
         if (G > 16) ss += lane_xor<16>(ss);
         if (G > 32) ss += lane_xor<32>(ss);
-        const float r = 1.0f / sqrtf(ss * inv_dh + a.eps);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            x[u][e] *= r;
-            y[u][e] *= r;
-            if (t.gain) {
-              const int dx = ADJ && E == 4 ? lo[u] + 2 * e : lo[u] + e;
-              const int dy = ADJ && E == 4 ? lo[u] + 2 * e + 1 : hi[u] + e;
-              x[u][e] *= t.gain[dx];
-              y[u][e] *= t.gain[dy];
-            }
-          }
+        r = 1.0f / sqrtf(ss * inv_dh + a.eps);
       }
-      T* out = (T*)t.out + (int64_t)row * t.out_row + (int64_t)tok * t.out_tok +
-               (int64_t)(h >= a.heads0 ? h - a.heads0 : h) * t.out_head;
+      T* const o = out + (int64_t)h * t.out_head;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         float p[E], q[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const float px = turns[u] ? x[u][e] * cs[u][e] - y[u][e] * sn[u][e] : x[u][e];
-          const float py = turns[u] ? x[u][e] * sn[u][e] + y[u][e] * cs[u][e] : y[u][e];
-          p[e] = px;
-          q[e] = py;
+          if constexpr (NORM) x[u][e] *= r, y[u][e] *= r;
+          // a dim that stays is not touched by its neighbour, which may be infinite
+          p[e] = turns[u] ? x[u][e] * xx[u][e] + y[u][e] * xy[u][e] : x[u][e] * xx[u][e];
+          q[e] = turns[u] ? x[u][e] * yx[u][e] + y[u][e] * yy[u][e] : y[u][e] * yy[u][e];
         }
         if constexpr (ADJ && E == 4) {
           const float lo4[4] = {p[0], q[0], p[1], q[1]}, hi4[4] = {p[2], q[2], p[3], q[3]};
@@ -223,8 +240,13 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
           for (int e = 0; e < 4; ++e) p[e] = lo4[e], q[e] = hi4[e];
         }
         if (here && on[u]) {
-          store<T, E>(out + lo[u], p);
-          store<T, E>(out + hi[u], q);
+          if constexpr (ADJ && E == 4 && sizeof(T) == 2) {
+            const float all[8] = {p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]};
+            store<T, 8>(o + lo[u], all);
+          } else {
+            store<T, E>(o + lo[u], p);
+            store<T, E>(o + hi[u], q);
+          }
         }
       }
     }
@@ -254,13 +276,21 @@ hipError_t launch_rope(bool is_bf16, bool norm, bool rotate, RopeArgs a, hipStre
   const int lanes = whole ? a.dh / 8 : (a.dh / 2 + 1) / 2;
   a.group_log2 = 0;
   while ((1 << a.group_log2) < lanes) ++a.group_log2;
+  for (int i = 0; i < a.axes; ++i) {
+    // frequencies fall by 2^rate from pair to pair
+    const int n = a.spread ? a.pairs : a.first[i + 1] - a.first[i];
+    a.rate[i] = n > 0 ? a.log2_theta / n : 0.0;
+    a.step[i] = exp2(-a.rate[i]);
+  }
   const int64_t per_wave = 64 >> a.group_log2;
   const int64_t waves = ((int64_t)a.rows * a.tokens + per_wave - 1) / per_wave;
-  // heads are split over wavefronts while there are fewer than eight per CU
-  int64_t splits = (2048 + waves - 1) / waves;
+  // heads are split over wavefronts while there are fewer than kWaves of them
+  int64_t splits = (ROPE_WAVES + waves - 1) / waves;
   if (splits > a.heads) splits = a.heads;
   a.head_step = (int)((a.heads + splits - 1) / splits);
-  const dim3 grid((uint32_t)((waves + 3) / 4), (uint32_t)((a.heads + a.head_step - 1) / a.head_step));
+  a.splits0 = (a.heads0 + a.head_step - 1) / a.head_step;
+  const int splits1 = (a.heads - a.heads0 + a.head_step - 1) / a.head_step;
+  const dim3 grid((uint32_t)((waves + 3) / 4), (uint32_t)(a.splits0 + splits1));
   if (is_bf16) {
     if (norm) return rotate ? launch_rope_as<bf16, true, true>(a, whole, grid, s) : launch_rope_as<bf16, true, false>(a, whole, grid, s);
     return launch_rope_as<bf16, false, true>(a, whole, grid, s);

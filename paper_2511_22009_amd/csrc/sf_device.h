@@ -257,12 +257,34 @@ __device__ __forceinline__ RowQuant row_quant(uint32_t top_bits) {
 // 2^-15 of a half. Then the quotient decides, in fp64: 127 x is exact there, and a quotient
 // of at least 1/2 that is not itself a half differs from one by at least 2^-33 (x and top
 // have 24-bit significands, and x is at least top / 254), far above the division's rounding.
+constexpr float kQuantSure = 0.5f - 0x1p-15f;
+__device__ __forceinline__ int quant_code_exact(float x, const RowQuant& r) {
+  return r.top > 0.0f ? (int)rint((double)x * 127.0 / (double)r.top) : 0;
+}
 __device__ __forceinline__ int quant_code(float x, const RowQuant& r) {
-  const float y = x * r.inv;
-  float q = rintf(y);
-  if (!(fabsf(y - q) < 0.5f - 0x1p-15f) || r.inv == 0.0f)
-    q = r.top > 0.0f ? (float)rint((double)x * 127.0 / (double)r.top) : 0.0f;
-  return (int)q;
+  const float y = x * r.inv, q = rintf(y);
+  return fabsf(y - q) < kQuantSure && r.inv != 0.0f ? (int)q : quant_code_exact(x, r);
+}
+// Eight codes, first in the low byte. y + 1.5 2^23 rounds y to a whole number, ties to even, and
+// has its low byte in its own.
+__device__ __forceinline__ uint2 quant_codes8(const float (&x)[8], const RowQuant& r) {
+  constexpr float kWhole = 12582912.0f;
+  uint32_t b[8];
+  float off = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float y = x[e] * r.inv, t = y + kWhole;
+    off = fmaxf(off, fabsf(y - (t - kWhole)));
+    b[e] = __float_as_uint(t);
+  }
+  if (!(off < kQuantSure) || r.inv == 0.0f) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) b[e] = (uint32_t)quant_code_exact(x[e], r);
+  }
+  // bytes: __builtin_amdgcn_perm(hi, lo, sel) takes 0..3 from lo and 4..7 from hi
+  const uint32_t p0 = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), p1 = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0cu);
+  const uint32_t p2 = __builtin_amdgcn_perm(b[5], b[4], 0x0c0c0400u), p3 = __builtin_amdgcn_perm(b[7], b[6], 0x04000c0cu);
+  return uint2{p0 | p1, p2 | p3};
 }
 
 }  // namespace sf

@@ -283,11 +283,13 @@ struct RopeArgs {
   int inverse;
   const float* pos;     // [rows][tokens][axes]
   int64_t pos_row;
+  // filled in by launch_rope
+  double rate[kRopeAxes], step[kRopeAxes];  // log2 of theta per pair of an axis; 2^-rate
   int head_step;        // heads of a wavefront
+  int splits0;          // wavefronts that share a token's heads of q
   int group_log2;       // lanes that share a head: 2^group_log2
 };
 // norm: divide by the root mean square and multiply by the gain; rotate: turn the pairs.
-// Fills in heads per wavefront and lanes per head.
 hipError_t launch_rope(bool is_bf16, bool norm, bool rotate, RopeArgs a, hipStream_t s);
 
 }  // namespace sf
