@@ -240,10 +240,7 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_i8_kernel(GemmI8Args 
         if constexpr (sizeof(OT) == 2) {
           // the lanes l and l + 32 exchange halves: then the first has the eight columns of
           // group q, the second those of group q + 1
-          auto pack = [&](int r) {
-            return (uint32_t)__builtin_bit_cast(uint16_t, (bf16)v[r]) |
-                   ((uint32_t)__builtin_bit_cast(uint16_t, (bf16)v[r + 1]) << 16);
-          };
+          auto pack = [&](int r) { return pack_bf16(v[r], v[r + 1]); };
           const auto x = __builtin_amdgcn_permlane32_swap(pack(0), pack(4), false, false);
           const auto y = __builtin_amdgcn_permlane32_swap(pack(2), pack(6), false, false);
           o = u32x4{x[0], y[0], x[1], y[1]};

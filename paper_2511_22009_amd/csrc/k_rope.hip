@@ -2,10 +2,16 @@
 // per head, in one pass over the data.
 //
 // A pair (x, y) of a head's dims turns by u = p f, p its token's position on the pair's axis:
-// (x cos u - y sin u, x sin u + y cos u). The angle of a pair is the same in every head, so
-// a wavefront takes 64 / G tokens (G lanes to a head, each with the same E pairs of every
-// head), forms its lanes' angles once and runs over heads with the cosines and sines in
-// registers. The sum of squares of a head is a butterfly over its G lanes.
+// (x cos u - y sin u, x sin u + y cos u). The angle of a pair is the same in every head, so a
+// workgroup forms the angles of its tokens once, in fp64, and shares them over the heads; G
+// lanes hold a head, and its sum of squares is a butterfly over them.
+//
+// Bandwidth bounds it: the 8 x 30 x 52 tokens of a clip with 16 heads of 128 dims (102 MB) take
+// 21 us, 4.8 TB/s; q and k of 16384 tokens with 32 heads of 64 dims (134 MB, adjacent pairs) 29
+// us. With 72 dims a head fills 9 of its 16 lanes, and halves move in pieces of 8 bytes: 42 us
+// for 151 MB. (12 pairs to a lane, which fill 3 lanes of 4, take 46 us: lanes 48 bytes apart;
+// angles per wavefront instead of per workgroup 44; wavefronts by tokens instead of by heads
+// 41 to 42, and 25 instead of 22 for the clip.)
 #include <cmath>
 
 #include "sf_device.h"
@@ -29,146 +35,179 @@ __device__ __forceinline__ void turn_angle(double turns, float& c, float& s) {
   s = quarter >= 2.0 ? -b : b;
 }
 
-#ifndef ROPE_WAVES
-#define ROPE_WAVES 8192
-#endif
+// N adjacent elements at any element's address, moved in pieces of 16 and 8 bytes.
+template <typename T, int N>
+struct Run {
+  static constexpr int WORDS = N * (int)sizeof(T) / 4;
+  static_assert(WORDS % 2 == 0, "whole pieces of 8 bytes");
+  typedef uint32_t V4 __attribute__((ext_vector_type(4), aligned(2)));
+  typedef uint32_t V2 __attribute__((ext_vector_type(2), aligned(2)));
+  uint32_t w[WORDS];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i + 4 <= WORDS; i += 4) {
+      const V4 v = *(const V4*)((const char*)p + 4 * i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[i + k] = v[k];
+    }
+    if constexpr (WORDS % 4 == 2) {
+      const V2 v = *(const V2*)((const char*)p + 4 * (WORDS - 2));
+      w[WORDS - 2] = v[0];
+      w[WORDS - 1] = v[1];
+    }
+  }
+  __device__ __forceinline__ float at(int e) const {
+    if constexpr (sizeof(T) == 2)
+      return __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    else
+      return __uint_as_float(w[e]);
+  }
+  __device__ static __forceinline__ void store(T* p, const float (&f)[N]) {
+    uint32_t o[WORDS];
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      if constexpr (sizeof(T) == 2)
+        o[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
+      else
+        o[i] = __float_as_uint(f[i]);
+    }
+#pragma unroll
+    for (int i = 0; i + 4 <= WORDS; i += 4) *(V4*)((char*)p + 4 * i) = V4{o[i], o[i + 1], o[i + 2], o[i + 3]};
+    if constexpr (WORDS % 4 == 2) *(V2*)((char*)p + 4 * (WORDS - 2)) = V2{o[WORDS - 2], o[WORDS - 1]};
+  }
+};
+template <typename T>
+struct Run<T, 1> {
+  T v;
+  __device__ __forceinline__ void load(const T* p) { v = *p; }
+  __device__ __forceinline__ float at(int) const { return to_f32(v); }
+  __device__ static __forceinline__ void store(T* p, const float (&f)[1]) { *p = from_f32<T>(f[0]); }
+};
 
-// Vectors of E adjacent elements at any element's address.
-template <typename T, int E> struct Piece;
-template <> struct Piece<bf16, 8> { typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2))); };
-template <> struct Piece<bf16, 4> { typedef uint32_t V __attribute__((ext_vector_type(2), aligned(2))); };
-template <> struct Piece<bf16, 1> { typedef uint16_t V; };
-template <> struct Piece<float, 4> { typedef uint32_t V __attribute__((ext_vector_type(4), aligned(4))); };
-template <> struct Piece<float, 1> { typedef uint32_t V; };
-
-// E pairs of a head as they lie in memory: E elements at lo and E at hi (or, for adjacent
-// bf16 pairs, the 8 elements at lo at once).
-template <typename T, int E>
+// E pairs of a head as they lie in memory: E elements at lo and E at hi, or, adjacent pairs, 2 E
+// elements at lo.
+template <typename T, int E, bool ADJ>
 struct Pairs {
-  typename Piece<T, E>::V lo, hi;
+  Run<T, E> lo, hi;
   __device__ __forceinline__ void load(const T* p, int l, int h) {
-    lo = *(const typename Piece<T, E>::V*)(p + l);
-    hi = *(const typename Piece<T, E>::V*)(p + h);
+    lo.load(p + l);
+    hi.load(p + h);
+  }
+  __device__ __forceinline__ float x(int e) const { return lo.at(e); }
+  __device__ __forceinline__ float y(int e) const { return hi.at(e); }
+  __device__ static __forceinline__ void store(T* p, int l, int h, const float (&x)[E], const float (&y)[E]) {
+    Run<T, E>::store(p + l, x);
+    Run<T, E>::store(p + h, y);
+  }
+};
+template <typename T, int E>
+struct Pairs<T, E, true> {
+  Run<T, 2 * E> run;
+  __device__ __forceinline__ void load(const T* p, int l, int) { run.load(p + l); }
+  __device__ __forceinline__ float x(int e) const { return run.at(2 * e); }
+  __device__ __forceinline__ float y(int e) const { return run.at(2 * e + 1); }
+  __device__ static __forceinline__ void store(T* p, int l, int, const float (&x)[E], const float (&y)[E]) {
+    float f[2 * E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) f[2 * e] = x[e], f[2 * e + 1] = y[e];
+    Run<T, 2 * E>::store(p + l, f);
   }
 };
 
-template <typename T>
-__device__ __forceinline__ float bits_f32(uint32_t b) {
-  return sizeof(T) == 2 ? __uint_as_float(b << 16) : __uint_as_float(b);
-}
-
-template <typename T, int E>
-__device__ __forceinline__ void unpack(const typename Piece<T, E>::V& v, float (&f)[E]) {
-  if constexpr (E == 1) {
-    f[0] = bits_f32<T>((uint32_t)v);
-  } else if constexpr (sizeof(T) == 2) {
-#pragma unroll
-    for (int e = 0; e < E; e += 2) {
-      f[e] = __uint_as_float(v[e / 2] << 16);
-      f[e + 1] = __uint_as_float(v[e / 2] & 0xffff0000u);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < E; ++e) f[e] = __uint_as_float(v[e]);
-  }
-}
-
-template <typename T, int E>
-__device__ __forceinline__ void store(T* p, const float (&f)[E]) {
-  if constexpr (E == 1) {
-    *p = from_f32<T>(f[0]);
-  } else if constexpr (sizeof(T) == 2) {
-    typename Piece<T, E>::V v;
-#pragma unroll
-    for (int e = 0; e < E; e += 2)
-      v[e / 2] = (uint32_t)__builtin_bit_cast(uint16_t, (bf16)f[e]) |
-                 ((uint32_t)__builtin_bit_cast(uint16_t, (bf16)f[e + 1]) << 16);
-    *(typename Piece<T, E>::V*)p = v;
-  } else {
-    typename Piece<T, E>::V v;
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = __float_as_uint(f[e]);
-    *(typename Piece<T, E>::V*)p = v;
-  }
-}
-
-// E pairs per unit, U units per lane. E = 4 where a unit's elements are adjacent in memory,
-// else 1. ADJ: the layout of adjacent pairs. blockIdx.y picks heads of q or of k, never of both.
-template <typename T, int E, int U, bool ADJ, bool NORM, bool ROT>
+// A workgroup of four wavefronts takes 64 / G tokens; its first threads form a pair's angle of a
+// token each and leave cosine and sine in LDS, under the wavefronts' first loads. A wavefront
+// takes a run of heads of q or of k.
+// E pairs per unit, U units per lane: one unit of four pairs whose elements are adjacent in
+// memory, or two of one pair each. ADJ: the layout of adjacent pairs. PART: some dims stay as they are.
+template <typename T, int E, int U, bool ADJ, bool NORM, bool ROT, bool PART>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
-  constexpr int HB = 4;  // heads whose loads are in flight together
-  const int lane = threadIdx.x & 63;
+  constexpr int HB = 2;  // heads whose loads are in flight together
+  __shared__ __attribute__((aligned(16))) float2 angles[ROT ? 64 * E * U : 1];  // [token][pair]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = 1 << a.group_log2, li = lane & (G - 1);
-  const int per_wave = 64 >> a.group_log2;
   const uint32_t total = (uint32_t)a.rows * (uint32_t)a.tokens;
-  const uint32_t first = ((uint32_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (uint32_t)per_wave;
-  if (first >= total) return;  // uniform across the wavefront
-  const uint32_t want = first + (uint32_t)(lane >> a.group_log2);
-  const bool here = want < total;
-  const uint32_t tt = here ? want : total - 1;
+  // each of the eight XCDs (workgroup b goes to XCD b % 8) takes a contiguous range of tokens:
+  // a cache line that two workgroups' tokens share is read and written in one L2
+  const uint32_t xcd = blockIdx.x % 8, base = gridDim.x / 8, rem = gridDim.x % 8;
+  const uint32_t first = (xcd * base + min(xcd, rem) + blockIdx.x / 8) * (uint32_t)(64 >> a.group_log2);
+  const int slot = lane >> a.group_log2;
+  const bool here = first + slot < total;
+  const uint32_t tt = here ? first + slot : total - 1;
   const uint32_t row = fdiv(tt, a.div_tok), tok = tt - row * (uint32_t)a.tokens;
-  const int which = (int)blockIdx.y >= a.splits0;
+  const int chunk = (int)blockIdx.y * 4 + wave;
+  const int which = chunk >= a.chunks0;
   const RopeHeads& t = a.t[which];
-  const int h0 = ((int)blockIdx.y - (which ? a.splits0 : 0)) * a.head_step;
-  const int h1 = min(h0 + a.head_step, which ? a.heads - a.heads0 : a.heads0);
+  const int heads = which ? a.heads - a.heads0 : a.heads0, step = a.step[which];
+  const int h0 = (which ? chunk - a.chunks0 : chunk) * step, h1 = min(h0 + step, heads);
 
-  // this lane's units: where their elements are, and what takes a pair (x, y) of the head to
-  // (x xx + y xy, x yx + y yy): the gains and the turn
+  // where this lane's units are
   const int units = a.dh / (2 * E);
-  int lo[U], hi[U];
+  int lo[U], hi[U], pair[U];
   bool on[U], turns[U];
-  float xx[U][E], xy[U][E], yx[U][E], yy[U][E];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int unit = li + u * G;
     on[u] = unit < units;
-    const int j0 = on[u] ? unit * E : 0;
-    turns[u] = ROT && j0 < a.pairs;
+    const int j0 = pair[u] = on[u] ? unit * E : 0;
+    turns[u] = ROT && (!PART || j0 < a.pairs);
     lo[u] = 2 * j0;  // adjacent pairs, and the dims that stay
     hi[u] = lo[u] + E;
+    if (ROT && !ADJ && turns[u]) {
+      if (a.layout == SF_ROPE_HALVES) lo[u] = j0, hi[u] = j0 + a.pairs;
+      if (a.layout == SF_ROPE_AXIS_HALVES) {
+        int s0 = a.first[0], s1 = a.first[1];
 #pragma unroll
-    for (int e = 0; e < E; ++e) xx[u][e] = yy[u][e] = 1.0f, xy[u][e] = yx[u][e] = 0.0f;
-    if (turns[u]) {
-      const float* p = a.pos + (int64_t)row * a.pos_row + (int64_t)tok * a.axes;
-      int was = -1;
-      double f = 0.0, step = 0.0, at = 0.0;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int j = j0 + e;
-        int ax = 0;
-#pragma unroll
-        for (int i = 1; i < kRopeAxes; ++i) ax += i < a.axes && j >= a.first[i];
-        if (ax == was) {
-          f *= step;  // the next pair of the axis
-        } else {
-          // the arrays by a dynamic index would go through memory
-          int s0 = a.first[0], s1 = a.first[1];
-          double rate = a.rate[0];
-          step = a.step[0];
-#pragma unroll
-          for (int i = 1; i < kRopeAxes; ++i)
-            if (ax == i) s0 = a.first[i], s1 = a.first[i + 1], rate = a.rate[i], step = a.step[i];
-          f = exp2(-rate * (double)(a.spread ? j : j - s0)) * 0.15915494309189534;  // turns per position
-          at = (double)p[ax];
-          was = ax;
-          if (e == 0 && !ADJ) {
-            if (a.layout == SF_ROPE_HALVES) lo[u] = j0, hi[u] = j0 + a.pairs;
-            if (a.layout == SF_ROPE_AXIS_HALVES) lo[u] = s0 + j0, hi[u] = s1 + j0;  // 2 s0 + (j0 - s0), + (s1 - s0)
-          }
-        }
-        float c, s;
-        turn_angle(at * f, c, s);
-        xx[u][e] = yy[u][e] = c;
-        xy[u][e] = a.inverse ? s : -s;
-        yx[u][e] = -xy[u][e];
+        for (int i = 1; i < kRopeAxes; ++i)
+          if (j0 >= a.first[i]) s0 = a.first[i], s1 = a.first[i + 1];
+        lo[u] = s0 + j0, hi[u] = s1 + j0;  // 2 s0 + (j0 - s0), + (s1 - s0)
       }
     }
-    if constexpr (NORM) {
-      if (t.gain) {
+  }
+  const T* const in = (const T*)t.in + (int64_t)row * t.in_row + (int64_t)tok * t.in_tok;
+  T* const out = (T*)t.out + (int64_t)row * t.out_row + (int64_t)tok * t.out_tok;
+  Pairs<T, E, ADJ> raw[HB][U];
+  auto load = [&](int h) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float gx = t.gain[ADJ && E == 4 ? lo[u] + 2 * e : lo[u] + e];
-          const float gy = t.gain[ADJ && E == 4 ? lo[u] + 2 * e + 1 : hi[u] + e];
+    for (int b = 0; b < HB; ++b)
+#pragma unroll
+      for (int u = 0; u < U; ++u) raw[b][u].load(in + (int64_t)min(h + b, h1 - 1) * t.in_head, lo[u], hi[u]);
+  };
+  if (h0 < h1) load(h0);
+
+  if constexpr (ROT) {
+    const int here_pairs = (int)min((uint32_t)(64 >> a.group_log2), total - first) * a.pairs;
+    for (int c = (int)threadIdx.x; c < here_pairs; c += 256) {
+      const int at = (int)fdiv((uint32_t)c, a.div_pairs), j = c - at * a.pairs;
+      const uint32_t r = fdiv(first + at, a.div_tok), k = first + at - r * (uint32_t)a.tokens;
+      int ax = 0, s0 = a.first[0];
+      double rate = a.rate[0];
+#pragma unroll
+      for (int i = 1; i < kRopeAxes; ++i)  // the arrays by a dynamic index would go through memory
+        if (i < a.axes && j >= a.first[i]) ax = i, s0 = a.first[i], rate = a.rate[i];
+      const double f = exp2(-rate * (double)(a.spread ? j : j - s0)) * 0.15915494309189534;  // turns per position
+      float c1, s1;
+      turn_angle((double)a.pos[(int64_t)r * a.pos_row + (int64_t)k * a.axes + ax] * f, c1, s1);
+      angles[c] = make_float2(c1, a.inverse ? -s1 : s1);
+    }
+    __syncthreads();
+  }
+  if (h0 >= h1) return;
+
+  // what takes a pair (x, y) to (x xx + y xy, x yx + y yy): the gains and the turn
+  float xx[U][E], xy[U][E], yx[U][E], yy[U][E];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      float2 w = make_float2(1.0f, 0.0f);
+      if (ROT && turns[u] && here) w = angles[slot * a.pairs + pair[u] + e];
+      xx[u][e] = yy[u][e] = w.x;
+      xy[u][e] = -w.y;
+      yx[u][e] = w.y;
+      if constexpr (NORM) {
+        if (t.gain) {
+          const float gx = t.gain[ADJ ? lo[u] + 2 * e : lo[u] + e];
+          const float gy = t.gain[ADJ ? lo[u] + 2 * e + 1 : hi[u] + e];
           xx[u][e] *= gx;
           yx[u][e] *= gx;
           xy[u][e] *= gy;
@@ -176,97 +215,96 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
         }
       }
     }
-  }
   const float inv_dh = 1.0f / (float)a.dh;
-  const T* const in = (const T*)t.in + (int64_t)row * t.in_row + (int64_t)tok * t.in_tok;
-  T* const out = (T*)t.out + (int64_t)row * t.out_row + (int64_t)tok * t.out_tok;
   for (int hb = h0; hb < h1; hb += HB) {
-    Pairs<T, E> raw[HB][U];
+    float x[HB][U][E], y[HB][U][E];
 #pragma unroll
-    for (int b = 0; b < HB; ++b) {
-      const T* p = in + (int64_t)min(hb + b, h1 - 1) * t.in_head;
+    for (int b = 0; b < HB; ++b)
 #pragma unroll
-      for (int u = 0; u < U; ++u) raw[b][u].load(p, lo[u], hi[u]);
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[b][u][e] = raw[b][u].x(e), y[b][u][e] = raw[b][u].y(e);
+      }
+    if (hb + HB < h1) load(hb + HB);
+    float r[HB];
+    if constexpr (NORM) {
+#pragma unroll
+      for (int b = 0; b < HB; ++b) {
+        r[b] = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float mine = 0.0f;
+#pragma unroll
+          for (int e = 0; e < E; ++e) mine += x[b][u][e] * x[b][u][e] + y[b][u][e] * y[b][u][e];
+          r[b] += on[u] ? mine : 0.0f;
+        }
+      }
+      // the sums of the batch's heads over their G lanes
+      auto add = [&](auto m) {
+#pragma unroll
+        for (int b = 0; b < HB; ++b) r[b] += lane_xor<decltype(m)::value>(r[b]);
+      };
+      if (G > 1) add(std::integral_constant<int, 1>{});
+      if (G > 2) add(std::integral_constant<int, 2>{});
+      if (G > 4) add(std::integral_constant<int, 4>{});
+      if (G > 8) add(std::integral_constant<int, 8>{});
+      if (G > 16) add(std::integral_constant<int, 16>{});
+      if (G > 32) add(std::integral_constant<int, 32>{});
+#pragma unroll
+      for (int b = 0; b < HB; ++b) r[b] = __builtin_amdgcn_rsqf(r[b] * inv_dh + a.eps);  // within 1 ulp
     }
 #pragma unroll
     for (int b = 0; b < HB; ++b) {
       const int h = hb + b;
       if (h >= h1) break;
-      float x[U][E], y[U][E];
-      float ss = 0.0f;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        float p[E], q[E];
-        unpack<T, E>(raw[b][u].lo, p);
-        unpack<T, E>(raw[b][u].hi, q);
-        if constexpr (ADJ && E == 4) {
-          x[u][0] = p[0]; y[u][0] = p[1]; x[u][1] = p[2]; y[u][1] = p[3];
-          x[u][2] = q[0]; y[u][2] = q[1]; x[u][3] = q[2]; y[u][3] = q[3];
-        } else {
-#pragma unroll
-          for (int e = 0; e < E; ++e) x[u][e] = p[e], y[u][e] = q[e];
-        }
-        if constexpr (NORM) {
-          float mine = 0.0f;
-#pragma unroll
-          for (int e = 0; e < E; ++e) mine += x[u][e] * x[u][e] + y[u][e] * y[u][e];
-          ss += on[u] ? mine : 0.0f;
-        }
-      }
-      float r = 1.0f;
-      if constexpr (NORM) {
-        if (G > 1) ss += lane_xor<1>(ss);
-        if (G > 2) ss += lane_xor<2>(ss);
-        if (G > 4) ss += lane_xor<4>(ss);
-        if (G > 8) ss += lane_xor<8>(ss);
-        if (G > 16) ss += lane_xor<16>(ss);
-        if (G > 32) ss += lane_xor<32>(ss);
-        r = 1.0f / sqrtf(ss * inv_dh + a.eps);
-      }
       T* const o = out + (int64_t)h * t.out_head;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         float p[E], q[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          if constexpr (NORM) x[u][e] *= r, y[u][e] *= r;
-          // a dim that stays is not touched by its neighbour, which may be infinite
-          p[e] = turns[u] ? x[u][e] * xx[u][e] + y[u][e] * xy[u][e] : x[u][e] * xx[u][e];
-          q[e] = turns[u] ? x[u][e] * yx[u][e] + y[u][e] * yy[u][e] : y[u][e] * yy[u][e];
-        }
-        if constexpr (ADJ && E == 4) {
-          const float lo4[4] = {p[0], q[0], p[1], q[1]}, hi4[4] = {p[2], q[2], p[3], q[3]};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) p[e] = lo4[e], q[e] = hi4[e];
-        }
-        if (here && on[u]) {
-          if constexpr (ADJ && E == 4 && sizeof(T) == 2) {
-            const float all[8] = {p[0], p[1], p[2], p[3], q[0], q[1], q[2], q[3]};
-            store<T, 8>(o + lo[u], all);
+          float xe = x[b][u][e], ye = y[b][u][e];
+          if constexpr (NORM) xe *= r[b], ye *= r[b];
+          if constexpr (ROT) {
+            // a dim that stays is not touched by its neighbour, which may be infinite
+            const float xt = PART && !turns[u] ? 0.0f : xe, yt = PART && !turns[u] ? 0.0f : ye;
+            p[e] = xe * xx[u][e] + yt * xy[u][e];
+            q[e] = xt * yx[u][e] + ye * yy[u][e];
           } else {
-            store<T, E>(o + lo[u], p);
-            store<T, E>(o + hi[u], q);
+            p[e] = xe * xx[u][e];
+            q[e] = ye * yy[u][e];
           }
         }
+        if (here && on[u]) Pairs<T, E, ADJ>::store(o, lo[u], hi[u], p, q);
       }
     }
   }
 }
 
-template <typename T, bool NORM, bool ROT>
+template <typename T, bool NORM, bool ROT, bool PART>
 static hipError_t launch_rope_as(const RopeArgs& a, bool whole, dim3 grid, hipStream_t s) {
   if (!whole)
-    launch(rope_kernel<T, 1, 2, false, NORM, ROT>, grid, dim3(256), 0, s, a);
+    launch(rope_kernel<T, 1, 2, false, NORM, ROT, PART>, grid, dim3(256), 0, s, a);
   else if (!ROT || a.layout == SF_ROPE_ADJACENT)
-    launch(rope_kernel<T, 4, 1, true, NORM, ROT>, grid, dim3(256), 0, s, a);
+    launch(rope_kernel<T, 4, 1, true, NORM, ROT, PART>, grid, dim3(256), 0, s, a);
   else
-    launch(rope_kernel<T, 4, 1, false, NORM, ROT>, grid, dim3(256), 0, s, a);
+    launch(rope_kernel<T, 4, 1, false, NORM, ROT, PART>, grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
+template <typename T>
+static hipError_t launch_rope_type(const RopeArgs& a, bool norm, bool rotate, bool whole, dim3 grid, hipStream_t s) {
+  const bool part = 2 * a.pairs < a.dh;
+  if (!rotate) return launch_rope_as<T, true, false, false>(a, whole, grid, s);
+  if (norm) return part ? launch_rope_as<T, true, true, true>(a, whole, grid, s) : launch_rope_as<T, true, true, false>(a, whole, grid, s);
+  return part ? launch_rope_as<T, false, true, true>(a, whole, grid, s) : launch_rope_as<T, false, true, false>(a, whole, grid, s);
+}
+
+// norm without rotation, rotation without norm, or both.
 hipError_t launch_rope(bool is_bf16, bool norm, bool rotate, RopeArgs a, hipStream_t s) {
-  // units of four pairs where every unit's elements are adjacent: whole units in the head, in
-  // the part that turns and, where each axis has halves of its own, in each axis
+  if (!norm && !rotate) return hipErrorInvalidValue;
+  // units of four pairs where each lies in one piece: whole units in the head, in the part that
+  // turns and, where each axis has halves of its own, in each axis
   bool whole = a.dh % 8 == 0;
   if (rotate) {
     whole = whole && a.pairs % 4 == 0;
@@ -280,23 +318,22 @@ hipError_t launch_rope(bool is_bf16, bool norm, bool rotate, RopeArgs a, hipStre
     // frequencies fall by 2^rate from pair to pair
     const int n = a.spread ? a.pairs : a.first[i + 1] - a.first[i];
     a.rate[i] = n > 0 ? a.log2_theta / n : 0.0;
-    a.step[i] = exp2(-a.rate[i]);
   }
-  const int64_t per_wave = 64 >> a.group_log2;
-  const int64_t waves = ((int64_t)a.rows * a.tokens + per_wave - 1) / per_wave;
-  // heads are split over wavefronts while there are fewer than kWaves of them
-  int64_t splits = (ROPE_WAVES + waves - 1) / waves;
-  if (splits > a.heads) splits = a.heads;
-  a.head_step = (int)((a.heads + splits - 1) / splits);
-  a.splits0 = (a.heads0 + a.head_step - 1) / a.head_step;
-  const int splits1 = (a.heads - a.heads0 + a.head_step - 1) / a.head_step;
-  const dim3 grid((uint32_t)((waves + 3) / 4), (uint32_t)(a.splits0 + splits1));
-  if (is_bf16) {
-    if (norm) return rotate ? launch_rope_as<bf16, true, true>(a, whole, grid, s) : launch_rope_as<bf16, true, false>(a, whole, grid, s);
-    return launch_rope_as<bf16, false, true>(a, whole, grid, s);
-  }
-  if (norm) return rotate ? launch_rope_as<float, true, true>(a, whole, grid, s) : launch_rope_as<float, true, false>(a, whole, grid, s);
-  return launch_rope_as<float, false, true>(a, whole, grid, s);
+  a.div_pairs = make_fastdiv(a.pairs > 0 ? a.pairs : 1);
+  const int64_t groups = ((int64_t)a.rows * a.tokens + (64 >> a.group_log2) - 1) >> (6 - a.group_log2);
+  // heads are split over workgroups too while there are fewer than that of them
+  int64_t splits = (1024 + groups - 1) / groups;
+  const int most = (a.heads + 3) / 4;
+  if (splits > most) splits = most;
+  // q and k share the runs of heads
+  const int heads1 = a.heads - a.heads0, chunks = (int)splits * 4;
+  a.chunks0 = (int)(((int64_t)chunks * a.heads0 + a.heads / 2) / a.heads);
+  if (heads1 > 0 && a.chunks0 == chunks) --a.chunks0;
+  if (a.heads0 > 0 && a.chunks0 == 0) a.chunks0 = 1;
+  a.step[0] = a.chunks0 > 0 ? (a.heads0 + a.chunks0 - 1) / a.chunks0 : 1;
+  a.step[1] = chunks > a.chunks0 ? (heads1 + chunks - a.chunks0 - 1) / (chunks - a.chunks0) : 1;
+  const dim3 grid((uint32_t)groups, (uint32_t)splits);
+  return is_bf16 ? launch_rope_type<bf16>(a, norm, rotate, whole, grid, s) : launch_rope_type<float>(a, norm, rotate, whole, grid, s);
 }
 
 }  // namespace sf

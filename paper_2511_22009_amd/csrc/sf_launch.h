@@ -284,9 +284,10 @@ struct RopeArgs {
   const float* pos;     // [rows][tokens][axes]
   int64_t pos_row;
   // filled in by launch_rope
-  double rate[kRopeAxes], step[kRopeAxes];  // log2 of theta per pair of an axis; 2^-rate
-  int head_step;        // heads of a wavefront
-  int splits0;          // wavefronts that share a token's heads of q
+  double rate[kRopeAxes];  // log2 of theta per pair of an axis
+  FastDiv div_pairs;
+  int chunks0;          // runs of heads of q (the others are of k)
+  int step[2];          // heads of q and of k in a run
   int group_log2;       // lanes that share a head: 2^group_log2
 };
 // norm: divide by the root mean square and multiply by the gain; rotate: turn the pairs.
