@@ -204,6 +204,7 @@ enum {
   SF_KC_CROSS,      /* every cross-attention kernel */
   SF_KC_HEAD,       /* final LayerNorm + modulate + linear + unpatchify */
   SF_KC_EULER,      /* guidance combine, Euler update and queue shift */
+  SF_KC_QK,         /* norm and rotation of the self-attention's queries and keys (sf_set_qk) */
   SF_KC_COUNT
 };
 
@@ -394,6 +395,27 @@ int sf_rotate(const sf_heads* x, int type, int rows, int tokens, int dh, const s
 int sf_qk_norm_rotate(const sf_heads* q, const sf_heads* k, const float* q_gain, const float* k_gain, float eps, int type,
                       int rows, int tokens, int dh, const sf_rope* rope, const float* pos, long long pos_row,
                       void* hip_stream);
+
+/* A network whose self-attention normalises its queries and keys per head and turns them by
+ * the token's place, instead of or besides the position table of its embedding (the usual
+ * form of rectified-flow transformers for images): between the QKV projection and the
+ * attention of every block, q and k go through sf_qk_norm_rotate in place. */
+typedef struct sf_qk {
+  int norm;                /* nonzero: divide each head by its root mean square and multiply by its gain */
+  float eps;               /* of the norm, finite, >= 0 (1e-6) */
+  const float* q_gain;     /* HOST fp32 [L][dh]: every block's gain per dim; NULL: 1. Copied. */
+  const float* k_gain;
+  const sf_rope* rope;     /* NULL: no rotation; else axes = 2 (patch row, patch column) */
+} sf_qk;
+
+/* Set (p != NULL) or clear (p == NULL, the default) the queries' and keys' treatment in
+ * sf_velocity, sf_stream_step and sf_residual. Synchronous: waits for the device, uploads the
+ * gains and the tokens' places (one device allocation, kept until the next set, clear or
+ * sf_free) and drops cached graphs. SF_E_INVAL for neither norm nor rope, gains without norm, or
+ * a rope that sf_rotate would refuse or whose axes are not 2; nothing changes then. On
+ * SF_E_OOM or SF_E_HIP the treatment is cleared. The allocation fails when
+ * SF_FAIL_ALLOC_AFTER is 0, to exercise that path. */
+int sf_set_qk(sf_model* m, const sf_qk* p);
 
 #ifdef __cplusplus
 }

@@ -18,7 +18,8 @@ What it computes (StreamFlow, arXiv 2511.22009):
   * the whole Alg. 2 driver over M images;
   * PeRFlow's time-window conversion of a noise prediction into a velocity, batched
     over heterogeneous timesteps (Sec. 2 time windows; Sec. 3.3; Alg. 1), in
-    `oracle.perflow`.
+    `oracle.perflow`;
+  * the norm and rotation of self-attention's queries and keys, in `oracle.qk`.
 
 The network itself is not in the paper (the paper runs a pretrained UNet that
 predicts noise); this oracle uses a DiT-style adaLN transformer that outputs v
@@ -34,6 +35,7 @@ from .weights import OracleModel, load_blob
 from .dit import (timestep_frequencies, timestep_embedding, modulation_table, patchify,
                   unpatchify, layer_norm, gelu_tanh, silu, attention, residual_one, forward_one,
                   velocity)
+from .qk import QK
 from .stream import euler, stream_step, run_stream, sequential_sample, noise_latent
 from . import perflow
 
@@ -41,5 +43,5 @@ __all__ = [
     "OracleModel", "load_blob", "timestep_frequencies", "timestep_embedding",
     "modulation_table", "patchify", "unpatchify", "layer_norm", "gelu_tanh", "silu",
     "attention", "residual_one", "forward_one", "velocity", "euler", "stream_step", "run_stream",
-    "sequential_sample", "noise_latent", "perflow",
+    "sequential_sample", "noise_latent", "perflow", "QK",
 ]

@@ -33,6 +33,8 @@ import math
 
 import numpy as np
 
+from .qk import treat
+
 LN_EPS = 1e-6
 T_MAX = 1000.0
 MAX_PERIOD = 10000.0
@@ -136,6 +138,10 @@ def block_forward(m, b, h, s, ctx=None, trace=None):
     a = layer_norm(h) * (1.0 + scale1) + shift1
     qkv = linear(a, b["W_qkv"], b["b_qkv"])
     q, k, v = qkv[:, :D], qkv[:, D:2 * D], qkv[:, 2 * D:]
+    if m.qk is not None:
+        l = next(i for i, c in enumerate(m.blocks) if c is b)
+        gq, gk = (None if g is None else np.asarray(g)[l] for g in (m.qk.q_gain, m.qk.k_gain))
+        q, k = (treat(z, m.heads, g, m.qk, m.W // m.p) for z, g in ((q, gq), (k, gk)))
     o = attention(q, k, v, m.heads)
     h = h + gate1 * linear(o, b["W_o"], b["b_o"])
     if trace is not None:

@@ -29,6 +29,7 @@ class OracleModel:
     seed: int
     top: dict = field(default_factory=dict)      # non-block tensors
     blocks: list = field(default_factory=list)   # per-block dicts
+    qk: object = None    # oracle.qk.QK: norm and rotation of q and k in self-attention
 
     @property
     def N(self):
@@ -43,6 +44,7 @@ class OracleModel:
         m = OracleModel(**{k: getattr(self, k) for k in _FIELDS}, seed=self.seed)
         m.top = {k: v.astype(dtype) for k, v in self.top.items()}
         m.blocks = [{k: v.astype(dtype) for k, v in b.items()} for b in self.blocks]
+        m.qk = self.qk
         return m
 
 

@@ -34,6 +34,7 @@ class KernelClass(enum.IntEnum):
     CROSS = 8
     HEAD = 9
     EULER = 10
+    QK = 11
 
 
 class Buffer(enum.IntEnum):
@@ -81,6 +82,11 @@ class _Heads(ctypes.Structure):
                [(n, ctypes.c_longlong) for n in ("in_row", "in_token", "in_head", "out_row", "out_token", "out_head")]
 
 
+class _QK(ctypes.Structure):
+    _fields_ = [("norm", ctypes.c_int), ("eps", ctypes.c_float), ("q_gain", ctypes.c_void_p), ("k_gain", ctypes.c_void_p),
+                ("rope", ctypes.POINTER(_Rope))]
+
+
 _LIB = None
 _P = ctypes.c_void_p
 _I = ctypes.c_int
@@ -109,6 +115,7 @@ _SIGS = {
     "sf_modulation_cache_stats": (_I, [_P, ctypes.POINTER(ctypes.c_long)]),
     "sf_context_cache": (_I, [_P, _I]),
     "sf_context_cache_stats": (_I, [_P, ctypes.POINTER(ctypes.c_long), ctypes.POINTER(ctypes.c_long)]),
+    "sf_set_qk": (_I, [_P, ctypes.POINTER(_QK)]),
     "sf_quantize_rows": (_I, [_P, _I, _J, _I, _J, _P, _J, _P, _P]),
     "sf_matmul_i8": (_I, [_P, _J, _P, _P, _J, _P, _P, _I, _I, _I, _P, _J, _I, _P]),
     "sf_rotate": (_I, [_P, _I, _I, _I, _I, _P, _P, _J, _I, _P]),
@@ -334,6 +341,20 @@ class Model:
 
     def clear_scheduler(self):
         _check(load_library().sf_set_scheduler(self._h, None), "sf_set_scheduler")
+
+    def set_qk(self, norm=True, q_gain=None, k_gain=None, rotary=None, eps=1e-6):
+        """Normalise the self-attention's queries and keys per head and turn them by the
+        token's place in the latent grid (see sf_set_qk). q_gain, k_gain: host arrays
+        [L, head dim] or None (1); rotary: a `Rotary` of two axes (patch row, patch column)
+        or None."""
+        n = self.info["L"] * (self.info["D"] // self.info["heads"])
+        gains = [None if g is None else _host_f32(g, n, what) for g, what in ((q_gain, "q_gain"), (k_gain, "k_gain"))]
+        p = _QK(int(bool(norm)), float(eps), *[None if g is None else _ptr(g) for g in gains],
+                None if rotary is None else ctypes.pointer(rotary._struct))
+        _check(load_library().sf_set_qk(self._h, ctypes.byref(p)), "sf_set_qk")
+
+    def clear_qk(self):
+        _check(load_library().sf_set_qk(self._h, None), "sf_set_qk")
 
     def scheduler_shift(self, x, out, t, dt, B, z_new, x_done=None, stream=None):
         """The update + shift of a stream step for a given network output `out`."""

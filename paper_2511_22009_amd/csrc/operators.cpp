@@ -8,6 +8,30 @@
 
 #include "sf_launch.h"
 
+namespace sf {
+
+bool take_rope(int axes, const int* dims, int layout, int spread, double theta, int dh, RopeArgs* a) {
+  if (axes < 1 || axes > SF_ROPE_AXES || layout < SF_ROPE_ADJACENT || layout > SF_ROPE_AXIS_HALVES ||
+      (spread != 0 && spread != 1) || !std::isfinite(theta) || !(theta > 1.0))
+    return false;
+  int pairs = 0;
+  for (int i = 0; i < axes; ++i) {
+    if (dims[i] < 0 || dims[i] % 2 || dims[i] > dh) return false;
+    a->first[i] = pairs;
+    pairs += dims[i] / 2;
+  }
+  if (2 * pairs > dh) return false;
+  for (int i = axes; i <= SF_ROPE_AXES; ++i) a->first[i] = pairs;
+  a->axes = axes;
+  a->pairs = pairs;
+  a->layout = layout;
+  a->spread = spread;
+  a->log2_theta = std::log2(theta);
+  return true;
+}
+
+}  // namespace sf
+
 namespace {
 
 static_assert(sf::kRopeAxes == SF_ROPE_AXES, "axes of a rotation");
@@ -15,27 +39,6 @@ static_assert(sf::kRopeAxes == SF_ROPE_AXES, "axes of a rotation");
 bool is_type(int t) { return t == SF_PREC_BF16 || t == SF_PREC_FP32; }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 int status(hipError_t e) { return e == hipSuccess ? SF_OK : SF_E_HIP; }
-
-// True when the plan fits heads of dh dims; fills the kernel's form of it.
-bool take_rope(const sf_rope& r, int dh, sf::RopeArgs& a) {
-  if (r.axes < 1 || r.axes > SF_ROPE_AXES || r.layout < SF_ROPE_ADJACENT || r.layout > SF_ROPE_AXIS_HALVES ||
-      (r.spread != 0 && r.spread != 1) || !std::isfinite(r.theta) || !(r.theta > 1.0))
-    return false;
-  int pairs = 0;
-  for (int i = 0; i < r.axes; ++i) {
-    if (r.dims[i] < 0 || r.dims[i] % 2 || r.dims[i] > dh) return false;
-    a.first[i] = pairs;
-    pairs += r.dims[i] / 2;
-  }
-  if (2 * pairs > dh) return false;
-  for (int i = r.axes; i <= SF_ROPE_AXES; ++i) a.first[i] = pairs;
-  a.axes = r.axes;
-  a.pairs = pairs;
-  a.layout = r.layout;
-  a.spread = r.spread;
-  a.log2_theta = std::log2(r.theta);
-  return true;
-}
 
 // Whether every entry of the output has a place of its own as far as a stride of 0 tells.
 bool own_places(const sf_heads& t, int rows, int tokens) {
@@ -55,7 +58,7 @@ int rope_call(const sf_heads* q, const sf_heads* k, const float* q_gain, const f
       !std::isfinite(eps))
     return SF_E_INVAL;
   sf::RopeArgs a{};
-  if (rope && !take_rope(*rope, dh, a)) return SF_E_INVAL;
+  if (rope && !sf::take_rope(rope->axes, rope->dims, rope->layout, rope->spread, rope->theta, dh, &a)) return SF_E_INVAL;
   a.heads0 = q->heads;
   a.heads = q->heads + (k ? k->heads : 0);
   if (rows == 0 || tokens == 0 || a.heads == 0) return SF_OK;

@@ -290,6 +290,8 @@ struct RopeArgs {
   int step[2];          // heads of q and of k in a run
   int group_log2;       // lanes that share a head: 2^group_log2
 };
+// Fills in a plan's part of the arguments; false for a plan that does not fit heads of dh dims.
+bool take_rope(int axes, const int* dims, int layout, int spread, double theta, int dh, RopeArgs* a);
 // norm: divide by the root mean square and multiply by the gain; rotate: turn the pairs.
 hipError_t launch_rope(bool is_bf16, bool norm, bool rotate, RopeArgs a, hipStream_t s);
 

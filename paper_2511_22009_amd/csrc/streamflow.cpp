@@ -130,6 +130,12 @@ struct sf_model {
   double win_eps = 0.0;
   double* abar = nullptr;
   int n_abar = 0;
+  // norm and rotation of q and k between projection and attention (qk_on): the plan, and in
+  // qkmem every block's gains of q, then of k (null: 1), and the tokens' places [N][2]
+  bool qk_on = false, qk_norm = false, qk_rope = false;
+  sf::RopeArgs qk{};
+  char* qkmem = nullptr;
+  float *q_gain = nullptr, *k_gain = nullptr, *places = nullptr;
   bool graph_on = false;
   std::vector<GraphEntry> graphs;
   unsigned long long graph_clock = 0;
@@ -446,6 +452,25 @@ sf::GemmArgs gemm_base(const void* A, int lda, const void* B, int ldb, int M, in
   return g;
 }
 
+// Norm and rotation of block l's q and k, [rows][heads][N][dh] each, in place.
+hipError_t run_qk(const sf_model* m, int l, int rows, hipStream_t s) {
+  const int heads = (int)m->hd.heads;
+  const int64_t head = (int64_t)m->N * m->dh, row = head * heads;
+  sf::RopeArgs a = m->qk;
+  const size_t gain = (size_t)l * m->dh;
+  a.t[0] = sf::RopeHeads{(const char*)m->q, (char*)m->q, m->q_gain ? m->q_gain + gain : nullptr, row, m->dh, head, row, m->dh, head};
+  a.t[1] = sf::RopeHeads{(const char*)m->k, (char*)m->k, m->k_gain ? m->k_gain + gain : nullptr, row, m->dh, head, row, m->dh, head};
+  a.heads0 = heads;
+  a.heads = 2 * heads;
+  a.rows = rows;
+  a.tokens = m->N;
+  a.dh = m->dh;
+  a.div_tok = sf::make_fastdiv((uint32_t)m->N);
+  a.pos = m->places;
+  a.pos_row = 0;
+  return sf::launch_rope(m->bf16, m->qk_norm, m->qk_rope, a, s);
+}
+
 // The network call on `rows` rows built from n_lat latents (rows = n_lat, or 2 n_lat
 // with guidance: cond rows then uncond rows, each using its latent's t). Runs through
 // `nblocks` blocks; if head_out != nullptr also the output head into head_out [rows][E].
@@ -499,6 +524,7 @@ int run_network(sf_model* m, const float* x, const float* t, int n_lat, int rows
       g.div_ntok = div_n; g.div_D = div_d; g.div_dh = div_dh;
       return sf::launch_gemm(m->bf16, sf::EPI_QKV, g, s);
     }));
+    if (m->qk_on) SF_TRY(timed(m, SF_KC_QK, s, [&]() { return run_qk(m, l, rows, s); }));
     SF_TRY(timed(m, SF_KC_ATTN, s, [&]() {
       sf::AttnArgs a{m->q, m->k, m->vT, m->o, rows, (int)h.heads, N, N, m->dh, m->ldv, D,
                      (float)(1.0 / std::sqrt((double)m->dh)), m->vperm};
@@ -809,6 +835,7 @@ void sf_free(sf_model* m) {
   if (m->wmem || m->wsmem) (void)hipDeviceSynchronize();
   drop_graphs(m);
   if (m->abar) (void)hipFree(m->abar);
+  if (m->qkmem) (void)hipFree(m->qkmem);
   for (auto& tm : m->timing)
     for (hipEvent_t e : tm.ev) (void)hipEventDestroy(e);
   if (m->wmem) (void)hipFree(m->wmem);
@@ -1091,6 +1118,65 @@ int sf_set_scheduler(sf_model* m, const sf_perflow* p) {
     return SF_E_HIP;
   m->win_eps = p->eps;
   m->windows = p->windows;
+  return SF_OK;
+}
+
+int sf_set_qk(sf_model* m, const sf_qk* p) {
+  if (!m) return SF_E_NOTLOADED;
+  sf::RopeArgs plan{};
+  if (p) {
+    const bool norm = p->norm != 0;
+    if ((!norm && !p->rope) || (!norm && (p->q_gain || p->k_gain)) || !std::isfinite(p->eps) || !(p->eps >= 0.0f) ||
+        (p->rope && (p->rope->axes != 2 || !sf::take_rope(2, p->rope->dims, p->rope->layout, p->rope->spread, p->rope->theta,
+                                                          m->dh, &plan))))
+      return SF_E_INVAL;
+  } else if (!m->qk_on) {
+    return SF_OK;
+  }
+  if (hipDeviceSynchronize() != hipSuccess) return SF_E_HIP;
+  drop_graphs(m);
+  m->qk_on = false;  // until the new treatment is in place
+  if (m->qkmem) (void)hipFree(m->qkmem);
+  m->qkmem = nullptr;
+  m->q_gain = m->k_gain = m->places = nullptr;
+  if (!p) return SF_OK;
+  const size_t gains = (size_t)m->hd.L * m->dh;
+  auto carve = [&](char* base) {
+    Carver cv;
+    cv.base = base;
+    m->q_gain = p->q_gain ? cv.take<float>(gains) : nullptr;
+    m->k_gain = p->k_gain ? cv.take<float>(gains) : nullptr;
+    m->places = cv.take<float>((size_t)m->N * 2);
+    return cv.off;
+  };
+  const size_t bytes = carve(nullptr);
+  std::vector<float> at;
+  try {
+    at.resize((size_t)m->N * 2);
+  } catch (...) {
+    return SF_E_OOM;
+  }
+  const int gw = (int)(m->hd.W / m->hd.p);
+  for (int n = 0; n < m->N; ++n) {
+    at[2 * (size_t)n] = (float)(n / gw);
+    at[2 * (size_t)n + 1] = (float)(n % gw);
+  }
+  if (fail_alloc_after() == 0 || hipMalloc((void**)&m->qkmem, bytes) != hipSuccess) {
+    m->qkmem = nullptr;
+    m->q_gain = m->k_gain = m->places = nullptr;
+    (void)hipGetLastError();
+    return SF_E_OOM;
+  }
+  carve(m->qkmem);
+  if ((gains > 0 && p->q_gain && hipMemcpy(m->q_gain, p->q_gain, gains * sizeof(float), hipMemcpyHostToDevice) != hipSuccess) ||
+      (gains > 0 && p->k_gain && hipMemcpy(m->k_gain, p->k_gain, gains * sizeof(float), hipMemcpyHostToDevice) != hipSuccess) ||
+      hipMemcpy(m->places, at.data(), at.size() * sizeof(float), hipMemcpyHostToDevice) != hipSuccess)
+    return SF_E_HIP;
+  plan.eps = p->eps;
+  m->qk = plan;
+  m->qk_norm = p->norm != 0;
+  m->qk_rope = p->rope != nullptr;
+  m->qk_on = true;
   return SF_OK;
 }
 

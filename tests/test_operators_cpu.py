@@ -166,3 +166,8 @@ def test_choice_of_8_bit_tiles(tmp_path):
                     "-o", exe], check=True)
     r = subprocess.run([exe], capture_output=True, text=True, timeout=60)
     assert r.returncode == 0, (r.returncode, r.stdout, r.stderr)
+
+
+def test_model_settings_need_a_model():
+    L = load_library()
+    assert L.sf_set_qk(None, None) == -3
