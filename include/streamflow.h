@@ -205,6 +205,7 @@ enum {
   SF_KC_HEAD,       /* final LayerNorm + modulate + linear + unpatchify */
   SF_KC_EULER,      /* guidance combine, Euler update and queue shift */
   SF_KC_QK,         /* norm and rotation of the self-attention's queries and keys (sf_set_qk) */
+  SF_KC_QUANT,      /* rows to 8-bit codes (sf_set_int8) */
   SF_KC_COUNT
 };
 
@@ -416,6 +417,22 @@ typedef struct sf_qk {
  * SF_E_OOM or SF_E_HIP the treatment is cleared. The allocation fails when
  * SF_FAIL_ALLOC_AFTER is 0, to exercise that path. */
 int sf_set_qk(sf_model* m, const sf_qk* p);
+
+/* The four projections of every block (QKV, attention output, MLP up and down) in 8 bits:
+ * their weights as codes with a scale per output channel, made once by the call from the
+ * model's bf16 weights, and their inputs as codes with a scale per token, made as they pass
+ * (sf_quantize_rows; LayerNorm + modulate leaves codes itself, from fp32), multiplied as in
+ * sf_matmul_i8 with the epilogues of the bf16 projections. Everything else, the
+ * cross-attention's projections included, stays as it is. */
+
+/* Enable (nonzero) or disable (0, the default) 8-bit projections in sf_velocity,
+ * sf_stream_step and sf_residual. Needs a model loaded in SF_PREC_BF16 (SF_E_INVAL
+ * otherwise). Synchronous: waits for the device, makes the codes (one device allocation of
+ * about half the blocks' weights plus, per row of the workspace, the widest input, held until it
+ * is disabled or sf_free) and drops cached graphs; the bf16 weights stay. While
+ * enabled SF_BUF_ACT does not follow the calls. On SF_E_OOM or SF_E_HIP it is
+ * disabled; the allocation fails when SF_FAIL_ALLOC_AFTER is 0, to exercise that path. */
+int sf_set_int8(sf_model* m, int enable);
 
 #ifdef __cplusplus
 }

@@ -35,6 +35,7 @@ class KernelClass(enum.IntEnum):
     HEAD = 9
     EULER = 10
     QK = 11
+    QUANT = 12
 
 
 class Buffer(enum.IntEnum):
@@ -116,6 +117,7 @@ _SIGS = {
     "sf_context_cache": (_I, [_P, _I]),
     "sf_context_cache_stats": (_I, [_P, ctypes.POINTER(ctypes.c_long), ctypes.POINTER(ctypes.c_long)]),
     "sf_set_qk": (_I, [_P, ctypes.POINTER(_QK)]),
+    "sf_set_int8": (_I, [_P, _I]),
     "sf_quantize_rows": (_I, [_P, _I, _J, _I, _J, _P, _J, _P, _P]),
     "sf_matmul_i8": (_I, [_P, _J, _P, _P, _J, _P, _P, _I, _I, _I, _P, _J, _I, _P]),
     "sf_rotate": (_I, [_P, _I, _I, _I, _I, _P, _P, _J, _I, _P]),
@@ -355,6 +357,10 @@ class Model:
 
     def clear_qk(self):
         _check(load_library().sf_set_qk(self._h, None), "sf_set_qk")
+
+    def set_int8(self, on=True):
+        """Run the projections of every block in 8 bits (bf16 models; see sf_set_int8)."""
+        _check(load_library().sf_set_int8(self._h, 1 if on else 0), "sf_set_int8")
 
     def scheduler_shift(self, x, out, t, dt, B, z_new, x_done=None, stream=None):
         """The update + shift of a stream step for a given network output `out`."""

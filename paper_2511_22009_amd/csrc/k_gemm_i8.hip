@@ -1,5 +1,6 @@
 // Products of 8-bit codes on the matrix cores, out[m][n] = (sum_k A[m][k] B[n][k]) sa[m] sb[n]
-// + bias[n]: v_mfma_i32_32x32x32_i8, whose 32-bit sums are exact for every K the entry point
+// + bias[n], or, in a network's blocks, that value's GELU, its place among the heads' queries,
+// keys and transposed values, or h += gate times it: v_mfma_i32_32x32x32_i8, whose 32-bit sums are exact for every K the entry point
 // allows, so no choice of tile changes a bit of a result. The weights are the first operand, so
 // a lane ends up with four adjacent output columns of one row.
 //
@@ -40,7 +41,7 @@ __device__ __forceinline__ void i8_tile(int nbm, int nbn, int& mt, int& nt) {
 // Codes past K: whole chunks read as zeros (an offset past the resource); in a chunk that K
 // ends in, A's bytes past K are cleared in LDS before the last slice is read (a code times 0
 // is 0, whatever B holds there).
-template <int BM, int BN, int WM, int WN, int STAGES, int MINW, typename OT>
+template <int BM, int BN, int WM, int WN, int STAGES, int MINW, I8Kind KIND>
 __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_i8_kernel(GemmI8Args a) {
   constexpr int NT = WM * WN * 64, BK = 128, CPR = 8, KS = 4;
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
@@ -216,11 +217,30 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_i8_kernel(GemmI8Args 
 
   // lane (l32, g) holds row l32 of each block and the columns 8 q + 4 g + 0..3, and stores
   // straight from its registers (through LDS, in whole rows of a wavefront's part, the
-  // launches took as long or up to 10 % longer)
+  // launches took as long or up to 10 % longer). bf16 outputs leave in eights: lanes l and l + 32
+  // exchange halves, then the first has the eight columns of group q, the second those of q + 1
+  constexpr bool kEights = KIND != I8_F32 && KIND != I8_RES_GATE;
+  constexpr int QS = kEights ? 2 : 1;  // groups of four columns to a store
   typedef uint32_t out16 __attribute__((ext_vector_type(4), aligned(2)));
-  constexpr int QS = sizeof(OT) == 2 ? 2 : 1;  // groups of four columns to a store
 #pragma unroll
-  for (int j = 0; j < TN; ++j)
+  for (int j = 0; j < TN; ++j) {
+    // the residual and the gates of a block column are loaded before any is used (rows past M
+    // and columns past N read others that exist; N is a multiple of four here)
+    f32x4 h[KIND == I8_RES_GATE ? 4 : 1][TM], gate[KIND == I8_RES_GATE ? 4 : 1][TM];
+    if constexpr (KIND == I8_RES_GATE) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const int m = min(m0 + (wm * TM + i) * 32 + l32, a.M - 1);
+        const int r = (int)fdiv((uint32_t)m, a.e.div_ntok);
+        const float* const gates = a.e.table + (size_t)(r < a.e.n_slots ? r : r - a.e.n_slots) * a.e.ldt + a.e.gate_off;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int n = min(n0 + (wn * TN + j) * 32 + 8 * q + 4 * g, a.N - 4);
+          h[q][i] = *(const f32x4*)(a.e.h + (size_t)m * a.e.ldh + n);
+          gate[q][i] = *(const f32x4*)(gates + n);
+        }
+      }
+    }
 #pragma unroll
     for (int q = 0; q < 4; q += QS) {
       float sb[4 * QS], bias[4 * QS];
@@ -230,40 +250,63 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_i8_kernel(GemmI8Args 
         sb[r] = __shfl(sb_v[j], from);
         bias[r] = __shfl(bias_v[j], from);
       }
-      const int n = n0 + (wn * TN + j) * 32 + 8 * q + (sizeof(OT) == 2 ? 8 * g : 4 * g);
+      const int n = n0 + (wn * TN + j) * 32 + 8 * q + (kEights ? 8 * g : 4 * g);
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
+        const int m = m0 + (wm * TM + i) * 32 + l32;
         float v[4 * QS];
 #pragma unroll
-        for (int r = 0; r < 4 * QS; ++r) v[r] = (float)acc[i][j][4 * q + r] * sa_v[i] * sb[r] + bias[r];
-        u32x4 o;
-        if constexpr (sizeof(OT) == 2) {
-          // the lanes l and l + 32 exchange halves: then the first has the eight columns of
-          // group q, the second those of group q + 1
-          auto pack = [&](int r) { return pack_bf16(v[r], v[r + 1]); };
-          const auto x = __builtin_amdgcn_permlane32_swap(pack(0), pack(4), false, false);
-          const auto y = __builtin_amdgcn_permlane32_swap(pack(2), pack(6), false, false);
-          o = u32x4{x[0], y[0], x[1], y[1]};
-        } else {
-          o = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        for (int r = 0; r < 4 * QS; ++r) {
+          v[r] = (float)acc[i][j][4 * q + r] * sa_v[i] * sb[r] + bias[r];
+          if constexpr (KIND == I8_GELU) v[r] = gelu_tanh(v[r]);
         }
-        const int m = m0 + (wm * TM + i) * 32 + l32;
-        OT* const p = (OT*)a.out + (int64_t)m * a.ldo + n;
-        constexpr int E = 16 / (int)sizeof(OT);
-        if (m < a.M && n + E <= a.N) {
-          *(out16*)p = o;
-        } else if (m < a.M) {
+        if constexpr (KIND == I8_RES_GATE) {
+          f32x4 o = h[q][i];
 #pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (n + e < a.N) {
-              if constexpr (sizeof(OT) == 2)
-                ((uint16_t*)p)[e] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
-              else
-                ((uint32_t*)p)[e] = o[e];
+          for (int e = 0; e < 4; ++e) o[e] += gate[q][i][e] * v[e];
+          if (m < a.M && n < a.N) *(f32x4*)(a.e.h + (size_t)m * a.e.ldh + n) = o;
+        } else if constexpr (KIND == I8_F32) {
+          float* const p = (float*)a.out + (int64_t)m * a.ldo + n;
+          if (m < a.M && n + 4 <= a.N) {
+            *(out16*)p = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+          } else if (m < a.M) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (n + e < a.N) p[e] = v[e];
+          }
+        } else {
+          const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16(v[0], v[1]), pack_bf16(v[4], v[5]), false, false);
+          const auto y = __builtin_amdgcn_permlane32_swap(pack_bf16(v[2], v[3]), pack_bf16(v[6], v[7]), false, false);
+          const u32x4 o = {x[0], y[0], x[1], y[1]};
+          if constexpr (KIND == I8_QKV) {
+            // the eight columns belong to one head (widths of heads are multiples of eight)
+            if (m >= a.M || n >= a.N) continue;
+            const int part = (int)fdiv((uint32_t)n, a.e.div_D), rem = n - part * a.e.D;
+            const int head = (int)fdiv((uint32_t)rem, a.e.div_dh), d = rem - head * a.e.dh;
+            const int r = (int)fdiv((uint32_t)m, a.e.div_ntok), tok = m - r * a.e.ntok;
+            const size_t bh = (size_t)r * a.e.heads + head;
+            if (part < 2) {
+              *(u32x4*)((bf16*)(part == 0 ? a.e.q : a.e.k) + (bh * a.e.ntok + tok) * a.e.dh + d) = o;
+            } else {
+              // transposed, adjacent lanes adjacent tokens (in groups of four, vt_pos)
+              uint16_t* const vt = (uint16_t*)a.e.vT + (bh * a.e.dh + d) * a.e.ldv + vt_pos(tok);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) vt[(size_t)e * a.e.ldv] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
             }
+          } else {
+            bf16* const p = (bf16*)a.out + (int64_t)m * a.ldo + n;
+            if (m < a.M && n + 8 <= a.N) {
+              *(out16*)p = o;
+            } else if (m < a.M) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (n + e < a.N) ((uint16_t*)p)[e] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
+            }
+          }
         }
       }
     }
+  }
 }
 
 // Tiles: BM x BN, wave grid, LDS stages, wavefronts per SIMD.
@@ -274,14 +317,14 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_i8_kernel(GemmI8Args 
   X(kI8Tile128x192, 128, 192, 2, 2, 2, 2) \
   X(kI8Tile256x192, 256, 192, 4, 2, 2, 2)
 
-template <typename OT>
+template <I8Kind KIND>
 static hipError_t launch_i8(const GemmI8Args& a, hipStream_t s) {
   switch (choose_gemm_i8_tile(a.M, a.N, a.K)) {
 #define SF_I8_CASE(id, bm, bn, wm, wn, st, mw)                                                               \
   case id: {                                                                                                 \
     const int64_t tiles = (((int64_t)a.M + bm - 1) / bm) * (((int64_t)a.N + bn - 1) / bn);                   \
     if (tiles > 0x7fffffff) return hipErrorInvalidValue;                                                     \
-    launch(gemm_i8_kernel<bm, bn, wm, wn, st, mw, OT>, dim3((uint32_t)tiles), dim3(wm * wn * 64), 0, s, a);  \
+    launch(gemm_i8_kernel<bm, bn, wm, wn, st, mw, KIND>, dim3((uint32_t)tiles), dim3(wm * wn * 64), 0, s, a);  \
     break;                                                                                                   \
   }
     SF_I8_TILES(SF_I8_CASE)
@@ -290,8 +333,15 @@ static hipError_t launch_i8(const GemmI8Args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_gemm_i8(bool out_bf16, const GemmI8Args& a, hipStream_t s) {
-  return out_bf16 ? launch_i8<bf16>(a, s) : launch_i8<float>(a, s);
+hipError_t launch_gemm_i8(I8Kind kind, const GemmI8Args& a, hipStream_t s) {
+  switch (kind) {
+    case I8_BF16: return launch_i8<I8_BF16>(a, s);
+    case I8_F32: return launch_i8<I8_F32>(a, s);
+    case I8_QKV: return launch_i8<I8_QKV>(a, s);
+    case I8_GELU: return launch_i8<I8_GELU>(a, s);
+    case I8_RES_GATE: return launch_i8<I8_RES_GATE>(a, s);
+  }
+  return hipErrorInvalidValue;
 }
 
 }  // namespace sf

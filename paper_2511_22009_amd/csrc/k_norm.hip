@@ -136,6 +136,76 @@ hipError_t launch_ln(bool out_bf16, const LnArgs& a, hipStream_t s) {
   return out_bf16 ? launch_ln_t<bf16>(a, s) : launch_ln_t<float>(a, s);
 }
 
+// The same rows as 8-bit codes with a scale per row (sf_device.h), from the fp32 values: no
+// rounding to bf16 in between, and no pass over the rows of its own. One row per wavefront,
+// loads as in ln_mod_kernel. Bandwidth bounds it (5 bytes an element): LN_CODES.
+template <int NV>
+__global__ __launch_bounds__(256) void ln_codes_kernel(LnArgs a, int ldq, float* scale) {
+  const int lane = threadIdx.x & 63;
+  const int m = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (m >= a.M) return;
+  const int nv = a.D >> 2;
+  const float4* row = (const float4*)(a.h + (size_t)m * a.D);
+  const int s0 = (int)fdiv((uint32_t)m, a.tok), slot = s0 < a.n_slots ? s0 : s0 - a.n_slots;
+  const float4* tsh = (const float4*)(a.table + (size_t)slot * a.ldt + a.shift_off);
+  const float4* tsc = (const float4*)(a.table + (size_t)slot * a.ldt + a.scale_off);
+  float4 v[NV], sc[NV], sh[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = lane + i * 64 < nv ? lane + i * 64 : 0;
+    v[i] = row[c];
+    sc[i] = tsc[c];
+    sh[i] = tsh[c];
+  }
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) s += lane + i * 64 < nv ? (v[i].x + v[i].y) + (v[i].z + v[i].w) : 0.0f;
+  const float mean = wave_sum(s) / (float)a.D;
+  float q = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const float d0 = v[i].x - mean, d1 = v[i].y - mean, d2 = v[i].z - mean, d3 = v[i].w - mean;
+    q += lane + i * 64 < nv ? (d0 * d0 + d1 * d1) + (d2 * d2 + d3 * d3) : 0.0f;
+  }
+  const float rstd = 1.0f / sqrtf(wave_sum(q) / (float)a.D + kLnEps);
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    v[i].x = (v[i].x - mean) * rstd * (1.0f + sc[i].x) + sh[i].x;
+    v[i].y = (v[i].y - mean) * rstd * (1.0f + sc[i].y) + sh[i].y;
+    v[i].z = (v[i].z - mean) * rstd * (1.0f + sc[i].z) + sh[i].z;
+    v[i].w = (v[i].w - mean) * rstd * (1.0f + sc[i].w) + sh[i].w;
+    // a lane past the row's end holds chunk 0 again
+    top = max(top, max(max(abs_bits(v[i].x), abs_bits(v[i].y)), max(abs_bits(v[i].z), abs_bits(v[i].w))));
+  }
+  const RowQuant rq = row_quant(wave_max_bits(top));
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = lane + i * 64;
+    const float x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+    uint32_t code[1];
+    quant_codes(x, rq, code);
+    if (c < nv) *(uint32_t*)((int8_t*)a.out + (size_t)m * ldq + 4 * c) = code[0];
+  }
+  if (lane == 0) scale[m] = rq.scale;
+}
+
+hipError_t launch_ln_codes(const LnArgs& a, int ldq, float* scale, hipStream_t s) {
+  const dim3 grid((a.M + 3) / 4), block(256);
+  switch ((a.D + 255) / 256) {
+    case 1: launch(ln_codes_kernel<1>, grid, block, 0, s, a, ldq, scale); break;
+    case 2: launch(ln_codes_kernel<2>, grid, block, 0, s, a, ldq, scale); break;
+    case 3: launch(ln_codes_kernel<3>, grid, block, 0, s, a, ldq, scale); break;
+    case 4: launch(ln_codes_kernel<4>, grid, block, 0, s, a, ldq, scale); break;
+    case 5: launch(ln_codes_kernel<5>, grid, block, 0, s, a, ldq, scale); break;
+    case 6: launch(ln_codes_kernel<6>, grid, block, 0, s, a, ldq, scale); break;
+    case 7: launch(ln_codes_kernel<7>, grid, block, 0, s, a, ldq, scale); break;
+    case 8: launch(ln_codes_kernel<8>, grid, block, 0, s, a, ldq, scale); break;
+    default: return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
 // A workgroup takes four token rows. Each wavefront normalises and modulates one of them (lane
 // l holds 16-byte chunks l + 64 i) and leaves it in LDS; then wavefront w applies outputs
 // 4 w .. 4 w + 3 (and every 16th group of four after them) of the linear map D -> P to all four

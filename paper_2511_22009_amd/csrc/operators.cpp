@@ -101,8 +101,8 @@ int sf_matmul_i8(const signed char* a, long long lda, const float* a_scale, cons
   if (!a || !b || !a_scale || !b_scale || !out || !aligned16(a) || !aligned16(b) || lda % 16 || ldb % 16 || lda < need ||
       ldb < need || lda >= kMostLd || ldb >= kMostLd || ldo < N)
     return SF_E_INVAL;
-  const sf::GemmI8Args g{(const int8_t*)a, (const int8_t*)b, (int)lda, (int)ldb, M, N, K, a_scale, b_scale, bias, out, ldo};
-  return status(sf::launch_gemm_i8(out_type == SF_PREC_BF16, g, (hipStream_t)stream));
+  const sf::GemmI8Args g{(const int8_t*)a, (const int8_t*)b, (int)lda, (int)ldb, M, N, K, a_scale, b_scale, bias, out, ldo, {}};
+  return status(sf::launch_gemm_i8(out_type == SF_PREC_BF16 ? sf::I8_BF16 : sf::I8_F32, g, (hipStream_t)stream));
 }
 
 int sf_rotate(const sf_heads* x, int type, int rows, int tokens, int dh, const sf_rope* rope, const float* pos,

@@ -272,26 +272,28 @@ __device__ __forceinline__ int quant_code(float x, const RowQuant& r) {
   const float y = x * r.inv, q = rintf(y);
   return fabsf(y - q) < kQuantSure && r.inv != 0.0f ? (int)q : quant_code_exact(x, r);
 }
-// Eight codes, first in the low byte. y + 1.5 2^23 rounds y to a whole number, ties to even, and
-// has its low byte in its own.
-__device__ __forceinline__ uint2 quant_codes8(const float (&x)[8], const RowQuant& r) {
+// Codes of N elements, four to a word, the first in the low byte. y + 1.5 2^23 rounds y to a
+// whole number, ties to even, and has its low byte in its own.
+template <int N>
+__device__ __forceinline__ void quant_codes(const float (&x)[N], const RowQuant& r, uint32_t (&out)[N / 4]) {
   constexpr float kWhole = 12582912.0f;
-  uint32_t b[8];
+  uint32_t b[N];
   float off = 0.0f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int e = 0; e < N; ++e) {
     const float y = x[e] * r.inv, t = y + kWhole;
     off = fmaxf(off, fabsf(y - (t - kWhole)));
     b[e] = __float_as_uint(t);
   }
   if (!(off < kQuantSure) || r.inv == 0.0f) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) b[e] = (uint32_t)quant_code_exact(x[e], r);
+    for (int e = 0; e < N; ++e) b[e] = (uint32_t)quant_code_exact(x[e], r);
   }
-  // bytes: __builtin_amdgcn_perm(hi, lo, sel) takes 0..3 from lo and 4..7 from hi
-  const uint32_t p0 = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), p1 = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0cu);
-  const uint32_t p2 = __builtin_amdgcn_perm(b[5], b[4], 0x0c0c0400u), p3 = __builtin_amdgcn_perm(b[7], b[6], 0x04000c0cu);
-  return uint2{p0 | p1, p2 | p3};
+  // bytes: __builtin_amdgcn_perm(hi, lo, sel) takes 0..3 from lo, 4..7 from hi and 0 for 12
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i)
+    out[i] = __builtin_amdgcn_perm(b[4 * i + 1], b[4 * i], 0x0c0c0400u) |
+             __builtin_amdgcn_perm(b[4 * i + 3], b[4 * i + 2], 0x04000c0cu);
 }
 
 }  // namespace sf

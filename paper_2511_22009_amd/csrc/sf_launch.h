@@ -134,6 +134,9 @@ struct LnArgs {
   int n_slots;          // network row r uses table row (r < n_slots ? r : r - n_slots)
 };
 hipError_t launch_ln(bool out_bf16, const LnArgs& a, hipStream_t s);
+// The same rows as 8-bit codes, straight from their fp32 values: out int8, row length ldq (a
+// multiple of 16, 16-byte aligned), and scale [M].
+hipError_t launch_ln_codes(const LnArgs& a, int ldq, float* scale, hipStream_t s);
 
 // ---- K7: final LN + modulate + linear D -> p*p*C + unpatchify ----------------------
 struct HeadArgs {
@@ -254,10 +257,19 @@ struct GemmI8Args {
   const float* sa;      // [M]
   const float* sb;      // [N]
   const float* bias;    // [N] or nullptr
-  void* out;            // [M][N], row length ldo
+  void* out;            // [M][N], row length ldo (I8_BF16, I8_F32, I8_GELU)
   int64_t ldo;
+  GemmArgs e;           // the epilogue's fields (I8_QKV with which_base 0 and vperm, I8_RES_GATE);
+                        // N, head width and h's rows as the bf16 projections need them
 };
-hipError_t launch_gemm_i8(bool out_bf16, const GemmI8Args& a, hipStream_t s);
+enum I8Kind {
+  I8_BF16 = 0,   // out = value, bf16
+  I8_F32,        // out = value, fp32
+  I8_QKV,        // EPI_QKV
+  I8_GELU,       // out = GELU_tanh(value), bf16
+  I8_RES_GATE    // EPI_RES_GATE
+};
+hipError_t launch_gemm_i8(I8Kind kind, const GemmI8Args& a, hipStream_t s);
 
 // ---- per-head norm and rotation of heads ---------------------------------------------
 constexpr int kRopeAxes = 4;  // equals SF_ROPE_AXES

@@ -51,6 +51,12 @@ struct Block {
   float *b_qkv, *b_o, *b_fc1, *b_fc2, *b_qx, *b_kvx, *b_ox;
 };
 
+// A block's projections in 8 bits: codes with a scale per output channel.
+struct Block8 {
+  int8_t *qkv, *o, *fc1, *fc2;
+  float *s_qkv, *s_o, *s_fc1, *s_fc2;
+};
+
 struct Timing {
   bool on = false;
   std::vector<hipEvent_t> ev;  // start/end pairs
@@ -136,6 +142,14 @@ struct sf_model {
   sf::RopeArgs qk{};
   char* qkmem = nullptr;
   float *q_gain = nullptr, *k_gain = nullptr, *places = nullptr;
+  // 8-bit projections (int8_on): in mem8 every block's codes and scales, and the codes and
+  // scales of the rows on their way into a projection (at most the MLP's width)
+  bool int8_on = false;
+  char* mem8 = nullptr;
+  std::vector<Block8> blk8;
+  int8_t* rows8 = nullptr;
+  float* scale8 = nullptr;
+  int ldD8 = 0, ldF8 = 0;  // row lengths of codes of width D and mlp
   bool graph_on = false;
   std::vector<GraphEntry> graphs;
   unsigned long long graph_clock = 0;
@@ -471,6 +485,17 @@ hipError_t run_qk(const sf_model* m, int l, int rows, hipStream_t s) {
   return sf::launch_rope(m->bf16, m->qk_norm, m->qk_rope, a, s);
 }
 
+// Rows x [M][K] (bf16) as codes into the row buffer.
+hipError_t rows_to_codes(const sf_model* m, const void* x, int M, int K, int ld8, hipStream_t s) {
+  return sf::launch_quantize_rows(true, sf::QuantArgs{x, K, M, K, m->rows8, ld8, m->scale8}, s);
+}
+
+// An 8-bit projection of the rows in the row buffer.
+hipError_t project8(const sf_model* m, sf::I8Kind kind, const int8_t* W, const float* s_w, const sf::GemmArgs& g, int ld8,
+                    hipStream_t s) {
+  return sf::launch_gemm_i8(kind, sf::GemmI8Args{m->rows8, W, ld8, ld8, g.M, g.N, g.K, m->scale8, s_w, g.bias, g.out, g.ldo, g}, s);
+}
+
 // The network call on `rows` rows built from n_lat latents (rows = n_lat, or 2 n_lat
 // with guidance: cond rows then uncond rows, each using its latent's t). Runs through
 // `nblocks` blocks; if head_out != nullptr also the output head into head_out [rows][E].
@@ -513,15 +538,23 @@ int run_network(sf_model* m, const float* x, const float* t, int n_lat, int rows
     sf::LnArgs a{m->h, m->act, M, D, modulate ? m->table : nullptr, m->modw, shift_off, scale_off, div_n, n_lat};
     return sf::launch_ln(m->bf16, a, s);
   };
+  // LayerNorm + modulate into the input of a projection: bf16 or fp32 rows, or 8-bit codes
+  auto ln_in = [&](int shift_off, int scale_off) {
+    if (!m->int8_on) return ln(shift_off, scale_off, true);
+    const sf::LnArgs a{m->h, m->rows8, M, D, m->table, m->modw, shift_off, scale_off, div_n, n_lat};
+    return sf::launch_ln_codes(a, m->ldD8, m->scale8, s);
+  };
   for (int l = 0; l < nblocks; ++l) {
     const Block& b = m->blk[l];
+    const Block8* const b8 = m->int8_on ? &m->blk8[l] : nullptr;
     const int base = l * 6 * D;
-    SF_TRY(timed(m, SF_KC_LN, s, [&]() { return ln(base, base + D, true); }));
+    SF_TRY(timed(m, SF_KC_LN, s, [&]() { return ln_in(base, base + D); }));
     SF_TRY(timed(m, SF_KC_QKV, s, [&]() {
       sf::GemmArgs g = gemm_base(m->act, D, b.W_qkv, D, M, 3 * D, D, b.b_qkv);
       g.q = m->q; g.k = m->k; g.vT = m->vT;
       g.heads = h.heads; g.dh = m->dh; g.D = D; g.ntok = N; g.ldv = m->ldv; g.which_base = 0; g.vperm = m->vperm;
       g.div_ntok = div_n; g.div_D = div_d; g.div_dh = div_dh;
+      if (b8) return project8(m, sf::I8_QKV, b8->qkv, b8->s_qkv, g, m->ldD8, s);
       return sf::launch_gemm(m->bf16, sf::EPI_QKV, g, s);
     }));
     if (m->qk_on) SF_TRY(timed(m, SF_KC_QK, s, [&]() { return run_qk(m, l, rows, s); }));
@@ -530,10 +563,12 @@ int run_network(sf_model* m, const float* x, const float* t, int n_lat, int rows
                      (float)(1.0 / std::sqrt((double)m->dh)), m->vperm};
       return sf::launch_attention(m->bf16, a, s);
     }));
+    if (b8) SF_TRY(timed(m, SF_KC_QUANT, s, [&]() { return rows_to_codes(m, m->o, M, D, m->ldD8, s); }));
     SF_TRY(timed(m, SF_KC_PROJ, s, [&]() {
       sf::GemmArgs g = gemm_base(m->o, D, b.W_o, D, M, D, D, b.b_o);
       g.h = m->h; g.ldh = D; g.table = m->table; g.ldt = m->modw; g.gate_off = base + 2 * D;
       g.n_slots = n_lat; g.div_ntok = div_n;
+      if (b8) return project8(m, sf::I8_RES_GATE, b8->o, b8->s_o, g, m->ldD8, s);
       return sf::launch_gemm(m->bf16, sf::EPI_RES_GATE, g, s);
     }));
     if (h.has_cross) {
@@ -559,16 +594,19 @@ int run_network(sf_model* m, const float* x, const float* t, int n_lat, int rows
         return sf::launch_gemm(m->bf16, sf::EPI_RES, go, s);
       }));
     }
-    SF_TRY(timed(m, SF_KC_LN, s, [&]() { return ln(base + 3 * D, base + 4 * D, true); }));
+    SF_TRY(timed(m, SF_KC_LN, s, [&]() { return ln_in(base + 3 * D, base + 4 * D); }));
     SF_TRY(timed(m, SF_KC_FC1, s, [&]() {
       sf::GemmArgs g = gemm_base(m->act, D, b.W_fc1, D, M, h.mlp, D, b.b_fc1);
       g.out = m->f; g.ldo = h.mlp;
+      if (b8) return project8(m, sf::I8_GELU, b8->fc1, b8->s_fc1, g, m->ldD8, s);
       return sf::launch_gemm(m->bf16, sf::EPI_GELU, g, s);
     }));
+    if (b8) SF_TRY(timed(m, SF_KC_QUANT, s, [&]() { return rows_to_codes(m, m->f, M, h.mlp, m->ldF8, s); }));
     SF_TRY(timed(m, SF_KC_FC2, s, [&]() {
       sf::GemmArgs g = gemm_base(m->f, h.mlp, b.W_fc2, h.mlp, M, D, h.mlp, b.b_fc2);
       g.h = m->h; g.ldh = D; g.table = m->table; g.ldt = m->modw; g.gate_off = base + 5 * D;
       g.n_slots = n_lat; g.div_ntok = div_n;
+      if (b8) return project8(m, sf::I8_RES_GATE, b8->fc2, b8->s_fc2, g, m->ldF8, s);
       return sf::launch_gemm(m->bf16, sf::EPI_RES_GATE_MLP, g, s);
     }));
   }
@@ -836,6 +874,7 @@ void sf_free(sf_model* m) {
   drop_graphs(m);
   if (m->abar) (void)hipFree(m->abar);
   if (m->qkmem) (void)hipFree(m->qkmem);
+  if (m->mem8) (void)hipFree(m->mem8);
   for (auto& tm : m->timing)
     for (hipEvent_t e : tm.ev) (void)hipEventDestroy(e);
   if (m->wmem) (void)hipFree(m->wmem);
@@ -1177,6 +1216,65 @@ int sf_set_qk(sf_model* m, const sf_qk* p) {
   m->qk_norm = p->norm != 0;
   m->qk_rope = p->rope != nullptr;
   m->qk_on = true;
+  return SF_OK;
+}
+
+int sf_set_int8(sf_model* m, int enable) {
+  if (!m) return SF_E_NOTLOADED;
+  if (enable && !m->bf16) return SF_E_INVAL;
+  if ((enable != 0) == m->int8_on) return SF_OK;
+  if (hipDeviceSynchronize() != hipSuccess) return SF_E_HIP;
+  drop_graphs(m);
+  m->int8_on = false;
+  if (m->mem8) (void)hipFree(m->mem8);
+  m->mem8 = nullptr;
+  if (!enable) return SF_OK;
+  const Header& h = m->hd;
+  const size_t D = h.D, F = h.mlp, M = (size_t)m->max_rows * m->N;
+  const size_t ldD = (D + 15) / 16 * 16, ldF = (F + 15) / 16 * 16;
+  m->ldD8 = (int)ldD;
+  m->ldF8 = (int)ldF;
+  try {
+    m->blk8.resize(h.L);
+  } catch (...) {
+    return SF_E_OOM;
+  }
+  auto carve = [&](char* base) {
+    Carver cv;
+    cv.base = base;
+    for (Block8& b : m->blk8) {
+      b.qkv = cv.take<int8_t>(3 * D * ldD);
+      b.o = cv.take<int8_t>(D * ldD);
+      b.fc1 = cv.take<int8_t>(F * ldD);
+      b.fc2 = cv.take<int8_t>(D * ldF);
+      b.s_qkv = cv.take<float>(3 * D);
+      b.s_o = cv.take<float>(D);
+      b.s_fc1 = cv.take<float>(F);
+      b.s_fc2 = cv.take<float>(D);
+    }
+    m->rows8 = cv.take<int8_t>(M * (ldD > ldF ? ldD : ldF));
+    m->scale8 = cv.take<float>(M);
+    return cv.off;
+  };
+  const size_t bytes = carve(nullptr);
+  if (fail_alloc_after() == 0 || hipMalloc((void**)&m->mem8, bytes) != hipSuccess) {
+    m->mem8 = nullptr;
+    (void)hipGetLastError();
+    return SF_E_OOM;
+  }
+  carve(m->mem8);
+  auto weights = [&](const void* W, size_t N, size_t K, int8_t* codes, size_t ld, float* scale) {
+    return sf::launch_quantize_rows(true, sf::QuantArgs{W, (int64_t)K, (int)N, (int)K, codes, (int64_t)ld, scale}, nullptr);
+  };
+  for (uint32_t l = 0; l < h.L; ++l) {
+    const Block& b = m->blk[l];
+    const Block8& c = m->blk8[l];
+    if (weights(b.W_qkv, 3 * D, D, c.qkv, ldD, c.s_qkv) != hipSuccess || weights(b.W_o, D, D, c.o, ldD, c.s_o) != hipSuccess ||
+        weights(b.W_fc1, F, D, c.fc1, ldD, c.s_fc1) != hipSuccess || weights(b.W_fc2, D, F, c.fc2, ldF, c.s_fc2) != hipSuccess)
+      return SF_E_HIP;
+  }
+  if (hipDeviceSynchronize() != hipSuccess) return SF_E_HIP;
+  m->int8_on = true;
   return SF_OK;
 }
 

@@ -171,3 +171,4 @@ def test_choice_of_8_bit_tiles(tmp_path):
 def test_model_settings_need_a_model():
     L = load_library()
     assert L.sf_set_qk(None, None) == -3
+    assert L.sf_set_int8(None, 1) == -3
