@@ -310,16 +310,17 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_i8_kernel(GemmI8Args 
 }
 
 // Tiles: BM x BN, wave grid, LDS stages, wavefronts per SIMD.
-#define SF_I8_TILES(X)               \
-  X(kI8Deep64, 64, 64, 2, 2, 4, 2)   \
-  X(kI8Tile64, 64, 64, 2, 2, 2, 4)   \
-  X(kI8Tile128, 128, 128, 2, 2, 2, 2) \
+#define SF_I8_TILES(X)                    \
+  X(kI8Deep64, 64, 64, 2, 2, 4, 2)        \
+  X(kI8Tile64, 64, 64, 2, 2, 2, 4)        \
+  X(kI8Deep128, 128, 128, 2, 4, 4, 2)     \
+  X(kI8Tile128, 128, 128, 2, 2, 2, 2)     \
   X(kI8Tile128x192, 128, 192, 2, 2, 2, 2) \
   X(kI8Tile256x192, 256, 192, 4, 2, 2, 2)
 
 template <I8Kind KIND>
 static hipError_t launch_i8(const GemmI8Args& a, hipStream_t s) {
-  switch (choose_gemm_i8_tile(a.M, a.N, a.K)) {
+  switch (choose_gemm_i8_tile(a.M, a.N, a.K, KIND == I8_RES_GATE)) {
 #define SF_I8_CASE(id, bm, bn, wm, wn, st, mw)                                                               \
   case id: {                                                                                                 \
     const int64_t tiles = (((int64_t)a.M + bm - 1) / bm) * (((int64_t)a.N + bn - 1) / bn);                   \
