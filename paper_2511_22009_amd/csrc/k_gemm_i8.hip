@@ -11,7 +11,8 @@
 // outputs, 23 us at the rate of a plain fill, and the first slices' latency. Outputs that are
 // written while the next tile is under way, by workgroups that stay and fetch across tiles,
 // took the second part to 26 us at K = 128, but the larger kernel's loop lost as much.
-#include "sf_device.h"
+#include "sf_ops_device.h"
+#include "sf_ops_rules.h"
 
 namespace sf {
 

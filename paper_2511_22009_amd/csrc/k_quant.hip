@@ -3,7 +3,7 @@
 // written once), so a wavefront holds its whole row in registers between the maximum and the
 // codes: 16384 x 4608 bf16 takes 46 us, 5.0 TB/s; reading the row again for the codes, an
 // element per lane, took 134.
-#include "sf_device.h"
+#include "sf_ops_device.h"
 
 namespace sf {
 

@@ -14,7 +14,7 @@
 // 41 to 42, and 25 instead of 22 for the clip.)
 #include <cmath>
 
-#include "sf_device.h"
+#include "sf_ops_device.h"
 #include "streamflow.h"
 
 namespace sf {

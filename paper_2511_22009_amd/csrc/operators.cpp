@@ -6,7 +6,7 @@
 #include <cmath>
 #include <cstdint>
 
-#include "sf_launch.h"
+#include "sf_ops.h"
 
 namespace sf {
 

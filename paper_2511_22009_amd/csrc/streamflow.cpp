@@ -15,7 +15,7 @@
 #include <new>
 #include <vector>
 
-#include "sf_launch.h"
+#include "sf_ops.h"
 
 namespace sf {
 

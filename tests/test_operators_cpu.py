@@ -129,7 +129,7 @@ def test_python_refusals_without_a_gpu():
 
 TILES = r"""
 #include <cstdio>
-#include "sf_rules.h"
+#include "sf_ops_rules.h"
 int main() {
   const long sizes[] = {1, 2, 31, 64, 65, 129, 777, 1023, 4096, 16384, 70000, 1 << 20, 2147483647L};
   const long Ks[] = {1, 16, 100, 768, 4321, 131071};
