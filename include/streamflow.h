@@ -328,7 +328,8 @@ int sf_timing_read(sf_model* m, int kc, double* total_ms, long* launches);
  * whatever is computed from it is NaN.
  * x: [rows][cols], row length ldx, element type SF_PREC_BF16 or SF_PREC_FP32; codes:
  * [rows][cols], row length ldc, a multiple of 16 at an address that is one (the bytes past
- * cols stay as they are); scale: [rows]. cols 1..1048576. SF_E_INVAL otherwise. */
+ * cols stay as they are); scale: [rows]. rows 0..2^31 - 1, cols 1..1048576. SF_E_INVAL
+ * otherwise. */
 int sf_quantize_rows(const void* x, int type, long long rows, int cols, long long ldx, signed char* codes,
                      long long ldc, float* scale, void* hip_stream);
 
@@ -336,7 +337,8 @@ int sf_quantize_rows(const void* x, int type, long long rows, int cols, long lon
  * 8 bits: tokens A, weights B stored [out][in]):
  *   out[m][n] = (sum_k A[m][k] B[n][k]) a_scale[m] b_scale[n] + bias[n]
  * The sum is exact (32-bit integers); its conversion to fp32, the two products and the sum
- * with the bias are rounded to fp32 one after the other, and to the output's type last.
+ * with the bias are rounded to fp32 one after the other (the sum may take the last product
+ * unrounded), and to the output's type last.
  * a: [M][K], row length lda; b: [N][K], row length ldb; both row lengths multiples of 16
  * and at least K rounded up to one, at addresses that are multiples of 16, every row
  * readable to that length (what stands past K is not used). bias: fp32 [N] or NULL. out:
@@ -370,8 +372,9 @@ typedef struct sf_rope {
 } sf_rope;
 
 /* A tensor of heads [rows][tokens][heads][dh], read from `in` and written to `out`, which is
- * `in` itself with the same strides or does not overlap it. The dims of a head are adjacent;
- * the strides (in elements) are free, and those of `in` may be 0. */
+ * `in` itself with the same strides or does not overlap it, nor, in a call with q and k, the
+ * other's tensors. The dims of a head are adjacent; the strides (in elements) are free, and
+ * those of `in` may be 0. */
 typedef struct sf_heads {
   const void* in;
   void* out;
@@ -415,7 +418,9 @@ typedef struct sf_qk {
  * sf_free) and drops cached graphs. SF_E_INVAL for neither norm nor rope, gains without norm, or
  * a rope that sf_rotate would refuse or whose axes are not 2; nothing changes then. On
  * SF_E_OOM or SF_E_HIP the treatment is cleared. The allocation fails when
- * SF_FAIL_ALLOC_AFTER is 0, to exercise that path. */
+ * SF_FAIL_ALLOC_AFTER is 0, to exercise that path. A graph that the caller captured from the
+ * model's calls keeps the treatment it was captured with only until the next set or clear, which
+ * frees what it reads: capture again. */
 int sf_set_qk(sf_model* m, const sf_qk* p);
 
 /* The four projections of every block (QKV, attention output, MLP up and down) in 8 bits:
@@ -423,14 +428,18 @@ int sf_set_qk(sf_model* m, const sf_qk* p);
  * model's bf16 weights, and their inputs as codes with a scale per token, made as they pass
  * (sf_quantize_rows; LayerNorm + modulate leaves codes itself, from fp32), multiplied as in
  * sf_matmul_i8 with the epilogues of the bf16 projections. Everything else, the
- * cross-attention's projections included, stays as it is. */
+ * cross-attention's projections included, stays as it is. It pays in wide blocks: a velocity of
+ * four 1024^2 rows of width 1152 takes 1.65 ms instead of 1.85 (two blocks), of four 512^2 rows of
+ * that width 0.77 instead of 0.85 (four blocks), of width 768 1.39 instead of 1.32 (twelve): there
+ * the passes that make codes cost more than the products save. */
 
 /* Enable (nonzero) or disable (0, the default) 8-bit projections in sf_velocity,
  * sf_stream_step and sf_residual. Needs a model loaded in SF_PREC_BF16 (SF_E_INVAL
  * otherwise). Synchronous: waits for the device, makes the codes (one device allocation of
  * about half the blocks' weights plus, per row of the workspace, the widest input, held until it
  * is disabled or sf_free) and drops cached graphs; the bf16 weights stay. While
- * enabled SF_BUF_ACT does not follow the calls. On SF_E_OOM or SF_E_HIP it is
+ * enabled SF_BUF_ACT does not follow the calls. Disabling frees what a graph that the caller
+ * captured meanwhile reads. On SF_E_OOM or SF_E_HIP it is
  * disabled; the allocation fails when SF_FAIL_ALLOC_AFTER is 0, to exercise that path. */
 int sf_set_int8(sf_model* m, int enable);
 

@@ -7,11 +7,13 @@
 // lanes hold a head, and its sum of squares is a butterfly over them.
 //
 // Bandwidth bounds it: the 8 x 30 x 52 tokens of a clip with 16 heads of 128 dims (102 MB) take
-// 21 us, 4.8 TB/s; q and k of 16384 tokens with 32 heads of 64 dims (134 MB, adjacent pairs) 29
-// us. With 72 dims a head fills 9 of its 16 lanes, and halves move in pieces of 8 bytes: 42 us
-// for 151 MB. (12 pairs to a lane, which fill 3 lanes of 4, take 46 us: lanes 48 bytes apart;
-// angles per wavefront instead of per workgroup 44; wavefronts by tokens instead of by heads
-// 41 to 42, and 25 instead of 22 for the clip.)
+// 21 us, 4.8 TB/s; q and k of 16384 tokens with 32 heads of 64 dims (134 MB, adjacent pairs) 30
+// us, as halves 33. With 72 dims a head fills 9 of its 16 lanes, and halves move in pieces of 8
+// bytes: 42 us for 151 MB. Groups of 9 lanes, their sums in thirds through the LDS crossbar, take
+// 41, but 43 instead of 40 where q and k lie packed; pieces of 16 bytes, eight pairs to a lane, the
+// same 34 for 128 dims and 4.5 instead of 3.6 for a single token. (12 pairs to a lane, which fill 3
+// lanes of 4, take 46 us: lanes 48 bytes apart; angles per wavefront instead of per workgroup 44;
+// wavefronts by tokens instead of by heads 41 to 42, and 25 instead of 22 for the clip.)
 #include <cmath>
 
 #include "sf_ops_device.h"

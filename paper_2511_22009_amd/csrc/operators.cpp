@@ -1,8 +1,9 @@
-// C ABI of the operators on the caller's own tensors: argument checks and one launch each.
+// C ABI of the operators on the caller's own tensors: argument checks and launches.
 #include "streamflow.h"
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -38,7 +39,10 @@ static_assert(sf::kRopeAxes == SF_ROPE_AXES, "axes of a rotation");
 
 bool is_type(int t) { return t == SF_PREC_BF16 || t == SF_PREC_FP32; }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-int status(hipError_t e) { return e == hipSuccess ? SF_OK : SF_E_HIP; }
+
+// Rows (columns, tokens) of one launch: a grid holds less than 2^32 threads, and a row takes at
+// most 256. Longer calls are several launches.
+constexpr int64_t kMostRows = 1 << 23;
 
 // Whether every entry of the output has a place of its own as far as a stride of 0 tells.
 bool own_places(const sf_heads& t, int rows, int tokens) {
@@ -67,15 +71,27 @@ int rope_call(const sf_heads* q, const sf_heads* k, const float* q_gain, const f
   if (k && k->heads > 0 && (!k->in || !k->out || !own_places(*k, rows, tokens))) return SF_E_INVAL;
   a.t[0] = take_heads(*q, q_gain);
   if (k) a.t[1] = take_heads(*k, k_gain);
-  a.rows = rows;
-  a.tokens = tokens;
   a.dh = dh;
-  a.div_tok = sf::make_fastdiv((uint32_t)tokens);
   a.eps = eps;
   a.inverse = inverse != 0;
-  a.pos = pos;
   a.pos_row = pos_row;
-  return status(sf::launch_rope(type == SF_PREC_BF16, norm, rope != nullptr, a, (hipStream_t)stream));
+  const int64_t most_tokens = std::min<int64_t>(tokens, kMostRows), most_rows = kMostRows / most_tokens;
+  for (int64_t row = 0; row < rows; row += most_rows)
+    for (int64_t token = 0; token < tokens; token += most_tokens) {
+      sf::RopeArgs part = a;
+      part.rows = (int)std::min(most_rows, rows - row);
+      part.tokens = (int)std::min(most_tokens, tokens - token);
+      part.div_tok = sf::make_fastdiv((uint32_t)part.tokens);
+      for (sf::RopeHeads& t : part.t) {
+        const int64_t size = type == SF_PREC_BF16 ? 2 : 4;
+        if (t.in) t.in += size * (row * t.in_row + token * t.in_tok);
+        if (t.out) t.out += size * (row * t.out_row + token * t.out_tok);
+      }
+      if (pos) part.pos = pos + row * pos_row + token * a.axes;
+      const hipError_t e = sf::launch_rope(type == SF_PREC_BF16, norm, rope != nullptr, part, (hipStream_t)stream);
+      if (e != hipSuccess) return SF_E_HIP;
+    }
+  return SF_OK;
 }
 
 }  // namespace
@@ -87,8 +103,12 @@ int sf_quantize_rows(const void* x, int type, long long rows, int cols, long lon
   if (!is_type(type) || rows < 0 || rows > 0x7fffffff || cols < 1 || cols > (1 << 20)) return SF_E_INVAL;
   if (rows == 0) return SF_OK;
   if (!x || !codes || !scale || ldx < 0 || ldc % 16 || ldc < cols || !aligned16(codes)) return SF_E_INVAL;
-  const sf::QuantArgs a{x, ldx, (int)rows, cols, (int8_t*)codes, ldc, scale};
-  return status(sf::launch_quantize_rows(type == SF_PREC_BF16, a, (hipStream_t)stream));
+  for (int64_t row = 0; row < rows; row += kMostRows) {
+    const char* const from = (const char*)x + row * ldx * (type == SF_PREC_BF16 ? 2 : 4);
+    const sf::QuantArgs a{from, ldx, (int)std::min<int64_t>(kMostRows, rows - row), cols, (int8_t*)codes + row * ldc, ldc, scale + row};
+    if (sf::launch_quantize_rows(type == SF_PREC_BF16, a, (hipStream_t)stream) != hipSuccess) return SF_E_HIP;
+  }
+  return SF_OK;
 }
 
 int sf_matmul_i8(const signed char* a, long long lda, const float* a_scale, const signed char* b, long long ldb,
@@ -101,8 +121,16 @@ int sf_matmul_i8(const signed char* a, long long lda, const float* a_scale, cons
   if (!a || !b || !a_scale || !b_scale || !out || !aligned16(a) || !aligned16(b) || lda % 16 || ldb % 16 || lda < need ||
       ldb < need || lda >= kMostLd || ldb >= kMostLd || ldo < N)
     return SF_E_INVAL;
-  const sf::GemmI8Args g{(const int8_t*)a, (const int8_t*)b, (int)lda, (int)ldb, M, N, K, a_scale, b_scale, bias, out, ldo, {}};
-  return status(sf::launch_gemm_i8(out_type == SF_PREC_BF16 ? sf::I8_BF16 : sf::I8_F32, g, (hipStream_t)stream));
+  for (int64_t m = 0; m < M; m += kMostRows)
+    for (int64_t n = 0; n < N; n += kMostRows) {
+      char* const to = (char*)out + (m * ldo + n) * (out_type == SF_PREC_BF16 ? 2 : 4);
+      const sf::GemmI8Args g{(const int8_t*)a + m * lda, (const int8_t*)b + n * ldb, (int)lda, (int)ldb,
+                             (int)std::min<int64_t>(kMostRows, M - m), (int)std::min<int64_t>(kMostRows, N - n), K,
+                             a_scale + m, b_scale + n, bias ? bias + n : nullptr, to, ldo, {}};
+      const hipError_t e = sf::launch_gemm_i8(out_type == SF_PREC_BF16 ? sf::I8_BF16 : sf::I8_F32, g, (hipStream_t)stream);
+      if (e != hipSuccess) return SF_E_HIP;
+    }
+  return SF_OK;
 }
 
 int sf_rotate(const sf_heads* x, int type, int rows, int tokens, int dh, const sf_rope* rope, const float* pos,

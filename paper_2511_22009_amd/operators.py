@@ -34,11 +34,11 @@ def _raw_stream(index):
 def _stream_of(index, stream):
     """The raw stream of a call, and `stream` itself where it is not the current one."""
     raw = _raw_stream(index)
-    if stream is None or stream.cuda_stream == raw:
+    if stream is None:
         return raw, None
     if stream.device.index != index:
         raise ValueError(f"stream of {stream.device}, tensors on cuda:{index}")
-    return stream.cuda_stream, stream
+    return stream.cuda_stream, None if stream.cuda_stream == raw else stream
 
 
 def _empty(side, sizes, strides, dtype, device):
@@ -214,6 +214,10 @@ def _heads(x, what, out, side):
             with torch.cuda.stream(side):
                 out = torch.empty_like(x)
         so = out.stride()
+        if so[3] != 1:  # an x whose entries overlap (windows): its strides' order is not the output's
+            n, t, h, d = x.shape
+            so = (t * h * d, h * d, d, 1)
+            out = _empty(side, x.shape, so, x.dtype, x.device)
     else:
         _tensor(out, what + " out", (x.dtype,))
         so = out.stride()
@@ -225,6 +229,8 @@ def _heads(x, what, out, side):
 
 
 def _positions(pos, rotary, shape, index):
+    if not isinstance(rotary, Rotary):
+        raise TypeError(f"rotary: expected a Rotary, got {type(rotary).__name__}")
     if not (isinstance(pos, _T) and pos.is_cuda and pos.dtype is _FP32):
         _tensor(pos, "positions", (_FP32,))
     rows, tokens, axes = shape[0], shape[1], len(rotary.dims)
@@ -257,7 +263,7 @@ def qk_norm_rotate(q, k, q_gain=None, k_gain=None, positions=None, rotary=None, 
     """Queries q [rows, tokens, heads, dims] and keys k (the same with their own number of
     heads, or None), every head divided by its root mean square (sqrt(mean + eps)),
     multiplied by its gain (fp32 [dims], None: 1) and, with `rotary`, turned by its token's
-    position. Returns (q, k); `out` = (q, k) takes the results and may be the inputs."""
+    position. Returns (q, k); `out` = (q, k) takes the results and may be the inputs (of each its own)."""
     shape = _check_heads(q, "q")
     rows, tokens, _, dims = shape
     index, dtype = q.get_device(), q.dtype

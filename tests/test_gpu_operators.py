@@ -533,6 +533,81 @@ def test_operators_on_another_stream_and_in_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(out, eager))
 
 
+def test_operators_one_after_the_other():
+    """Tokens to codes, their product with weights, norm and rotation of its queries and keys,
+    against the same in 64 bits from the codes. The product is rounded to bf16 before the norm
+    (with its 3 fp32 roundings within d = 1.001 2^-8, so a normalised element is off by less than
+    2 d / (1 - d) of itself), the result once more: 2.04 2^-8 of the pair and 1.02 2^-8 of the value."""
+    from paper_2511_22009_amd import quantize_rows
+    for seed in (31, 35):
+        x, w, sw, gq, gk, pos, r, H = args = chain_inputs(seed)
+        a, sa = quantize_rows(x)
+        v = (a.double() @ w.double().t()) * sa.double()[:, None] * sw.double()
+        v = v.view(1, x.shape[0], 3 * H, -1)
+        for got, gain, part in zip(chain(*args), (gq, gk), (v[:, :, :H], v[:, :, H:2 * H])):
+            want, size = plain_turn(plain_qk(part, gain, 1e-6), pos, r.dims, r.layout)
+            assert worst(got, want, 2.04 * 2.0 ** -8 * size + 1.02 * 2.0 ** -8 * want.abs()) <= 1.0
+
+
+@pytest.mark.parametrize("layout,dims", [("adjacent", [8]), ("halves", [4, 4])])
+def test_rope_of_overlapping_windows(layout, dims):
+    """Inputs whose entries overlap (windows, expanded heads): the outputs have places of their own."""
+    from paper_2511_22009_amd import Rotary, qk_norm_rotate, rotate
+    g = gen(51)
+    r, base, pos = Rotary(dims, layout=layout), randn(g, 400), positions(g, 2, 5, len(dims))
+    for strides in ((50, 9, 1, 1), (0, 3, 1, 1), (0, 1, 1, 1), (40, 8, 0, 1), (0, 0, 8, 1), (40, 8, 2, 1)):
+        x = base.as_strided((2, 5, 4, 8), strides)
+        apart = x.clone(memory_format=torch.contiguous_format)
+        assert torch.equal(rotate(x, pos, r), rotate(apart, pos, r))
+        for got, want in zip(qk_norm_rotate(x, x, None, None, pos, r), qk_norm_rotate(apart, apart, None, None, pos, r)):
+            assert torch.equal(got, want)
+
+
+# a launch takes 2^23 rows, so these are several
+LONG = 2 ** 23
+
+
+def test_more_rows_to_codes_than_a_launch_takes():
+    from paper_2511_22009_amd import quantize_rows
+    x = randn(gen(52), LONG + 5, 16, dtype=BF16)
+    codes, scale = quantize_rows(x)
+    for part in (slice(0, 1000), slice(LONG - 1000, LONG), slice(LONG, LONG + 5)):
+        q, s = plain_quantize(x[part])
+        np.testing.assert_array_equal(codes[part].cpu().numpy(), q)
+        np.testing.assert_array_equal(scale[part].cpu().numpy(), s)
+
+
+@pytest.mark.parametrize("M,N", [(LONG + 3, 2), (2, LONG + 9), (1, 2 * LONG + 1)])
+def test_larger_products_than_a_launch_takes(M, N):
+    """Codes of few values: every result is a small whole number, exact in fp32."""
+    from paper_2511_22009_amd import matmul_i8
+    g = gen(53)
+    a, b = (torch.randint(-9, 10, (n, 16), generator=g, device="cuda", dtype=torch.int8) for n in (M, N))
+    sa, sb = (torch.randint(1, 5, (n,), generator=g, device="cuda").float() for n in (M, N))
+    bias = torch.randint(-50, 50, (N,), generator=g, device="cuda").float()
+    got = matmul_i8(a, sa, b, sb, bias, dtype=FP32)
+    want = torch.zeros(M, N, dtype=FP32, device="cuda")
+    for k in range(16):
+        want += a[:, k, None].float() * b[None, :, k].float()
+    assert torch.equal(got, want * sa[:, None] * sb + bias)
+
+
+@pytest.mark.parametrize("rows,tokens", [(2, LONG + 3), (LONG // 4 + 1, 5)])
+def test_more_tokens_turned_than_a_launch_takes(rows, tokens):
+    from paper_2511_22009_amd import Rotary, qk_norm_rotate, rotate
+    g = gen(54)
+    r = Rotary([4])
+    x, pos = randn(g, rows, tokens, 1, 4, dtype=BF16), positions(g, rows, tokens, 1)
+    turned, (normed, _) = rotate(x, pos, r), qk_norm_rotate(x, None, None, None, pos, r)
+    for i in {0, rows // 2, rows - 2, rows - 1}:
+        for part in (slice(0, 70), slice(max(0, tokens - 70), tokens)):
+            y, p = x[i:i + 1, part].contiguous(), pos[i:i + 1, part].contiguous()
+            assert torch.equal(turned[i:i + 1, part], rotate(y, p, r))
+            assert torch.equal(normed[i:i + 1, part], qk_norm_rotate(y, None, None, None, p, r)[0])
+    shared = rotate(x, pos[0], r)
+    assert torch.equal(shared[-1, -70:], rotate(x[-1:, -70:], pos[0, -70:], r)[0])
+
+
 def test_python_refusals():
     from paper_2511_22009_amd import Rotary, SFError, matmul_i8, qk_norm_rotate, quantize_rows, rotate
     g = gen(41)
@@ -570,6 +645,8 @@ def test_python_refusals():
         rotate(h.half(), pos, r)
     with pytest.raises(TypeError):
         rotate(h, pos.double(), r)
+    with pytest.raises(TypeError):
+        rotate(h, pos, None)
     for bad in (pos[:, :1], pos[:2], pos[None].expand(3, 3, 2), pos.t().contiguous().t()):
         with pytest.raises(ValueError):
             rotate(h, bad, r)
@@ -593,3 +670,12 @@ def test_python_refusals():
         qk_norm_rotate(h, h, None, None, None, r)
     with pytest.raises(SFError):
         qk_norm_rotate(h, h, eps=-1.0)
+
+
+def test_a_stream_of_another_device_is_refused():
+    from types import SimpleNamespace
+
+    from paper_2511_22009_amd import quantize_rows
+    other = SimpleNamespace(cuda_stream=torch.cuda.current_stream().cuda_stream, device=torch.device("cuda", 1))
+    with pytest.raises(ValueError):
+        quantize_rows(torch.ones((2, 16), device="cuda"), stream=other)
