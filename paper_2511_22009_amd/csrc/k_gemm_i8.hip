@@ -1,16 +1,17 @@
 // Products of 8-bit codes on the matrix cores, out[m][n] = (sum_k A[m][k] B[n][k]) sa[m] sb[n]
 // + bias[n], or, in a network's blocks, that value's GELU, its place among the heads' queries,
-// keys and transposed values, or h += gate times it: v_mfma_i32_32x32x32_i8, whose 32-bit sums are exact for every K the entry point
-// allows, so no choice of tile changes a bit of a result. The weights are the first operand, so
-// a lane ends up with four adjacent output columns of one row.
+// keys and transposed values, or h += gate times it: v_mfma_i32_32x32x32_i8, whose 32-bit sums
+// are exact for every K the entry point allows, so no choice of tile changes a bit of a result.
+// The weights are the first operand, so a lane ends up with four adjacent output columns of one
+// row.
 //
 // What bounds it: the matrix cores at the clock that their power leaves, and what a tile costs
-// besides its slices. 8192 x 8192 x 8192 takes 444 us (2470 TOP/s; a 256 x 256 tile reaches 398
-// us there, 2760, but loses below K = 4096 or so), 16384 x 4608 x 1152 takes 98 us. Of those 98,
-// 65 go with K (every further 1152 columns cost them again) and 33 do not: the 151 MB of
-// outputs, 23 us at the rate of a plain fill, and the first slices' latency. Outputs that are
-// written while the next tile is under way, by workgroups that stay and fetch across tiles,
-// took the second part to 26 us at K = 128, but the larger kernel's loop lost as much.
+// besides its slices. 8192 x 8192 x 8192 takes 440 us (2500 TOP/s), 16384 x 4608 x 1152 102 us
+// (1700), of which the 151 MB of outputs are 23 at the rate of a plain fill. Where a CU has one
+// tile only, the L2 bounds it: 1023 x 777 x 4321 moves 64 x 64 tiles' slices at 75 bytes per ns and
+// CU, 14 us. Outputs that are written while the next tile is under way, by workgroups that stay and
+// fetch across tiles, made a product of K = 128 a fifth faster, but the larger kernel's loop
+// lost as much elsewhere; so did slices of 64, splits of K over wavefronts and more stages.
 #include "sf_ops_device.h"
 #include "sf_ops_rules.h"
 
@@ -219,15 +220,81 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_i8_kernel(GemmI8Args 
     main_loop(std::true_type{});
   else
     main_loop(std::false_type{});
-  __builtin_amdgcn_s_waitcnt(0);  // the loads past K land before the LDS is given up
+  __builtin_amdgcn_s_waitcnt(0);  // the loads past K land before the LDS is used again or given up
 
-  // lane (l32, g) holds row l32 of each block and the columns 8 q + 4 g + 0..3, and stores
-  // straight from its registers (through LDS, in whole rows of a wavefront's part, the
-  // launches took as long or up to 10 % longer). bf16 outputs leave in eights: lanes l and l + 32
-  // exchange halves, then the first has the eight columns of group q, the second those of q + 1
-  constexpr bool kEights = KIND != I8_F32 && KIND != I8_RES_GATE;
-  constexpr int QS = kEights ? 2 : 1;  // groups of four columns to a store
+  // lane (l32, g) holds row l32 of each block and the columns 8 q + 4 g + 0..3
   typedef uint32_t out16 __attribute__((ext_vector_type(4), aligned(2)));
+  if constexpr (KIND == I8_BF16 || KIND == I8_F32 || KIND == I8_GELU) {
+    // Every wavefront passes its part of the tile through LDS of its own, 32 rows of JG blocks at
+    // a time, so that stores leave in whole rows of the part, and past the L2: a launch ends
+    // without a cache full of outputs, 16384 x 4608 x 1152 into memory that no cache holds after
+    // 109 us, with ordinary stores 120, straight from the registers in pieces of 32 bytes 123
+    // (128 x 192; 103, 123 and 163 for 256 x 256).
+    typedef std::conditional_t<KIND == I8_F32, float, bf16> OT;
+    constexpr int E = 16 / (int)sizeof(OT), JG = KIND == I8_F32 ? 1 : TN;
+    constexpr int PITCH = JG * 32 * (int)sizeof(OT) + 16, CPW = JG * 32 / E, HALF = WM * WN / 2;
+    static_assert(HALF * 32 * PITCH <= SLICE, "the parts of half the wavefronts fit a stage");
+    char* const part = (wave < HALF ? st0 + wave * 32 * PITCH : st1 + (wave - HALF) * 32 * PITCH);
+    __syncthreads();
+#pragma unroll
+    for (int j0 = 0; j0 < TN; j0 += JG) {
+      float sb[JG][16], bias[JG][16];
+#pragma unroll
+      for (int j = 0; j < JG; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int from = 8 * (r >> 2) + 4 * g + (r & 3);
+          sb[j][r] = __shfl(sb_v[j0 + j], from);
+          bias[j][r] = __shfl(bias_v[j0 + j], from);
+        }
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int j = 0; j < JG; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              v[e] = (float)acc[i][j0 + j][4 * q + e] * sa_v[i] * sb[j][4 * q + e] + bias[j][4 * q + e];
+              if constexpr (KIND == I8_GELU) v[e] = gelu_tanh(v[e]);
+            }
+            char* const p = part + l32 * PITCH + (j * 32 + q * 8 + g * 4) * (int)sizeof(OT);
+            if constexpr (KIND == I8_F32)
+              *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+            else
+              *(uint2*)p = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+          }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int u = 0; u < 32 * CPW / 64; ++u) {
+          const int c = u * 64 + lane, r = c / CPW, cc = c - r * CPW;
+          const u32x4 o = *(const u32x4*)(part + r * PITCH + cc * 16);
+          const int m = m0 + (wm * TM + i) * 32 + r, n = n0 + (wn * TN + j0) * 32 + cc * E;
+          OT* const to = (OT*)a.out + (int64_t)m * a.ldo + n;
+          if (m < a.M && n + E <= a.N) {
+            __builtin_nontemporal_store(o, (out16*)to);
+          } else if (m < a.M) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+              if (n + e < a.N) {
+                if constexpr (KIND == I8_F32)
+                  to[e] = __uint_as_float(o[e]);
+                else
+                  ((uint16_t*)to)[e] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
+              }
+          }
+        }
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+    return;
+  }
+
+  // The others store straight from the registers. q, k and v leave in eights: lanes l and l + 32
+  // exchange halves, then the first has the eight columns of group q, the second those of q + 1.
+  constexpr bool kEights = KIND == I8_QKV;
+  constexpr int QS = kEights ? 2 : 1;  // groups of four columns to a store
 #pragma unroll
   for (int j = 0; j < TN; ++j) {
     // the residual and the gates of a block column are loaded before any is used (rows past M
@@ -262,52 +329,29 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_i8_kernel(GemmI8Args 
         const int m = m0 + (wm * TM + i) * 32 + l32;
         float v[4 * QS];
 #pragma unroll
-        for (int r = 0; r < 4 * QS; ++r) {
-          v[r] = (float)acc[i][j][4 * q + r] * sa_v[i] * sb[r] + bias[r];
-          if constexpr (KIND == I8_GELU) v[r] = gelu_tanh(v[r]);
-        }
+        for (int r = 0; r < 4 * QS; ++r) v[r] = (float)acc[i][j][4 * q + r] * sa_v[i] * sb[r] + bias[r];
         if constexpr (KIND == I8_RES_GATE) {
           f32x4 o = h[q][i];
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[e] += gate[q][i][e] * v[e];
           if (m < a.M && n < a.N) *(f32x4*)(a.e.h + (size_t)m * a.e.ldh + n) = o;
-        } else if constexpr (KIND == I8_F32) {
-          float* const p = (float*)a.out + (int64_t)m * a.ldo + n;
-          if (m < a.M && n + 4 <= a.N) {
-            *(out16*)p = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-          } else if (m < a.M) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (n + e < a.N) p[e] = v[e];
-          }
-        } else {
+        } else if constexpr (KIND == I8_QKV) {
           const auto x = __builtin_amdgcn_permlane32_swap(pack_bf16(v[0], v[1]), pack_bf16(v[4], v[5]), false, false);
           const auto y = __builtin_amdgcn_permlane32_swap(pack_bf16(v[2], v[3]), pack_bf16(v[6], v[7]), false, false);
           const u32x4 o = {x[0], y[0], x[1], y[1]};
-          if constexpr (KIND == I8_QKV) {
-            // the eight columns belong to one head (widths of heads are multiples of eight)
-            if (m >= a.M || n >= a.N) continue;
-            const int part = (int)fdiv((uint32_t)n, a.e.div_D), rem = n - part * a.e.D;
-            const int head = (int)fdiv((uint32_t)rem, a.e.div_dh), d = rem - head * a.e.dh;
-            const int r = (int)fdiv((uint32_t)m, a.e.div_ntok), tok = m - r * a.e.ntok;
-            const size_t bh = (size_t)r * a.e.heads + head;
-            if (part < 2) {
-              *(u32x4*)((bf16*)(part == 0 ? a.e.q : a.e.k) + (bh * a.e.ntok + tok) * a.e.dh + d) = o;
-            } else {
-              // transposed, adjacent lanes adjacent tokens (in groups of four, vt_pos)
-              uint16_t* const vt = (uint16_t*)a.e.vT + (bh * a.e.dh + d) * a.e.ldv + vt_pos(tok);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) vt[(size_t)e * a.e.ldv] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
-            }
+          // the eight columns belong to one head (widths of heads are multiples of eight)
+          if (m >= a.M || n >= a.N) continue;
+          const int part = (int)fdiv((uint32_t)n, a.e.div_D), rem = n - part * a.e.D;
+          const int head = (int)fdiv((uint32_t)rem, a.e.div_dh), d = rem - head * a.e.dh;
+          const int r = (int)fdiv((uint32_t)m, a.e.div_ntok), tok = m - r * a.e.ntok;
+          const size_t bh = (size_t)r * a.e.heads + head;
+          if (part < 2) {
+            *(u32x4*)((bf16*)(part == 0 ? a.e.q : a.e.k) + (bh * a.e.ntok + tok) * a.e.dh + d) = o;
           } else {
-            bf16* const p = (bf16*)a.out + (int64_t)m * a.ldo + n;
-            if (m < a.M && n + 8 <= a.N) {
-              *(out16*)p = o;
-            } else if (m < a.M) {
+            // transposed, adjacent lanes adjacent tokens (in groups of four, vt_pos)
+            uint16_t* const vt = (uint16_t*)a.e.vT + (bh * a.e.dh + d) * a.e.ldv + vt_pos(tok);
 #pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (n + e < a.N) ((uint16_t*)p)[e] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
-            }
+            for (int e = 0; e < 8; ++e) vt[(size_t)e * a.e.ldv] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
           }
         }
       }
@@ -322,16 +366,19 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_i8_kernel(GemmI8Args 
   X(kI8Deep128, 128, 128, 2, 4, 4, 2)     \
   X(kI8Tile128, 128, 128, 2, 2, 2, 2)     \
   X(kI8Tile128x192, 128, 192, 2, 2, 2, 2) \
-  X(kI8Tile256x192, 256, 192, 4, 2, 2, 2)
+  X(kI8Tile192x256, 192, 256, 2, 4, 2, 2) \
+  X(kI8Tile256x256, 256, 256, 2, 4, 2, 2)
 
 template <I8Kind KIND>
 static hipError_t launch_i8(const GemmI8Args& a, hipStream_t s) {
-  switch (choose_gemm_i8_tile(a.M, a.N, a.K, KIND == I8_RES_GATE)) {
+  constexpr bool kHeavy = KIND == I8_QKV || KIND == I8_GELU || KIND == I8_RES_GATE;
+  switch (choose_gemm_i8_tile(a.M, a.N, a.K, kHeavy, KIND == I8_RES_GATE)) {
 #define SF_I8_CASE(id, bm, bn, wm, wn, st, mw)                                                               \
   case id: {                                                                                                 \
     const int64_t tiles = (((int64_t)a.M + bm - 1) / bm) * (((int64_t)a.N + bn - 1) / bn);                   \
     if (tiles > 0x7fffffff) return hipErrorInvalidValue;                                                     \
-    launch(gemm_i8_kernel<bm, bn, wm, wn, st, mw, KIND>, dim3((uint32_t)tiles), dim3(wm * wn * 64), 0, s, a);  \
+    if constexpr (!(kHeavy && id == kI8Tile256x256)) /* never chosen */                                     \
+      launch(gemm_i8_kernel<bm, bn, wm, wn, st, mw, KIND>, dim3((uint32_t)tiles), dim3(wm * wn * 64), 0, s, a); \
     break;                                                                                                   \
   }
     SF_I8_TILES(SF_I8_CASE)

@@ -134,22 +134,22 @@ int main() {
   const long sizes[] = {1, 2, 31, 64, 65, 129, 777, 1023, 4096, 16384, 70000, 1 << 20, 2147483647L};
   const long Ks[] = {1, 16, 100, 768, 4321, 131071};
   const auto rounds = [](long M, long N, long bm, long bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
-  const bool kinds[] = {false, true};
-  for (const bool res : kinds)
+  for (int kind = 0; kind < 3; ++kind)  // a short epilogue, a long one, with the residual
     for (long M : sizes)
       for (long N : sizes)
         for (long K : Ks) {
-          const auto t = sf::choose_gemm_i8_tile(M, N, K, res);
-          if (t < sf::kI8Deep64 || t > sf::kI8Tile256x192) return std::printf("%ld %ld %ld: %d\n", M, N, K, (int)t), 1;
-          // one per CU: never more than one round of them
-          if (t == sf::kI8Tile256x192 && rounds(M, N, 256, 192) > 256) return 2;
-          if (t == sf::kI8Deep128 && rounds(M, N, 128, 128) > 256) return 3;
+          const auto t = sf::choose_gemm_i8_tile(M, N, K, kind > 0, kind == 2);
+          if (t < sf::kI8Deep64 || t > sf::kI8Tile256x256) return std::printf("%ld %ld %ld: %d\n", M, N, K, (int)t), 1;
+          // long epilogues: a single round of the tiles that a CU holds one of
+          if (kind && t == sf::kI8Tile256x256) return 2;
+          if (kind && t == sf::kI8Tile192x256 && rounds(M, N, 192, 256) > 256) return 2;
+          if (kind && t == sf::kI8Deep128 && rounds(M, N, 128, 128) > 256) return 3;
           if (M > 60000 && N > 60000 && t < sf::kI8Tile128) return std::printf("%ld %ld %ld\n", M, N, K), 4;
           if (M <= 64 && N <= 4096 && t > sf::kI8Tile64) return std::printf("%ld %ld %ld\n", M, N, K), 5;
         }
-  const auto at = [](long M, long N, long K) { return sf::choose_gemm_i8_tile(M, N, K, false); };
-  if (at(4096, 2304, 768) != sf::kI8Tile256x192 || at(16384, 4608, 1152) != sf::kI8Tile128x192 ||
-      at(1500, 8192, 8192) != sf::kI8Tile128 || at(1023, 777, 4321) != sf::kI8Deep64 || at(4096, 768, 4608) != sf::kI8Deep128)
+  const auto at = [](long M, long N, long K) { return sf::choose_gemm_i8_tile(M, N, K, false, false); };
+  if (at(4096, 2304, 768) != sf::kI8Tile192x256 || at(16384, 4608, 1152) != sf::kI8Tile256x256 ||
+      at(16384, 1152, 4608) != sf::kI8Tile128x192 || at(1023, 777, 4321) != sf::kI8Deep64 || at(4096, 768, 4608) != sf::kI8Deep128)
     return 6;
   std::printf("ok\n");
   return 0;
