@@ -172,6 +172,21 @@ def test_matmul_i8(M, N, K, dtype):
     assert torch.equal(got, matmul_i8(a, sa, b, sb, bias, dtype=dtype))       # the same bits again
 
 
+# sizes that each tile takes, from 128 x 128 on, ending inside one, K inside a slice: within a
+# stage's first fill and long enough for the loop that checks no load
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("M,N,K", [(1999, 2047, 2050), (700, 3001, 260), (700, 3001, 1300), (700, 6001, 129), (700, 6001, 1025), (1500, 6001, 17),
+                                   (1500, 6001, 1300), (2500, 5001, 100), (2500, 5001, 777), (2500, 5001, 900)])
+def test_matmul_i8_in_large_tiles(M, N, K, dtype):
+    g = gen(M + 3 * N + 7 * K)
+    a, b = codes(g, M, K), codes(g, N, K)
+    sa, sb = torch.rand(M, generator=g, device="cuda") + 0.01, torch.rand(N, generator=g, device="cuda") * 0.1
+    out = torch.full((M + 2, N + 8), 3.0, dtype=dtype, device="cuda")
+    check_matmul(a, sa, b, sb, randn(g, N) * 50, dtype, out=out[1:-1, 3:N + 3])
+    out[1:-1, 3:N + 3] = 3.0
+    assert (out == 3.0).all()                                                  # nothing around it is touched
+
+
 def test_matmul_i8_a_row_does_not_depend_on_the_others():
     """The sums are exact, so a token's outputs are the same bits however many there are."""
     from paper_2511_22009_amd import matmul_i8
