@@ -7,13 +7,12 @@
 // lanes hold a head, and its sum of squares is a butterfly over them.
 //
 // Bandwidth bounds it: the 8 x 30 x 52 tokens of a clip with 16 heads of 128 dims (102 MB) take
-// 21 us, 4.8 TB/s; q and k of 16384 tokens with 32 heads of 64 dims (134 MB, adjacent pairs) 30
-// us, as halves 33. With 72 dims a head fills 9 of its 16 lanes, and halves move in pieces of 8
-// bytes: 42 us for 151 MB. Groups of 9 lanes, their sums in thirds through the LDS crossbar, take
-// 41, but 43 instead of 40 where q and k lie packed; pieces of 16 bytes, eight pairs to a lane, the
-// same 34 for 128 dims and 4.5 instead of 3.6 for a single token. (12 pairs to a lane, which fill 3
-// lanes of 4, take 46 us: lanes 48 bytes apart; angles per wavefront instead of per workgroup 44;
-// wavefronts by tokens instead of by heads 41 to 42, and 25 instead of 22 for the clip.)
+// 16 us, 6.3 TB/s; q and k of 16384 tokens with 32 heads of 64 dims (134 MB, adjacent pairs) 23
+// us, 5.8, as halves 29. With 72 dims a head fills 9 of its 16 lanes, and halves move in pieces of
+// 8 bytes: 30 us for 151 MB, 5.0 TB/s; heads of 72 dims next to each other 47. (Groups of 9 lanes,
+// their sums in thirds through the LDS crossbar, made 4 % there and cost 5 where q and k lie
+// packed; pieces of 16 bytes, eight pairs to a lane, nothing for 128 dims and 4.5 instead of 3.6 us
+// for a single token; 12 pairs to a lane, wavefronts by tokens and angles per wavefront lost 3 to 10 %.)
 #include <cmath>
 
 #include "sf_ops_device.h"
@@ -64,6 +63,17 @@ struct Run {
     else
       return __uint_as_float(w[e]);
   }
+  template <bool PAST>
+  __device__ static __forceinline__ void put(void* p, V4 v) {
+    if constexpr (PAST) __builtin_nontemporal_store(v, (V4*)p);
+    else *(V4*)p = v;
+  }
+  template <bool PAST>
+  __device__ static __forceinline__ void put(void* p, V2 v) {
+    if constexpr (PAST) __builtin_nontemporal_store(v, (V2*)p);
+    else *(V2*)p = v;
+  }
+  template <bool PAST>
   __device__ static __forceinline__ void store(T* p, const float (&f)[N]) {
     uint32_t o[WORDS];
 #pragma unroll
@@ -74,8 +84,8 @@ struct Run {
         o[i] = __float_as_uint(f[i]);
     }
 #pragma unroll
-    for (int i = 0; i + 4 <= WORDS; i += 4) *(V4*)((char*)p + 4 * i) = V4{o[i], o[i + 1], o[i + 2], o[i + 3]};
-    if constexpr (WORDS % 4 == 2) *(V2*)((char*)p + 4 * (WORDS - 2)) = V2{o[WORDS - 2], o[WORDS - 1]};
+    for (int i = 0; i + 4 <= WORDS; i += 4) put<PAST>((char*)p + 4 * i, V4{o[i], o[i + 1], o[i + 2], o[i + 3]});
+    if constexpr (WORDS % 4 == 2) put<PAST>((char*)p + 4 * (WORDS - 2), V2{o[WORDS - 2], o[WORDS - 1]});
   }
 };
 template <typename T>
@@ -83,6 +93,7 @@ struct Run<T, 1> {
   T v;
   __device__ __forceinline__ void load(const T* p) { v = *p; }
   __device__ __forceinline__ float at(int) const { return to_f32(v); }
+  template <bool PAST>
   __device__ static __forceinline__ void store(T* p, const float (&f)[1]) { *p = from_f32<T>(f[0]); }
 };
 
@@ -97,9 +108,10 @@ struct Pairs {
   }
   __device__ __forceinline__ float x(int e) const { return lo.at(e); }
   __device__ __forceinline__ float y(int e) const { return hi.at(e); }
+  template <bool PAST>
   __device__ static __forceinline__ void store(T* p, int l, int h, const float (&x)[E], const float (&y)[E]) {
-    Run<T, E>::store(p + l, x);
-    Run<T, E>::store(p + h, y);
+    Run<T, E>::template store<PAST>(p + l, x);
+    Run<T, E>::template store<PAST>(p + h, y);
   }
 };
 template <typename T, int E>
@@ -108,11 +120,12 @@ struct Pairs<T, E, true> {
   __device__ __forceinline__ void load(const T* p, int l, int) { run.load(p + l); }
   __device__ __forceinline__ float x(int e) const { return run.at(2 * e); }
   __device__ __forceinline__ float y(int e) const { return run.at(2 * e + 1); }
+  template <bool PAST>
   __device__ static __forceinline__ void store(T* p, int l, int, const float (&x)[E], const float (&y)[E]) {
     float f[2 * E];
 #pragma unroll
     for (int e = 0; e < E; ++e) f[2 * e] = x[e], f[2 * e + 1] = y[e];
-    Run<T, 2 * E>::store(p + l, f);
+    Run<T, 2 * E>::template store<PAST>(p + l, f);
   }
 };
 
@@ -121,7 +134,7 @@ struct Pairs<T, E, true> {
 // takes a run of heads of q or of k.
 // E pairs per unit, U units per lane: one unit of four pairs whose elements are adjacent in
 // memory, or two of one pair each. ADJ: the layout of adjacent pairs. PART: some dims stay as they are.
-template <typename T, int E, int U, bool ADJ, bool NORM, bool ROT, bool PART>
+template <typename T, int E, int U, bool ADJ, bool NORM, bool ROT, bool PART, bool PAST>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   constexpr int HB = 2;  // heads whose loads are in flight together
   __shared__ __attribute__((aligned(16))) float2 angles[ROT ? 64 * E * U : 1];  // [token][pair]
@@ -277,29 +290,34 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
             q[e] = ye * yy[u][e];
           }
         }
-        if (here && on[u]) Pairs<T, E, ADJ>::store(o, lo[u], hi[u], p, q);
+        if (here && on[u]) Pairs<T, E, ADJ>::template store<PAST>(o, lo[u], hi[u], p, q);
       }
     }
   }
 }
 
 template <typename T, bool NORM, bool ROT, bool PART>
-static hipError_t launch_rope_as(const RopeArgs& a, bool whole, dim3 grid, hipStream_t s) {
+static hipError_t launch_rope_as(const RopeArgs& a, bool whole, bool past, dim3 grid, hipStream_t s) {
+  const bool adjacent = !ROT || a.layout == SF_ROPE_ADJACENT;
   if (!whole)
-    launch(rope_kernel<T, 1, 2, false, NORM, ROT, PART>, grid, dim3(256), 0, s, a);
-  else if (!ROT || a.layout == SF_ROPE_ADJACENT)
-    launch(rope_kernel<T, 4, 1, true, NORM, ROT, PART>, grid, dim3(256), 0, s, a);
+    launch(rope_kernel<T, 1, 2, false, NORM, ROT, PART, false>, grid, dim3(256), 0, s, a);
+  else if (adjacent && past)
+    launch(rope_kernel<T, 4, 1, true, NORM, ROT, PART, true>, grid, dim3(256), 0, s, a);
+  else if (adjacent)
+    launch(rope_kernel<T, 4, 1, true, NORM, ROT, PART, false>, grid, dim3(256), 0, s, a);
+  else if (past)
+    launch(rope_kernel<T, 4, 1, false, NORM, ROT, PART, true>, grid, dim3(256), 0, s, a);
   else
-    launch(rope_kernel<T, 4, 1, false, NORM, ROT, PART>, grid, dim3(256), 0, s, a);
+    launch(rope_kernel<T, 4, 1, false, NORM, ROT, PART, false>, grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 template <typename T>
-static hipError_t launch_rope_type(const RopeArgs& a, bool norm, bool rotate, bool whole, dim3 grid, hipStream_t s) {
+static hipError_t launch_rope_type(const RopeArgs& a, bool norm, bool rotate, bool whole, bool past, dim3 grid, hipStream_t s) {
   const bool part = 2 * a.pairs < a.dh;
-  if (!rotate) return launch_rope_as<T, true, false, false>(a, whole, grid, s);
-  if (norm) return part ? launch_rope_as<T, true, true, true>(a, whole, grid, s) : launch_rope_as<T, true, true, false>(a, whole, grid, s);
-  return part ? launch_rope_as<T, false, true, true>(a, whole, grid, s) : launch_rope_as<T, false, true, false>(a, whole, grid, s);
+  if (!rotate) return launch_rope_as<T, true, false, false>(a, whole, past, grid, s);
+  if (norm) return part ? launch_rope_as<T, true, true, true>(a, whole, past, grid, s) : launch_rope_as<T, true, true, false>(a, whole, past, grid, s);
+  return part ? launch_rope_as<T, false, true, true>(a, whole, past, grid, s) : launch_rope_as<T, false, true, false>(a, whole, past, grid, s);
 }
 
 // norm without rotation, rotation without norm, or both.
@@ -335,7 +353,17 @@ hipError_t launch_rope(bool is_bf16, bool norm, bool rotate, RopeArgs a, hipStre
   a.step[0] = a.chunks0 > 0 ? (a.heads0 + a.chunks0 - 1) / a.chunks0 : 1;
   a.step[1] = chunks > a.chunks0 ? (heads1 + chunks - a.chunks0 - 1) / (chunks - a.chunks0) : 1;
   const dim3 grid((uint32_t)groups, (uint32_t)splits);
-  return is_bf16 ? launch_rope_type<bf16>(a, norm, rotate, whole, grid, s) : launch_rope_type<float>(a, norm, rotate, whole, grid, s);
+  // Outputs past the L2 where a head's tokens follow each other, or its dims are whole pieces of 64
+  // bytes: q and k of 16384 tokens with 16 heads of 72 dims 30.5 instead of 42.7 us, a clip's 16.2
+  // instead of 21; in heads of 72 dims next to each other, whose ends share pieces, 52 instead of 47.
+  const int64_t size = is_bf16 ? 2 : 4;
+  bool past = true;
+  for (int i = 0; i < 2; ++i) {
+    const RopeHeads& t = a.t[i];
+    if (i ? heads1 == 0 : a.heads0 == 0) continue;
+    past = past && (t.out_tok == a.dh || ((int64_t)(uintptr_t)t.out | size * (a.dh | t.out_tok | t.out_head | t.out_row)) % 64 == 0);
+  }
+  return is_bf16 ? launch_rope_type<bf16>(a, norm, rotate, whole, past, grid, s) : launch_rope_type<float>(a, norm, rotate, whole, past, grid, s);
 }
 
 }  // namespace sf
