@@ -578,6 +578,30 @@ def test_rope_of_overlapping_windows(layout, dims):
             assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("layout", ["adjacent", "halves"])
+@pytest.mark.parametrize("dh", [24, 64, 72, 128])
+def test_rope_outputs_apart_next_to_each_other_and_off_alignment(dh, layout, dtype):
+    """Heads whose tokens follow each other, heads next to each other, at addresses of every kind:
+    the same bits, and nothing around the outputs is touched."""
+    from paper_2511_22009_amd import Rotary, qk_norm_rotate, rotate
+    g = gen(55 + dh)
+    R, T, H = 2, 45, 5
+    r, pos = Rotary([dh // 4 // 2 * 2, dh // 2], layout=layout), positions(g, R, T, 2, 500.0)
+    x, gain = randn(g, R, T, H, dh, dtype=dtype), 1 + 0.2 * randn(g, dh)
+    want, (normed, _) = rotate(x, pos, r), qk_norm_rotate(x, None, gain, None, pos, r)
+    for strides in ((H * T * dh, dh, T * dh), (T * H * dh, H * dh, dh), (T * (H * dh + 3), H * dh + 3, dh)):
+        for off in (0, 1, 32):
+            room = torch.full((R * T * (H * dh + 3) + 100,), 7.0, dtype=dtype, device="cuda")
+            out = room.as_strided((R, T, H, dh), (*strides, 1), off)
+            assert torch.equal(rotate(x, pos, r, out=out), want)
+            out.fill_(7.0)
+            assert (room == 7.0).all()
+            out.copy_(x)
+            qk_norm_rotate(out, None, gain, None, pos, r, out=(out, None))
+            assert torch.equal(out, normed)
+
+
 # a launch takes 2^23 rows, so these are several
 LONG = 2 ** 23
 
