@@ -9,10 +9,11 @@
 // Bandwidth bounds it: the 8 x 30 x 52 tokens of a clip with 16 heads of 128 dims (102 MB) take
 // 16 us, 6.3 TB/s; q and k of 16384 tokens with 32 heads of 64 dims (134 MB, adjacent pairs) 23
 // us, 5.8, as halves 29. With 72 dims a head fills 9 of its 16 lanes, and halves move in pieces of
-// 8 bytes: 30 us for 151 MB, 5.0 TB/s; heads of 72 dims next to each other 47. (Groups of 9 lanes,
+// 8 bytes: 30 us for 151 MB, 5.0 TB/s; heads of 72 dims next to each other 42. (Groups of 9 lanes,
 // their sums in thirds through the LDS crossbar, made 4 % there and cost 5 where q and k lie
 // packed; pieces of 16 bytes, eight pairs to a lane, nothing for 128 dims and 4.5 instead of 3.6 us
-// for a single token; 12 pairs to a lane, wavefronts by tokens and angles per wavefront lost 3 to 10 %.)
+// for a single token; 12 pairs to a lane, wavefronts by tokens throughout and angles per wavefront
+// lost 3 to 10 %.)
 #include <cmath>
 
 #include "sf_ops_device.h"
@@ -134,22 +135,28 @@ struct Pairs<T, E, true> {
 // takes a run of heads of q or of k.
 // E pairs per unit, U units per lane: one unit of four pairs whose elements are adjacent in
 // memory, or two of one pair each. ADJ: the layout of adjacent pairs. PART: some dims stay as they are.
-template <typename T, int E, int U, bool ADJ, bool NORM, bool ROT, bool PART, bool PAST>
+// Where a lane's heads lie and how outputs leave (the choice is at launch_rope): a wavefront takes a
+// head of several tokens, through the L2 or past it, or several heads of one token, past it.
+enum RopeOut { ROPE_PLAIN, ROPE_PAST, ROPE_BY_HEADS };
+template <typename T, int E, int U, bool ADJ, bool NORM, bool ROT, bool PART, RopeOut OUT>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
-  constexpr int HB = 2;  // heads whose loads are in flight together
-  __shared__ __attribute__((aligned(16))) float2 angles[ROT ? 64 * E * U : 1];  // [token][pair]
+  constexpr int HB = 2;  // heads (of each lane) whose loads are in flight together
+  constexpr bool kByHeads = OUT == ROPE_BY_HEADS;
+  __shared__ __attribute__((aligned(16))) float2 angles[ROT ? (kByHeads ? 512 : 64 * E * U) : 1];  // [token][pair]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = 1 << a.group_log2, li = lane & (G - 1);
   const uint32_t total = (uint32_t)a.rows * (uint32_t)a.tokens;
   // each of the eight XCDs (workgroup b goes to XCD b % 8) takes a contiguous range of tokens:
   // a cache line that two workgroups' tokens share is read and written in one L2
   const uint32_t xcd = blockIdx.x % 8, base = gridDim.x / 8, rem = gridDim.x % 8;
-  const uint32_t first = (xcd * base + min(xcd, rem) + blockIdx.x / 8) * (uint32_t)(64 >> a.group_log2);
-  const int slot = lane >> a.group_log2;
+  const int slots = 64 >> a.group_log2, in_slot = lane >> a.group_log2;
+  const uint32_t first = (xcd * base + min(xcd, rem) + blockIdx.x / 8) * (uint32_t)(kByHeads ? 4 : slots);
+  // a lane's token of the workgroup's, the heads a wavefront takes at once, and the lane's of them
+  const int slot = kByHeads ? wave : in_slot, abreast = kByHeads ? slots : 1, mine = kByHeads ? in_slot : 0;
   const bool here = first + slot < total;
   const uint32_t tt = here ? first + slot : total - 1;
   const uint32_t row = fdiv(tt, a.div_tok), tok = tt - row * (uint32_t)a.tokens;
-  const int chunk = (int)blockIdx.y * 4 + wave;
+  const int chunk = kByHeads ? (int)blockIdx.y : (int)blockIdx.y * 4 + wave;
   const int which = chunk >= a.chunks0;
   const RopeHeads& t = a.t[which];
   const int heads = which ? a.heads - a.heads0 : a.heads0, step = a.step[which];
@@ -185,12 +192,12 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 #pragma unroll
     for (int b = 0; b < HB; ++b)
 #pragma unroll
-      for (int u = 0; u < U; ++u) raw[b][u].load(in + (int64_t)min(h + b, h1 - 1) * t.in_head, lo[u], hi[u]);
+      for (int u = 0; u < U; ++u) raw[b][u].load(in + (int64_t)min(h + b * abreast + mine, h1 - 1) * t.in_head, lo[u], hi[u]);
   };
   if (h0 < h1) load(h0);
 
   if constexpr (ROT) {
-    const int here_pairs = (int)min((uint32_t)(64 >> a.group_log2), total - first) * a.pairs;
+    const int here_pairs = (int)min((uint32_t)(kByHeads ? 4 : slots), total - first) * a.pairs;
     for (int c = (int)threadIdx.x; c < here_pairs; c += 256) {
       const int at = (int)fdiv((uint32_t)c, a.div_pairs), j = c - at * a.pairs;
       const uint32_t r = fdiv(first + at, a.div_tok), k = first + at - r * (uint32_t)a.tokens;
@@ -231,7 +238,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
       }
     }
   const float inv_dh = 1.0f / (float)a.dh;
-  for (int hb = h0; hb < h1; hb += HB) {
+  for (int hb = h0; hb < h1; hb += HB * abreast) {
     float x[HB][U][E], y[HB][U][E];
 #pragma unroll
     for (int b = 0; b < HB; ++b)
@@ -240,7 +247,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 #pragma unroll
         for (int e = 0; e < E; ++e) x[b][u][e] = raw[b][u].x(e), y[b][u][e] = raw[b][u].y(e);
       }
-    if (hb + HB < h1) load(hb + HB);
+    if (hb + HB * abreast < h1) load(hb + HB * abreast);
     float r[HB];
     if constexpr (NORM) {
 #pragma unroll
@@ -270,8 +277,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     }
 #pragma unroll
     for (int b = 0; b < HB; ++b) {
-      const int h = hb + b;
-      if (h >= h1) break;
+      const int h = hb + b * abreast + mine;
+      if (hb + b * abreast >= h1) break;
       T* const o = out + (int64_t)h * t.out_head;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -290,34 +297,38 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
             q[e] = ye * yy[u][e];
           }
         }
-        if (here && on[u]) Pairs<T, E, ADJ>::template store<PAST>(o, lo[u], hi[u], p, q);
+        if (here && on[u] && h < h1) Pairs<T, E, ADJ>::template store<OUT != ROPE_PLAIN>(o, lo[u], hi[u], p, q);
       }
     }
   }
 }
 
 template <typename T, bool NORM, bool ROT, bool PART>
-static hipError_t launch_rope_as(const RopeArgs& a, bool whole, bool past, dim3 grid, hipStream_t s) {
-  const bool adjacent = !ROT || a.layout == SF_ROPE_ADJACENT;
+static hipError_t launch_rope_as(const RopeArgs& a, bool whole, RopeOut out, dim3 grid, hipStream_t s) {
+  const auto go = [&](auto out) {
+    constexpr RopeOut O = decltype(out)::value;
+    if (!ROT || a.layout == SF_ROPE_ADJACENT)
+      launch(rope_kernel<T, 4, 1, true, NORM, ROT, PART, O>, grid, dim3(256), 0, s, a);
+    else
+      launch(rope_kernel<T, 4, 1, false, NORM, ROT, PART, O>, grid, dim3(256), 0, s, a);
+  };
   if (!whole)
-    launch(rope_kernel<T, 1, 2, false, NORM, ROT, PART, false>, grid, dim3(256), 0, s, a);
-  else if (adjacent && past)
-    launch(rope_kernel<T, 4, 1, true, NORM, ROT, PART, true>, grid, dim3(256), 0, s, a);
-  else if (adjacent)
-    launch(rope_kernel<T, 4, 1, true, NORM, ROT, PART, false>, grid, dim3(256), 0, s, a);
-  else if (past)
-    launch(rope_kernel<T, 4, 1, false, NORM, ROT, PART, true>, grid, dim3(256), 0, s, a);
+    launch(rope_kernel<T, 1, 2, false, NORM, ROT, PART, ROPE_PLAIN>, grid, dim3(256), 0, s, a);
+  else if (out == ROPE_BY_HEADS)
+    go(std::integral_constant<RopeOut, ROPE_BY_HEADS>{});
+  else if (out == ROPE_PAST)
+    go(std::integral_constant<RopeOut, ROPE_PAST>{});
   else
-    launch(rope_kernel<T, 4, 1, false, NORM, ROT, PART, false>, grid, dim3(256), 0, s, a);
+    go(std::integral_constant<RopeOut, ROPE_PLAIN>{});
   return hipGetLastError();
 }
 
 template <typename T>
-static hipError_t launch_rope_type(const RopeArgs& a, bool norm, bool rotate, bool whole, bool past, dim3 grid, hipStream_t s) {
+static hipError_t launch_rope_type(const RopeArgs& a, bool norm, bool rotate, bool whole, RopeOut out, dim3 grid, hipStream_t s) {
   const bool part = 2 * a.pairs < a.dh;
-  if (!rotate) return launch_rope_as<T, true, false, false>(a, whole, past, grid, s);
-  if (norm) return part ? launch_rope_as<T, true, true, true>(a, whole, past, grid, s) : launch_rope_as<T, true, true, false>(a, whole, past, grid, s);
-  return part ? launch_rope_as<T, false, true, true>(a, whole, past, grid, s) : launch_rope_as<T, false, true, false>(a, whole, past, grid, s);
+  if (!rotate) return launch_rope_as<T, true, false, false>(a, whole, out, grid, s);
+  if (norm) return part ? launch_rope_as<T, true, true, true>(a, whole, out, grid, s) : launch_rope_as<T, true, true, false>(a, whole, out, grid, s);
+  return part ? launch_rope_as<T, false, true, true>(a, whole, out, grid, s) : launch_rope_as<T, false, true, false>(a, whole, out, grid, s);
 }
 
 // norm without rotation, rotation without norm, or both.
@@ -340,30 +351,41 @@ hipError_t launch_rope(bool is_bf16, bool norm, bool rotate, RopeArgs a, hipStre
     a.rate[i] = n > 0 ? a.log2_theta / n : 0.0;
   }
   a.div_pairs = make_fastdiv(a.pairs > 0 ? a.pairs : 1);
-  const int64_t groups = ((int64_t)a.rows * a.tokens + (64 >> a.group_log2) - 1) >> (6 - a.group_log2);
+  const int heads1 = a.heads - a.heads0, slots = 64 >> a.group_log2;
+  // Outputs past the L2 where a head's tokens follow each other, or its dims are whole pieces of 64
+  // bytes: q and k of 16384 tokens with 16 heads of 72 dims 30.5 instead of 42.7 us, a clip's 16.2
+  // instead of 21. Where a token's heads follow each other instead, and only several of them are whole
+  // pieces, a wavefront takes several heads of one token, past the L2 too: q and k of 16384 tokens in
+  // packed rows with 16 heads of 72 dims 42 instead of 47 us, with 28 heads of 40 dims 38 instead of 55
+  // (a head of several tokens past the L2, its ends sharing pieces: 52 at 72 dims).
+  const int64_t size = is_bf16 ? 2 : 4;
+  bool past = true, runs = whole && size * a.dh * slots % 64 == 0;
+  for (int i = 0; i < 2; ++i) {
+    const RopeHeads& t = a.t[i];
+    if (i ? heads1 == 0 : a.heads0 == 0) continue;
+    const int64_t at = (int64_t)(uintptr_t)t.out | size * (t.out_tok | t.out_row);
+    past = past && (t.out_tok == a.dh || (at | size * (a.dh | t.out_head)) % 64 == 0);
+    runs = runs && t.out_head == a.dh && at % 64 == 0;
+  }
+  const RopeOut out = past ? ROPE_PAST : runs ? ROPE_BY_HEADS : ROPE_PLAIN;
+  const bool by_heads = out == ROPE_BY_HEADS;
+  const int per = by_heads ? 4 : slots, abreast = by_heads ? slots : 1, waves = by_heads ? 1 : 4;
+  const int64_t groups = ((int64_t)a.rows * a.tokens + per - 1) / per;
   // heads are split over workgroups too while there are fewer than that of them
   int64_t splits = (1024 + groups - 1) / groups;
   const int most = (a.heads + 3) / 4;
   if (splits > most) splits = most;
+  if (by_heads && a.heads0 > 0 && heads1 > 0 && splits < 2) splits = 2;
   // q and k share the runs of heads
-  const int heads1 = a.heads - a.heads0, chunks = (int)splits * 4;
+  const int chunks = (int)splits * waves;
   a.chunks0 = (int)(((int64_t)chunks * a.heads0 + a.heads / 2) / a.heads);
   if (heads1 > 0 && a.chunks0 == chunks) --a.chunks0;
   if (a.heads0 > 0 && a.chunks0 == 0) a.chunks0 = 1;
-  a.step[0] = a.chunks0 > 0 ? (a.heads0 + a.chunks0 - 1) / a.chunks0 : 1;
-  a.step[1] = chunks > a.chunks0 ? (heads1 + chunks - a.chunks0 - 1) / (chunks - a.chunks0) : 1;
+  const auto run = [&](int heads, int n) { return n > 0 ? ((heads + n - 1) / n + abreast - 1) / abreast * abreast : 1; };
+  a.step[0] = run(a.heads0, a.chunks0);
+  a.step[1] = run(heads1, chunks - a.chunks0);
   const dim3 grid((uint32_t)groups, (uint32_t)splits);
-  // Outputs past the L2 where a head's tokens follow each other, or its dims are whole pieces of 64
-  // bytes: q and k of 16384 tokens with 16 heads of 72 dims 30.5 instead of 42.7 us, a clip's 16.2
-  // instead of 21; in heads of 72 dims next to each other, whose ends share pieces, 52 instead of 47.
-  const int64_t size = is_bf16 ? 2 : 4;
-  bool past = true;
-  for (int i = 0; i < 2; ++i) {
-    const RopeHeads& t = a.t[i];
-    if (i ? heads1 == 0 : a.heads0 == 0) continue;
-    past = past && (t.out_tok == a.dh || ((int64_t)(uintptr_t)t.out | size * (a.dh | t.out_tok | t.out_head | t.out_row)) % 64 == 0);
-  }
-  return is_bf16 ? launch_rope_type<bf16>(a, norm, rotate, whole, past, grid, s) : launch_rope_type<float>(a, norm, rotate, whole, past, grid, s);
+  return is_bf16 ? launch_rope_type<bf16>(a, norm, rotate, whole, out, grid, s) : launch_rope_type<float>(a, norm, rotate, whole, out, grid, s);
 }
 
 }  // namespace sf

@@ -602,6 +602,23 @@ def test_rope_outputs_apart_next_to_each_other_and_off_alignment(dh, layout, dty
             assert torch.equal(out, normed)
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("dh", [8, 24, 40, 72])
+def test_rope_heads_next_to_each_other_and_apart_are_the_same_bits(dh, dtype):
+    """Whichever way a wavefront takes them, with heads and tokens that do not fill the last one."""
+    from paper_2511_22009_amd import Rotary, qk_norm_rotate, rotate
+    g = gen(56 + dh)
+    for R, T, Hq, Hk, layout in ((1, 1, 4, 4, "halves"), (3, 45, 12, 4, "adjacent"), (1, 7, 20, 28, "halves"), (2, 300, 16, 16, "axis_halves")):
+        r, pos = Rotary([dh // 8 * 4, dh // 8 * 4], layout=layout), positions(g, R, T, 2, 500.0)
+        q, k, gain = randn(g, R, T, Hq, dh, dtype=dtype), randn(g, R, T, Hk, dh, dtype=dtype), 1 + 0.2 * randn(g, dh)
+        apart = [t.transpose(1, 2).contiguous().transpose(1, 2) for t in (q, k)]
+        assert torch.equal(rotate(q, pos, r), rotate(apart[0], pos, r))
+        for got, want in zip(qk_norm_rotate(q, k, gain, None, pos, r), qk_norm_rotate(*apart, gain, None, pos, r)):
+            assert torch.equal(got, want)
+        for got, want in zip(qk_norm_rotate(q, k, gain, gain), qk_norm_rotate(*apart, gain, gain)):
+            assert torch.equal(got, want)
+
+
 # a launch takes 2^23 rows, so these are several
 LONG = 2 ** 23
 
