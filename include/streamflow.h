@@ -430,7 +430,7 @@ int sf_set_qk(sf_model* m, const sf_qk* p);
  * sf_matmul_i8 with the epilogues of the bf16 projections. Everything else, the
  * cross-attention's projections included, stays as it is. It pays in wide blocks: a velocity of
  * four 1024^2 rows of width 1152 takes 1.65 ms instead of 1.85 (two blocks), of four 512^2 rows of
- * that width 0.77 instead of 0.85 (four blocks), of width 768 1.39 instead of 1.32 (twelve): there
+ * that width 0.77 instead of 0.85 (four blocks), of width 768 1.37 instead of 1.33 (twelve): there
  * the passes that make codes cost more than the products save. */
 
 /* Enable (nonzero) or disable (0, the default) 8-bit projections in sf_velocity,

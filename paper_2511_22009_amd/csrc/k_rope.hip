@@ -307,10 +307,10 @@ template <typename T, bool NORM, bool ROT, bool PART>
 static hipError_t launch_rope_as(const RopeArgs& a, bool whole, RopeOut out, dim3 grid, hipStream_t s) {
   const auto go = [&](auto out) {
     constexpr RopeOut O = decltype(out)::value;
-    if (!ROT || a.layout == SF_ROPE_ADJACENT)
-      launch(rope_kernel<T, 4, 1, true, NORM, ROT, PART, O>, grid, dim3(256), 0, s, a);
-    else
-      launch(rope_kernel<T, 4, 1, false, NORM, ROT, PART, O>, grid, dim3(256), 0, s, a);
+    if constexpr (ROT) {
+      if (a.layout != SF_ROPE_ADJACENT) return launch(rope_kernel<T, 4, 1, false, NORM, ROT, PART, O>, grid, dim3(256), 0, s, a);
+    }
+    launch(rope_kernel<T, 4, 1, true, NORM, ROT, PART, O>, grid, dim3(256), 0, s, a);
   };
   if (!whole)
     launch(rope_kernel<T, 1, 2, false, NORM, ROT, PART, ROPE_PLAIN>, grid, dim3(256), 0, s, a);
