@@ -130,14 +130,16 @@ struct Pairs<T, E, true> {
   }
 };
 
-// A workgroup of four wavefronts takes 64 / G tokens; its first threads form a pair's angle of a
-// token each and leave cosine and sine in LDS, under the wavefronts' first loads. A wavefront
-// takes a run of heads of q or of k.
-// E pairs per unit, U units per lane: one unit of four pairs whose elements are adjacent in
-// memory, or two of one pair each (an element at a time: 98 dims 2.4 to 3.1 TB/s, 36 dims 2.3). ADJ: the layout of adjacent pairs. PART: some dims stay as they are.
 // Where a lane's heads lie and how outputs leave (the choice is at launch_rope): a wavefront takes a
 // head of several tokens, through the L2 or past it, or several heads of one token, past it.
 enum RopeOut { ROPE_PLAIN, ROPE_PAST, ROPE_BY_HEADS };
+
+// A workgroup of four wavefronts takes 64 / G tokens (by heads: four); its first threads form a
+// pair's angle of a token each and leave cosine and sine in LDS, under the wavefronts' first loads.
+// A wavefront takes a run of heads of q or of k.
+// E pairs per unit, U units per lane: one unit of four pairs whose elements are adjacent in
+// memory, or two of one pair each (an element at a time: 98 dims 2.4 to 3.1 TB/s, 36 dims 2.3).
+// ADJ: the layout of adjacent pairs. PART: some dims stay as they are.
 template <typename T, int E, int U, bool ADJ, bool NORM, bool ROT, bool PART, RopeOut OUT>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   constexpr int HB = 2;  // heads (of each lane) whose loads are in flight together

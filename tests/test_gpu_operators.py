@@ -548,6 +548,23 @@ def test_operators_on_another_stream_and_in_a_graph():
         assert all(torch.equal(a, b) for a, b in zip(out, eager))
 
 
+def test_operators_on_two_streams_at_once():
+    """Calls under way on two streams share nothing: the bits of calls alone."""
+    both = [chain_inputs(seed) for seed in (36, 37)]
+    want = [[t.clone() for t in chain(*args)] for args in both]
+    streams = [torch.cuda.Stream() for _ in both]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            got[i].append(chain(*both[i], stream=s))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for out in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(out, want[i]))
+
+
 def test_operators_one_after_the_other():
     """Tokens to codes, their product with weights, norm and rotation of its queries and keys,
     against the same in 64 bits from the codes. The product is rounded to bf16 before the norm
