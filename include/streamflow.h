@@ -394,8 +394,10 @@ int sf_rotate(const sf_heads* x, int type, int rows, int tokens, int dh, const s
 /* The norm of queries and keys for each head, and their rotation, in one pass:
  *   y = x / sqrt(mean_d x^2 + eps) * gain[d], then y turned as by sf_rotate.
  * k may be NULL (q alone), and may have other strides and fewer heads than q. q_gain, k_gain:
- * fp32 [dh] or NULL (1). rope NULL: the norm alone (pos is not read). eps >= 0. Statistics
- * and products in fp32, one rounding to the element type. Otherwise as sf_rotate. */
+ * fp32 [dh] or NULL (1). rope NULL: the norm alone (pos is not read). eps >= 0, also one below
+ * fp32's normal numbers. Statistics and products in fp32, one rounding to the element type; a head
+ * whose squares fp32 does not hold is scaled by a power of two first, so finite heads of every size
+ * are normalised. Otherwise as sf_rotate. */
 int sf_qk_norm_rotate(const sf_heads* q, const sf_heads* k, const float* q_gain, const float* k_gain, float eps, int type,
                       int rows, int tokens, int dh, const sf_rope* rope, const float* pos, long long pos_row,
                       void* hip_stream);

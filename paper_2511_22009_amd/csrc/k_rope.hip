@@ -140,12 +140,13 @@ enum RopeOut { ROPE_PLAIN, ROPE_PAST, ROPE_BY_HEADS };
 // E pairs per unit, U units per lane: one unit of four pairs whose elements are adjacent in
 // memory, or two of one pair each (an element at a time: 98 dims 2.4 to 3.1 TB/s, 36 dims 2.3).
 // ADJ: the layout of adjacent pairs. PART: some dims stay as they are.
-template <typename T, int E, int U, bool ADJ, bool NORM, bool ROT, bool PART, RopeOut OUT>
-__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+// One pass over a workgroup's heads; FAR: over those alone that the first pass leaves, whose squares fp32
+// does not hold. Returns whether it left a head of the lane's.
+template <typename T, int E, int U, bool ADJ, bool NORM, bool ROT, bool PART, RopeOut OUT, bool FAR>
+__device__ __forceinline__ bool rope_pass(const RopeArgs& a, int tid, float2* angles) {
   constexpr int HB = 2;  // heads (of each lane) whose loads are in flight together
   constexpr bool kByHeads = OUT == ROPE_BY_HEADS;
-  __shared__ __attribute__((aligned(16))) float2 angles[ROT ? (kByHeads ? 512 : 64 * E * U) : 1];  // [token][pair]
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int G = 1 << a.group_log2, li = lane & (G - 1);
   const uint32_t total = (uint32_t)a.rows * (uint32_t)a.tokens;
   // each of the eight XCDs (workgroup b goes to XCD b % 8) takes a contiguous range of tokens:
@@ -198,9 +199,9 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   };
   if (h0 < h1) load(h0);
 
-  if constexpr (ROT) {
+  if constexpr (ROT && !FAR) {
     const int here_pairs = (int)min((uint32_t)(kByHeads ? 4 : slots), total - first) * a.pairs;
-    for (int c = (int)threadIdx.x; c < here_pairs; c += 256) {
+    for (int c = tid; c < here_pairs; c += 256) {
       const int at = (int)fdiv((uint32_t)c, a.div_pairs), j = c - at * a.pairs;
       const uint32_t r = fdiv(first + at, a.div_tok), k = first + at - r * (uint32_t)a.tokens;
       int ax = 0, s0 = a.first[0];
@@ -215,7 +216,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     }
     __syncthreads();
   }
-  if (h0 >= h1) return;
+  if (h0 >= h1) return false;
 
   // what takes a pair (x, y) to (x xx + y xy, x yx + y yy): the gains and the turn
   float xx[U][E], xy[U][E], yx[U][E], yy[U][E];
@@ -240,6 +241,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
       }
     }
   const float inv_dh = 1.0f / (float)a.dh;
+  bool left = false;
   for (int hb = h0; hb < h1; hb += HB * abreast) {
     float x[HB][U][E], y[HB][U][E];
 #pragma unroll
@@ -251,31 +253,66 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
       }
     if (hb + HB * abreast < h1) load(hb + HB * abreast);
     float r[HB];
+    bool put[HB];
     if constexpr (NORM) {
+      // reciprocal roots of the mean squares and eps of the batch's heads, times the square of s(b)
+      auto roots = [&](auto s) {
+#pragma unroll
+        for (int b = 0; b < HB; ++b) {
+          r[b] = 0.0f;
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            float mine = 0.0f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              const float xe = x[b][u][e] * s(b), ye = y[b][u][e] * s(b);
+              mine += __builtin_fmaf(xe, xe, ye * ye);
+            }
+            r[b] += on[u] ? mine : 0.0f;
+          }
+        }
+        // the sums of the batch's heads over their G lanes
+        auto add = [&](auto m) {
+#pragma unroll
+          for (int b = 0; b < HB; ++b) r[b] += lane_xor<decltype(m)::value>(r[b]);
+        };
+        if (G > 1) add(std::integral_constant<int, 1>{});
+        if (G > 2) add(std::integral_constant<int, 2>{});
+        if (G > 4) add(std::integral_constant<int, 4>{});
+        if (G > 8) add(std::integral_constant<int, 8>{});
+        if (G > 16) add(std::integral_constant<int, 16>{});
+        if (G > 32) add(std::integral_constant<int, 32>{});
+#pragma unroll
+        for (int b = 0; b < HB; ++b) r[b] = __builtin_amdgcn_rsqf(r[b] * inv_dh + a.eps * s(b) * s(b));  // within 1 ulp
+      };
+      roots([](int) { return 1.0f; });
 #pragma unroll
       for (int b = 0; b < HB; ++b) {
-        r[b] = 0.0f;
+        // no root: 0, of a sum that overflows, or infinity, of 0 and of subnormal numbers, which the
+        // instruction takes for 0
+        put[b] = __builtin_amdgcn_classf(r[b], 0x240) == FAR;
+        left = left || !put[b];
+      }
+      if constexpr (FAR) {
+        // Times a power of two, which rounds nothing. A sum that overflows has a mean of 2^120 and more:
+        // times 2^-70, that is a normal number, and every square is below 2^116. A mean below 2^-126
+        // has elements below 2^-59: times 2^100, every square is a normal number. (A mean that is
+        // one has lost at most 2^-150 to subnormal squares, half a step of itself.) Heads of zeros with
+        // eps 0 and heads that hold an infinity keep a root of infinity and 0: 0 / 0, inf / inf.
+        constexpr float kDown = 0x1p-70f, kUp = 0x1p100f;
+        const bool down[HB] = {r[0] == 0.0f, r[1] == 0.0f};
+        roots([&](int b) { return down[b] ? kDown : kUp; });
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          float mine = 0.0f;
+        for (int b = 0; b < HB; ++b) {
+          // x (s / root), as x s would lose bits of small elements; upwards (x s) / root, as s / root
+          // would overflow
+          r[b] *= down[b] ? kDown : 1.0f;
 #pragma unroll
-          for (int e = 0; e < E; ++e) mine += x[b][u][e] * x[b][u][e] + y[b][u][e] * y[b][u][e];
-          r[b] += on[u] ? mine : 0.0f;
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[b][u][e] *= down[b] ? 1.0f : kUp, y[b][u][e] *= down[b] ? 1.0f : kUp;
         }
       }
-      // the sums of the batch's heads over their G lanes
-      auto add = [&](auto m) {
-#pragma unroll
-        for (int b = 0; b < HB; ++b) r[b] += lane_xor<decltype(m)::value>(r[b]);
-      };
-      if (G > 1) add(std::integral_constant<int, 1>{});
-      if (G > 2) add(std::integral_constant<int, 2>{});
-      if (G > 4) add(std::integral_constant<int, 4>{});
-      if (G > 8) add(std::integral_constant<int, 8>{});
-      if (G > 16) add(std::integral_constant<int, 16>{});
-      if (G > 32) add(std::integral_constant<int, 32>{});
-#pragma unroll
-      for (int b = 0; b < HB; ++b) r[b] = __builtin_amdgcn_rsqf(r[b] * inv_dh + a.eps);  // within 1 ulp
     }
 #pragma unroll
     for (int b = 0; b < HB; ++b) {
@@ -292,16 +329,42 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
           if constexpr (ROT) {
             // a dim that stays is not touched by its neighbour, which may be infinite
             const float xt = PART && !turns[u] ? 0.0f : xe, yt = PART && !turns[u] ? 0.0f : ye;
-            p[e] = xe * xx[u][e] + yt * xy[u][e];
-            q[e] = xt * yx[u][e] + ye * yy[u][e];
+            // (which of the two products is not rounded is written out, so that no build changes a bit)
+            p[e] = __builtin_fmaf(xe, xx[u][e], yt * xy[u][e]);
+            q[e] = NORM && PART ? __builtin_fmaf(ye, yy[u][e], xt * yx[u][e]) : __builtin_fmaf(xt, yx[u][e], ye * yy[u][e]);
           } else {
             p[e] = xe * xx[u][e];
             q[e] = ye * yy[u][e];
           }
         }
-        if (here && on[u] && h < h1) Pairs<T, E, ADJ>::template store<OUT != ROPE_PLAIN>(o, lo[u], hi[u], p, q);
+        if (here && on[u] && h < h1 && (!NORM || put[b])) Pairs<T, E, ADJ>::template store<OUT != ROPE_PLAIN>(o, lo[u], hi[u], p, q);
       }
     }
+  }
+  return left;
+}
+
+template <typename T, int E, int U, bool ADJ, bool NORM, bool ROT, bool PART, RopeOut OUT>
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+  __shared__ __attribute__((aligned(16))) float2 angles[ROT ? (OUT == ROPE_BY_HEADS ? 512 : 64 * E * U) : 1];  // [token][pair]
+  typedef const __attribute__((address_space(4))) RopeArgs* Kernarg;  // where `a` lies
+  Kernarg args = (Kernarg)__builtin_amdgcn_kernarg_segment_ptr();
+  bool left;
+  // Through the pointer the arguments are loaded where they are used, as `a` all at the start: by heads
+  // 31.4 and 32.8 us (q and k of 16384 tokens in packed rows, 16 heads of 72 dims), the others 6.2 and
+  // 6.0 (the same of 4096 tokens, 12 heads of 64).
+  if constexpr (OUT == ROPE_BY_HEADS)
+    left = rope_pass<T, E, U, ADJ, NORM, ROT, PART, OUT, false>(*(const RopeArgs*)args, (int)threadIdx.x, angles);
+  else
+    left = rope_pass<T, E, U, ADJ, NORM, ROT, PART, OUT, false>(a, (int)threadIdx.x, angles);
+  if constexpr (NORM) {
+    if (!__any(left)) return;
+    // The heads that were left, in a pass of their own, which finds its places again (the empty asm
+    // hides that it has them, so that no register is kept for it): a branch to the scaling within
+    // the loop cost 2 to 4 %.
+    int tid = (int)threadIdx.x;
+    asm volatile("" : "+v"(tid), "+s"(args));
+    rope_pass<T, E, U, ADJ, NORM, ROT, PART, OUT, true>(*(const RopeArgs*)args, tid, angles);
   }
 }
 

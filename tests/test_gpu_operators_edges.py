@@ -1,0 +1,69 @@
+"""Operators without a model at the edges of their ranges: heads whose squares leave fp32's,
+gains that are not finite, tensors that are no plain ones, calls that take long.
+
+Tolerances as in test_gpu_operators.py.
+"""
+import numpy as np
+import pytest
+
+from test_gpu_operators import BF16, DTYPES, FP32, HALF, NORM, gen, ids, plain_qk, plain_turn, positions, randn, worst
+
+pytestmark = pytest.mark.gpu
+
+from gpu_util import torch  # noqa: E402
+
+# sizes of heads for each eps: mean squares (and eps itself) below fp32's normal numbers, among
+# them heads of subnormal elements ("tiny"), above its largest, and ordinary ones beside them
+FAR = [(0.0, [1.0, 1e-19, 1e-22, 1e-30, 1e-37, "tiny", 1e19, 1e25, 3e37]), (1e-40, [1.0, 1e-19, 1e-22, 1e-30, 1e-37, 0.0, 1e25]),
+       (1e-30, [1.0, 1e-30, 1e-15, 1e-10, 0.0, 1e25]), (1e-6, [1.0, 1e-30, 1e-3, 0.0, 1e19, 1e25, 3e37]), (3e38, [1e20, 1e15, 1e25, 0.0])]
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("dims,layout,dh", [([32, 32], "halves", 64), ([24, 24], "adjacent", 72), ([18, 18], "halves", 36), ([50, 40], "axis_halves", 98),
+                                            ([256], "adjacent", 256), ([2], "adjacent", 2)])
+def test_norm_of_heads_whose_squares_leave_the_range(dims, layout, dh, dtype):
+    """Scaling by a power of two is exact, so the roundings are those of any other head (NORM); an
+    ordinary head has the same bits whatever heads it stands beside."""
+    from paper_2511_22009_amd import Rotary, qk_norm_rotate
+    g = gen(100 + dh)
+    r, T, H = Rotary(dims, layout=layout), 21, 16
+    pos = positions(g, 1, T, len(dims))
+    gain = 1 + 0.3 * randn(g, dh)
+    for eps, sizes in FAR:
+        eps = float(np.float32(eps))
+        tiny = 2.0 ** -140 if dtype == FP32 else 2.0 ** -130
+        size = torch.tensor([tiny if s == "tiny" else s for s in sizes], dtype=torch.float64, device="cuda")
+        at = torch.randint(len(sizes), (1, T, H, 1), generator=g, device="cuda")
+        plain = randn(g, 1, T, H, dh).double()
+        plain = torch.sign(plain) * plain.abs().clamp_min(0.5)       # no head is all zero by rounding
+        q = (plain * size[at]).to(dtype)
+        for x in (q, q.transpose(1, 2).contiguous().transpose(1, 2)):
+            for rotary in (r, None):
+                got, _ = qk_norm_rotate(x, None, gain, None, pos, rotary, eps=eps)
+                want = plain_qk(x, gain, eps)
+                want, pair = (want, want.abs()) if rotary is None else plain_turn(want, pos, dims, layout)
+                assert worst(got, want, NORM * pair + HALF[dtype] * want.abs()) <= 1.0
+        if 1.0 in sizes:
+            ordinary = at[..., 0] == sizes.index(1.0)
+            beside = q.clone()
+            beside[~ordinary] = 1.0
+            got, _ = qk_norm_rotate(q, None, gain, None, pos, r, eps=eps)
+            alone, _ = qk_norm_rotate(beside, None, gain, None, pos, r, eps=eps)
+            assert torch.equal(got[ordinary], alone[ordinary])
+
+
+def test_norm_of_far_heads_that_are_not_finite():
+    """An infinity divides the finite dims of its head to 0 and itself to NaN, as the formula does;
+    a NaN takes its head, and heads of other sizes beside them are as alone."""
+    from paper_2511_22009_amd import qk_norm_rotate
+    x = randn(gen(101), 1, 9, 4, 64) * 1e-25
+    want, _ = qk_norm_rotate(x, None, eps=0.0)
+    y = x.clone()
+    y[0, 2, 1, 5] = float("inf")
+    y[0, 3, 0, 7] = float("nan")
+    got, _ = qk_norm_rotate(y, None, eps=0.0)
+    assert torch.isnan(got[0, 2, 1, 5]) and torch.isnan(got[0, 3, 0]).all()
+    got[0, 2, 1, 5] = 0.0
+    assert not got[0, 2, 1].any()
+    got[0, 2, 1], got[0, 3, 0] = want[0, 2, 1], want[0, 3, 0]
+    assert torch.equal(got, want)
