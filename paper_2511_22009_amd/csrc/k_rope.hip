@@ -239,6 +239,8 @@ __device__ __forceinline__ bool rope_pass(const RopeArgs& a, int tid, float2* an
           yy[u][e] *= gy;
         }
       }
+      // a dim that stays has no part in its neighbour, whatever its gain
+      if (PART && !turns[u]) xy[u][e] = yx[u][e] = 0.0f;
     }
   const float inv_dh = 1.0f / (float)a.dh;
   bool left = false;

@@ -67,3 +67,23 @@ def test_norm_of_far_heads_that_are_not_finite():
     assert not got[0, 2, 1].any()
     got[0, 2, 1], got[0, 3, 0] = want[0, 2, 1], want[0, 3, 0]
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("dims,dh", [([32], 64), ([6, 4], 18)])
+def test_gains_of_dims_that_stay_are_their_own(dims, dh, bad, dtype):
+    """A gain that is not finite on a dim that no pair turns changes that dim alone."""
+    from paper_2511_22009_amd import Rotary, qk_norm_rotate
+    for layout in ("adjacent", "halves", "axis_halves"):
+        g = gen(102)
+        r, pos = Rotary(dims, layout=layout), positions(g, 2, 7, len(dims))
+        q, gain = randn(g, 2, 7, 3, dh, dtype=dtype), 1 + 0.2 * randn(g, dh)
+        want, _ = qk_norm_rotate(q, None, gain, None, pos, r)
+        for d in (sum(dims), dh - 1):
+            far = gain.clone()
+            far[d] = bad
+            got, _ = qk_norm_rotate(q, None, far, None, pos, r)
+            assert not torch.isfinite(got[..., d]).any()
+            got[..., d] = want[..., d]
+            assert torch.equal(got, want)
