@@ -92,6 +92,10 @@ class Rotary:
                              self.theta)
         self._address = ctypes.addressof(self._struct)
 
+    def __reduce__(self):
+        # copies and pickles are made anew: the address of another's struct would outlive it
+        return type(self), (self.dims, self.theta, self.layout, self.spread)
+
 
 def rotate(x, positions, rotary, inverse=False, out=None, stream=None):
     """x [rows, tokens, heads, dims] (bfloat16 or float32, dims adjacent, other strides
