@@ -32,3 +32,34 @@ def test_copies_of_a_plan_have_memory_of_their_own(way):
     assert c._address != r._address
     del r
     assert plan(c) == want
+
+
+def run(code):
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stderr
+    return r.stdout.split()
+
+
+NAMES = ["Rotary", "matmul_i8", "qk_norm_rotate", "quantize_rows", "rotate"]
+
+
+@pytest.mark.parametrize("missing", ["torch", "paper_2511_22009_amd._operators"])
+def test_every_name_of_the_package_without_torch_or_the_operators_binding(missing):
+    """`import *` gives what can be loaded: all but the operators, which need both; these say so."""
+    got = run(f"import sys; sys.modules[{missing!r}] = None\n"
+              "from paper_2511_22009_amd import *\n"
+              "import paper_2511_22009_amd as p\n"
+              "assert Model is p.Model and load_library() is not None\n"
+              "try:\n    p.rotate\nexcept ImportError: print('refused')\n"
+              "print(*(n for n in dir() if not n.startswith('_')))")
+    assert got[0] == "refused" and "Model" in got and "library_symbols" in got and not set(NAMES) & set(got)
+
+
+def test_every_name_of_the_package():
+    pytest.importorskip("torch")
+    got = run("from paper_2511_22009_amd import *\nprint(*(n for n in dir() if not n.startswith('_')))")
+    assert set(NAMES) < set(got) and "Model" in got
+
+
+def test_importing_the_package_needs_no_torch():
+    assert run("import paper_2511_22009_amd, sys\nprint('torch' in sys.modules)") == ["False"]
