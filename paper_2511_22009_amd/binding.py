@@ -349,6 +349,8 @@ class Model:
         token's place in the latent grid (see sf_set_qk). q_gain, k_gain: host arrays
         [L, head dim] or None (1); rotary: a `Rotary` of two axes (patch row, patch column)
         or None."""
+        if rotary is not None and not isinstance(getattr(rotary, "_struct", None), _Rope):
+            raise TypeError(f"rotary: expected a Rotary, got {type(rotary).__name__}")
         n = self.info["L"] * (self.info["D"] // self.info["heads"])
         gains = [None if g is None else _host_f32(g, n, what) for g, what in ((q_gain, "q_gain"), (k_gain, "k_gain"))]
         p = _QK(int(bool(norm)), float(eps), *[None if g is None else _ptr(g) for g in gains],

@@ -63,3 +63,19 @@ def test_every_name_of_the_package():
 
 def test_importing_the_package_needs_no_torch():
     assert run("import paper_2511_22009_amd, sys\nprint('torch' in sys.modules)") == ["False"]
+
+
+@pytest.mark.parametrize("bad", [(16, 16), {"dims": (16, 16)}, 5, object()])
+def test_set_qk_takes_a_plan_and_nothing_else(bad):
+    from paper_2511_22009_amd import Model, load_library
+    load_library()
+    m = Model.__new__(Model)                     # no handle: the library answers that none is loaded
+    m._h, m.info = None, dict(L=2, D=128, heads=4)
+    with pytest.raises(TypeError, match="rotary"):
+        m.set_qk(rotary=bad)
+    pytest.importorskip("torch")
+    from paper_2511_22009_amd import Rotary, SFError
+    for good in (None, Rotary([16, 16])):
+        with pytest.raises(SFError) as e:
+            m.set_qk(rotary=good)
+        assert e.value.code == -3
