@@ -8,6 +8,7 @@
 
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -55,6 +56,8 @@ const auto kCodes = {at::kChar};
 const at::Tensor& tensor(PyObject* o, const char* what, std::initializer_list<at::ScalarType> types) {
   if (!THPVariable_Check(o) || !THPVariable_Unpack(o).is_cuda()) bad_type(what, ": expected a CUDA tensor");
   const at::Tensor& t = THPVariable_Unpack(o);
+  if (t.requires_grad() && c10::GradMode::is_enabled())
+    bad_type(what, ": requires grad, and nothing here is differentiated; call under torch.no_grad() or detach it");
   for (const at::ScalarType s : types)
     if (t.scalar_type() == s) return t;
   bad_type(what, ": expected ", types.size() > 1 ? "BFloat16 or Float" : c10::toString(*types.begin()), ", got ",

@@ -8,7 +8,8 @@ for sizes and strides, SFError for what the library refuses. A call runs on the 
 its tensors, on `stream` or torch's current stream there. Outputs that are not given are
 allocated for that stream. With a `stream` other than the current one, ordering it after
 the work that fills the inputs is the caller's, as in torch; the inputs' memory is kept
-until the stream is done with it. Nothing is differentiated.
+until the stream is done with it. Nothing is differentiated: a tensor that requires grad is
+a TypeError unless gradients are off (torch.no_grad, torch.inference_mode).
 """
 import ctypes
 

@@ -87,3 +87,44 @@ def test_gains_of_dims_that_stay_are_their_own(dims, dh, bad, dtype):
             assert not torch.isfinite(got[..., d]).any()
             got[..., d] = want[..., d]
             assert torch.equal(got, want)
+
+
+def calls(x, codes, scale, h, pos, gain):
+    """Every operator's call with each of its tensors in turn replaced by f of it."""
+    from paper_2511_22009_amd import Rotary, matmul_i8, qk_norm_rotate, quantize_rows, rotate
+    r = Rotary([32, 32])
+    yield lambda f: quantize_rows(f(x))
+    yield lambda f: quantize_rows(x, scale=f(scale))
+    yield lambda f: matmul_i8(codes, f(scale), codes, scale)
+    yield lambda f: matmul_i8(codes, scale, codes, f(scale))
+    yield lambda f: matmul_i8(codes, scale, codes, scale, f(scale))
+    yield lambda f: matmul_i8(codes, scale, codes, scale, out=f(torch.empty((4, 4), device="cuda")))
+    yield lambda f: rotate(f(h), pos, r)
+    yield lambda f: rotate(h, f(pos), r)
+    yield lambda f: rotate(h, pos, r, out=f(h.clone()))
+    yield lambda f: qk_norm_rotate(f(h), h, gain, gain, pos, r)
+    yield lambda f: qk_norm_rotate(h, f(h), gain, gain, pos, r)
+    yield lambda f: qk_norm_rotate(h, h, f(gain), gain, pos, r)
+    yield lambda f: qk_norm_rotate(h, h, gain, f(gain), pos, r)
+    yield lambda f: qk_norm_rotate(h, h, gain, gain, f(pos), r)
+    yield lambda f: qk_norm_rotate(h, None, out=(f(h.clone()), None))
+
+
+def call_inputs():
+    from paper_2511_22009_amd import quantize_rows
+    g = gen(103)
+    x = randn(g, 4, 32)
+    return x, *quantize_rows(x), randn(g, 2, 3, 4, 64), positions(g, 1, 3, 2)[0], 1 + 0.2 * randn(g, 64)
+
+
+def test_tensors_that_require_grad_are_refused_while_gradients_are_recorded():
+    """Nothing is differentiated, so a gradient would be lost without a word."""
+    for call in calls(*call_inputs()):
+        with pytest.raises(TypeError, match="requires grad"):
+            call(lambda t: t.detach().clone().requires_grad_())
+        call(lambda t: t.detach().clone().requires_grad_().detach())
+        with torch.no_grad():
+            want = call(lambda t: t)
+            got = call(lambda t: t.detach().clone().requires_grad_())
+        for a, b in zip(*((v if isinstance(v, tuple) else (v,)) for v in (got, want))):
+            assert a is None and b is None or torch.equal(a, b)
