@@ -58,6 +58,7 @@ const at::Tensor& tensor(PyObject* o, const char* what, std::initializer_list<at
   const at::Tensor& t = THPVariable_Unpack(o);
   if (t.requires_grad() && c10::GradMode::is_enabled())
     bad_type(what, ": requires grad, and nothing here is differentiated; call under torch.no_grad() or detach it");
+  if (t.is_neg()) bad_type(what, ": a lazily negated view, whose memory holds the opposite values; call resolve_neg()");
   for (const at::ScalarType s : types)
     if (t.scalar_type() == s) return t;
   bad_type(what, ": expected ", types.size() > 1 ? "BFloat16 or Float" : c10::toString(*types.begin()), ", got ",

@@ -128,3 +128,16 @@ def test_tensors_that_require_grad_are_refused_while_gradients_are_recorded():
             got = call(lambda t: t.detach().clone().requires_grad_())
         for a, b in zip(*((v if isinstance(v, tuple) else (v,)) for v in (got, want))):
             assert a is None and b is None or torch.equal(a, b)
+
+
+def test_tensors_with_a_lazy_negation_are_refused():
+    """Their memory holds the values' opposites."""
+    for call in calls(*call_inputs()):
+        with pytest.raises(TypeError, match="negat"):
+            call(torch._neg_view)
+        call(lambda t: torch._neg_view(t.clone()).resolve_neg())
+    # one that public calls make: the imaginary part of a conjugate
+    from paper_2511_22009_amd import quantize_rows
+    z = torch.complex(randn(gen(104), 6), randn(gen(105), 6))
+    with pytest.raises(TypeError, match="negat"):
+        quantize_rows(z.conj().imag[:, None])
