@@ -100,6 +100,27 @@ int as_int(int64_t v, const char* what) {
   return (int)v;
 }
 
+// Other Python threads run while this one allocates or calls the library, either of which may wait for
+// the GPU; an exception takes the lock again on its way.
+class Unlocked {
+ public:
+  Unlocked() : state_(PyEval_SaveThread()) {}
+  ~Unlocked() { PyEval_RestoreThread(state_); }
+  Unlocked(const Unlocked&) = delete;
+
+ private:
+  PyThreadState* state_;
+};
+template <typename F>
+auto unlocked(F f) {
+  const Unlocked u;
+  return f();
+}
+
+at::Tensor made(at::IntArrayRef sizes, at::IntArrayRef strides, const at::TensorOptions& options) {
+  return unlocked([&] { return at::empty_strided(sizes, strides, options); });
+}
+
 PyObject* pair(PyObject* a, PyObject* b) {
   PyObject* const r = a && b ? PyTuple_Pack(2, a, b) : nullptr;
   Py_XDECREF(a);
@@ -135,7 +156,7 @@ PyObject* quantize_rows(PyObject* const* args) {
   int64_t ldc;
   if (args[1] == Py_None) {
     ldc = cols < 1024 ? need : (cols + 127) / 128 * 128;  // whole cache lines
-    codes = at::empty_strided({rows, ldc}, {ldc, 1}, x.options().dtype(at::kChar));
+    codes = made({rows, ldc}, {ldc, 1}, x.options().dtype(at::kChar));
     if (ldc != cols) codes = codes.narrow(1, 0, cols);
   } else {
     codes = tensor(args[1], "out", kCodes);
@@ -145,14 +166,17 @@ PyObject* quantize_rows(PyObject* const* args) {
   }
   float* to;
   if (args[2] == Py_None) {
-    scale = at::empty_strided({rows}, {1}, x.options().dtype(at::kFloat));
+    scale = made({rows}, {1}, x.options().dtype(at::kFloat));
     to = (float*)scale.data_ptr();
   } else {
     to = const_cast<float*>(vector(args[2], "scale", rows, device));
   }
-  check(g_quantize_rows(x.data_ptr(), type_of(x), rows, as_int(cols, "x"), x.stride(0), (signed char*)codes.data_ptr(), ldc, to,
-                        stream_of(device)),
-        "sf_quantize_rows");
+  const int width = as_int(cols, "x");
+  void* const stream = stream_of(device);
+  const int rc = unlocked([&] {
+    return g_quantize_rows(x.data_ptr(), type_of(x), rows, width, x.stride(0), (signed char*)codes.data_ptr(), ldc, to, stream);
+  });
+  check(rc, "sf_quantize_rows");
   return pair(given_or(args[1], codes), given_or(args[2], scale));
 }
 
@@ -183,7 +207,7 @@ PyObject* matmul_i8(PyObject* const* args) {
   if (args[6] == Py_None) {
     const long type = PyLong_AsLong(args[5]);
     if (type == -1 && PyErr_Occurred()) throw Raised{};
-    out = at::empty_strided({M, N}, {N, 1}, a.options().dtype(type == SF_PREC_BF16 ? at::kBFloat16 : at::kFloat));
+    out = made({M, N}, {N, 1}, a.options().dtype(type == SF_PREC_BF16 ? at::kBFloat16 : at::kFloat));
   } else {
     out = tensor(args[6], "out", kReals);
     if (out.dim() != 2 || out.size(0) != M || out.size(1) != N || out.get_device() != device || (N > 1 && out.stride(1) != 1) ||
@@ -192,9 +216,13 @@ PyObject* matmul_i8(PyObject* const* args) {
                 out.strides(), " on ", out.device());
     if (M > 1) ldo = out.stride(0);
   }
-  check(g_matmul_i8((const signed char*)a.data_ptr(), lda, sa, (const signed char*)b.data_ptr(), ldb, sb, bias, as_int(M, "a"),
-                    as_int(N, "b"), as_int(K, "a"), out.data_ptr(), ldo, type_of(out), stream_of(device)),
-        "sf_matmul_i8");
+  const int m = as_int(M, "a"), n = as_int(N, "b"), k = as_int(K, "a");
+  void* const stream = stream_of(device);
+  const int rc = unlocked([&] {
+    return g_matmul_i8((const signed char*)a.data_ptr(), lda, sa, (const signed char*)b.data_ptr(), ldb, sb, bias, m, n, k,
+                       out.data_ptr(), ldo, type_of(out), stream);
+  });
+  check(rc, "sf_matmul_i8");
   return given_or(args[6], out);
 }
 
@@ -208,9 +236,11 @@ const at::Tensor& heads_in(PyObject* o, const char* what) {
 // The output for x (allocated into `out` where none is given), and both as the library takes them.
 sf_heads heads_of(const at::Tensor& x, const char* what, PyObject* given, at::Tensor& out) {
   if (given == Py_None) {
-    out = at::empty_like(x);
-    // an x whose entries overlap (windows): its strides' order is not the output's
-    if (out.stride(3) != 1) out = at::empty_like(x, at::MemoryFormat::Contiguous);
+    out = unlocked([&] {
+      const at::Tensor like = at::empty_like(x);
+      // an x whose entries overlap (windows): its strides' order is not the output's
+      return like.stride(3) == 1 ? like : at::empty_like(x, at::MemoryFormat::Contiguous);
+    });
   } else {
     out = tensor(given, what, {x.scalar_type()});
     if (out.sizes() != x.sizes() || out.get_device() != x.get_device() || (x.size(3) > 1 && out.stride(3) != 1))
@@ -254,9 +284,10 @@ PyObject* rotate(PyObject* const* args) {
   const c10::DeviceGuard guard(x.device());
   at::Tensor out;
   const sf_heads h = heads_of(x, "x", args[4], out);
-  check(g_rotate(&h, type_of(x), as_int(x.size(0), "x"), as_int(x.size(1), "x"), as_int(x.size(3), "x"), rope, pos.at, pos.row,
-                 inverse, stream_of(x.get_device())),
-        "sf_rotate");
+  const int rows = as_int(x.size(0), "x"), tokens = as_int(x.size(1), "x"), dims = as_int(x.size(3), "x");
+  void* const stream = stream_of(x.get_device());
+  const int rc = unlocked([&] { return g_rotate(&h, type_of(x), rows, tokens, dims, rope, pos.at, pos.row, inverse, stream); });
+  check(rc, "sf_rotate");
   return given_or(args[4], out);
 }
 
@@ -289,9 +320,13 @@ PyObject* qk_norm_rotate(PyObject* const* args) {
   const sf_heads hq = heads_of(q, "q", args[7], q_out);
   sf_heads hk{};
   if (has_k) hk = heads_of(THPVariable_Unpack(args[1]), "k", args[8], k_out);
-  check(g_qk_norm_rotate(&hq, has_k ? &hk : nullptr, q_gain, k_gain, (float)eps, type_of(q), as_int(q.size(0), "q"),
-                         as_int(q.size(1), "q"), as_int(dims, "q"), rope, pos.at, pos.row, stream_of(device)),
-        "sf_qk_norm_rotate");
+  const int rows = as_int(q.size(0), "q"), tokens = as_int(q.size(1), "q"), dh = as_int(dims, "q");
+  void* const stream = stream_of(device);
+  const int rc = unlocked([&] {
+    return g_qk_norm_rotate(&hq, has_k ? &hk : nullptr, q_gain, k_gain, (float)eps, type_of(q), rows, tokens, dh, rope, pos.at,
+                            pos.row, stream);
+  });
+  check(rc, "sf_qk_norm_rotate");
   return pair(given_or(args[7], q_out), has_k ? given_or(args[8], k_out) : Py_NewRef(Py_None));
 }
 

@@ -141,3 +141,48 @@ def test_tensors_with_a_lazy_negation_are_refused():
     z = torch.complex(randn(gen(104), 6), randn(gen(105), 6))
     with pytest.raises(TypeError, match="negat"):
         quantize_rows(z.conj().imag[:, None])
+
+
+WAITS = r"""
+#include <time.h>
+volatile int flag = 0;
+extern "C" int wait_for_flag() {
+  struct timespec t = {0, 1000000};
+  for (int i = 0; i < 5000 && !flag; ++i) nanosleep(&t, 0);
+  return flag ? 0 : -1;
+}
+"""
+
+
+def test_other_threads_run_while_a_call_is_under_way(tmp_path):
+    """In the place of the library's entry points stands a function that waits (5 s at most) for what
+    another Python thread does. Nothing is launched."""
+    import ctypes
+    import subprocess
+    import threading
+
+    from paper_2511_22009_amd import operators
+    src, lib = str(tmp_path / "w.cpp"), str(tmp_path / "w.so")
+    with open(src, "w") as f:
+        f.write(WAITS)
+    subprocess.run(["g++", "-shared", "-fPIC", "-O1", src, "-o", lib], check=True)
+    w = ctypes.CDLL(lib)
+    flag = ctypes.c_int.in_dll(w, "flag")
+    inputs = call_inputs()
+    address = ctypes.cast(w.wait_for_flag, ctypes.c_void_p).value
+    entries = [ctypes.cast(getattr(operators.load_library(), "sf_" + n), ctypes.c_void_p).value
+               for n in ("quantize_rows", "matmul_i8", "rotate", "qk_norm_rotate")]
+    raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", operators._raw_stream)
+    try:
+        operators._ext.bind(operators._check, raw_stream, *[address] * 4)
+        for call in calls(*inputs):
+            flag.value = 0
+            setter = threading.Timer(0.02, lambda: setattr(flag, "value", 1))
+            setter.start()
+            call(lambda t: t)                      # SFError after 5 s if no other thread could run
+            setter.join()
+    finally:
+        operators._ext.bind(operators._check, raw_stream, *entries)
+    x = randn(gen(106), 4, 32)
+    codes, scale = operators.quantize_rows(x)          # the library's own again
+    assert float((codes * scale[:, None] - x).abs().max()) <= float(x.abs().max()) / 250
