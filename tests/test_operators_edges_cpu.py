@@ -79,3 +79,43 @@ def test_set_qk_takes_a_plan_and_nothing_else(bad):
         with pytest.raises(SFError) as e:
             m.set_qk(rotary=good)
         assert e.value.code == -3
+
+
+PAIRS = r"""
+#include <cstdio>
+#include <cstdlib>
+#include "sf_ops_rules.h"
+// widths, MLP widths and token rows; prints the tiles of QKV, GELU and residual
+int main(int n, char** v) {
+  for (int i = 1; i + 2 < n; i += 3) {
+    const long D = std::atol(v[i]), F = std::atol(v[i + 1]), M = std::atol(v[i + 2]);
+    std::printf("q%d g%d r%d r%d\n", (int)sf::choose_gemm_i8_tile(M, 3 * D, D, true, false), (int)sf::choose_gemm_i8_tile(M, F, D, true, false),
+                (int)sf::choose_gemm_i8_tile(M, D, D, true, true), (int)sf::choose_gemm_i8_tile(M, D, F, true, true));
+  }
+  return 0;
+}
+"""
+
+
+def test_gpu_cases_of_8_bit_projections_take_every_tile(tmp_path):
+    """Every tile that a projection with an epilogue of its own can take is one that a case of
+    test_gpu_int8_tiles.py takes: all but the largest, for each of the three epilogues."""
+    import os
+    pytest.importorskip("torch")
+    import workloads
+    from test_gpu_int8_tiles import SHAPES
+    csrc = os.path.join(ROOT, "paper_2511_22009_amd", "csrc")
+    src, exe = str(tmp_path / "t.cpp"), str(tmp_path / "t")
+    with open(src, "w") as f:
+        f.write(PAIRS)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", csrc, src, "-o", exe], check=True)
+
+    def tiles(shapes):
+        out = subprocess.run([exe, *(str(v) for s in shapes for v in s)], capture_output=True, text=True, check=True).stdout
+        return set(out.split())
+    got = tiles([(c.D, c.mlp, c.N * rows) for c, rows in SHAPES])
+    assert got == {k + str(t) for k in "qgr" for t in range(6)}
+    # the networks of the workloads, with one to all of their rows, and a wide sweep, reach no others
+    named = [workloads.get_config(n) for n in workloads.CONFIGS]
+    assert tiles([(c.D, c.mlp, c.N * r) for c in named for r in range(1, c.rows + 1)]) <= got
+    assert tiles([(D, m * D, M) for D in range(64, 2049, 64) for m in (1, 2, 4) for M in (1, 64, 300, 1024, 4096, 16384, 65536)]) <= got
