@@ -186,3 +186,61 @@ def test_other_threads_run_while_a_call_is_under_way(tmp_path):
     x = randn(gen(106), 4, 32)
     codes, scale = operators.quantize_rows(x)          # the library's own again
     assert float((codes * scale[:, None] - x).abs().max()) <= float(x.abs().max()) / 250
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("M,N,K", [(700, 3001, 1300), (1500, 6001, 1300), (2500, 5001, 777), (4096, 2304, 768), (4096, 768, 4608), (1100, 4608, 1152), (1500, 4600, 1152)])
+def test_products_have_the_same_bits_in_every_tile(M, N, K, dtype):
+    """The whole product in a large tile, against as few rows and columns at a time as take the
+    smallest (test_operators_edges_cpu.py asserts which)."""
+    from paper_2511_22009_amd import matmul_i8
+    g = gen(M + N + K)
+    a, b = (torch.randint(-127, 128, (n, (K + 15) // 16 * 16), generator=g, device="cuda").to(torch.int8)[:, :K] for n in (M, N))
+    sa, sb, bias = torch.rand(M, generator=g, device="cuda"), torch.rand(N, generator=g, device="cuda"), randn(g, N) * 50
+    whole = matmul_i8(a, sa, b, sb, bias, dtype=dtype)
+    bare = matmul_i8(a, sa, b, sb, dtype=dtype)
+    for m0, m1, n0, n1 in ((0, 64, 0, N), (M - 65, M, 0, N), (M // 2 - 7, M // 2, 0, N), (0, M, 0, 64), (0, M, N - 33, N)):
+        part = a[m0:m1], sa[m0:m1], b[n0:n1], sb[n0:n1]
+        assert torch.equal(whole[m0:m1, n0:n1], matmul_i8(*part, bias[n0:n1], dtype=dtype))
+        assert torch.equal(bare[m0:m1, n0:n1], matmul_i8(*part, dtype=dtype))
+
+
+def test_long_calls_on_two_streams_at_once():
+    """Both streams start behind one event that comes after some milliseconds of work, so that every
+    call is queued before the first runs, and each takes tens of us: the streams' kernels run side by side."""
+    from paper_2511_22009_amd import Rotary, matmul_i8, qk_norm_rotate, quantize_rows, rotate
+    r = Rotary([36, 36], layout="halves")
+
+    def chain(x, w, sw, gain, pos, stream=None):
+        a, sa = quantize_rows(x, stream=stream)
+        qkv = matmul_i8(a, sa, w, sw, stream=stream).view(4, -1, 24, 72)
+        q, k = qk_norm_rotate(qkv[:, :, :8], qkv[:, :, 8:16], gain, gain, pos, r, stream=stream)
+        return a, sa, qkv, q, k, rotate(qkv[:, :, 16:], pos, r, inverse=True, stream=stream)
+    sets, want = [], []
+    for seed in (107, 108):
+        g = gen(seed)
+        w, sw = quantize_rows(randn(g, 3 * 576, 1152, dtype=BF16))
+        sets.append((randn(g, 8192 + 64 * (seed - 107), 1152, dtype=BF16), w, sw, 1 + 0.1 * randn(g, 72),
+                     positions(g, 4, 2048 + 16 * (seed - 107), 2, 500.0)))
+        want.append([t.clone() for t in chain(*sets[-1])])
+    streams = [torch.cuda.Stream() for _ in sets]
+
+    def queue():
+        return [[chain(*args, stream=s) for args, s in zip(sets, streams)] for _ in range(8)]
+    torch.cuda.synchronize()
+    queue()                                                       # the outputs' memory, which the next ones take again
+    busy = torch.randn((8192, 8192), device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(6):
+        busy = (busy @ busy).clamp(-1, 1)
+    held = torch.cuda.Event()
+    held.record()
+    for s in streams:
+        s.wait_event(held)
+    got = queue()
+    queued = not held.query()
+    torch.cuda.synchronize()
+    assert queued, "the work in front ended before the calls were queued"
+    for both in got:
+        for out, alone in zip(both, want):
+            assert all(torch.equal(p, q) for p, q in zip(out, alone))

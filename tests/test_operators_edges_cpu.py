@@ -119,3 +119,32 @@ def test_gpu_cases_of_8_bit_projections_take_every_tile(tmp_path):
     named = [workloads.get_config(n) for n in workloads.CONFIGS]
     assert tiles([(c.D, c.mlp, c.N * r) for c in named for r in range(1, c.rows + 1)]) <= got
     assert tiles([(D, m * D, M) for D in range(64, 2049, 64) for m in (1, 2, 4) for M in (1, 64, 300, 1024, 4096, 16384, 65536)]) <= got
+
+
+TILE = r"""
+#include <cstdio>
+#include <cstdlib>
+#include "sf_ops_rules.h"
+int main(int n, char** v) {
+  for (int i = 1; i + 2 < n; i += 3) std::printf("%d ", (int)sf::choose_gemm_i8_tile(std::atol(v[i]), std::atol(v[i + 1]), std::atol(v[i + 2]), false, false));
+  return 0;
+}
+"""
+
+
+def test_gpu_cases_of_equal_bits_compare_different_tiles(tmp_path):
+    """Whole products in the tiles from 128 x 128 on, parts of them in 64 x 64."""
+    import os
+    pytest.importorskip("torch")
+    from test_gpu_operators_edges import test_products_have_the_same_bits_in_every_tile as t
+    sizes = next(m for m in t.pytestmark if m.args[0] == "M,N,K").args[1]
+    src, exe = str(tmp_path / "t.cpp"), str(tmp_path / "t")
+    with open(src, "w") as f:
+        f.write(TILE)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", os.path.join(ROOT, "paper_2511_22009_amd", "csrc"), src, "-o", exe], check=True)
+
+    def tiles(shapes):
+        return [int(w) for w in subprocess.run([exe, *(str(v) for s in shapes for v in s)], capture_output=True, text=True, check=True).stdout.split()]
+    whole = tiles(sizes)
+    assert set(whole) == {2, 3, 4, 5, 6}
+    assert max(tiles([s for M, N, K in sizes for s in ((64, N, K), (M, 64, K))])) <= 1
