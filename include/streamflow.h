@@ -318,7 +318,8 @@ int sf_timing_read(sf_model* m, int kc, double* total_ms, long* launches);
  * The calls below need no model. They enqueue on hip_stream of the current device, keep
  * no state and no workspace, allocate nothing (so they may be captured into a graph) and
  * give the same bits on every call. Device pointers; strides and row lengths count
- * elements. An empty tensor (a count of 0) is no work and returns SF_OK. */
+ * elements. An empty tensor (a count of 0) is no work and returns SF_OK. Results do not
+ * overlap what a call reads, except as sf_heads allows. */
 
 /* Rows of x to 8-bit codes with one scale per row (a token's activations, or an output
  * channel's weights):
@@ -373,8 +374,9 @@ typedef struct sf_rope {
 
 /* A tensor of heads [rows][tokens][heads][dh], read from `in` and written to `out`, which is
  * `in` itself with the same strides or does not overlap it, nor, in a call with q and k, the
- * other's tensors. The dims of a head are adjacent; the strides (in elements) are free, and
- * those of `in` may be 0. */
+ * other's tensors (SF_E_INVAL where the addresses alone tell otherwise: `out` at `in` with other
+ * strides, or at the other's `in` or `out`). The dims of a head are adjacent; the strides (in
+ * elements) are free, and those of `in` may be 0. At most 65535 heads in a call, q's and k's together. */
 typedef struct sf_heads {
   const void* in;
   void* out;

@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include "sf_ops.h"
 
@@ -49,6 +50,12 @@ bool own_places(const sf_heads& t, int rows, int tokens) {
   return !((rows > 1 && t.out_row == 0) || (tokens > 1 && t.out_token == 0) || (t.heads > 1 && t.out_head == 0));
 }
 
+// Whether results over their own inputs lie where these do, as far as the addresses tell.
+bool apart_or_in_place(const sf_heads& t, int rows, int tokens) {
+  return t.in != t.out || ((rows <= 1 || t.in_row == t.out_row) && (tokens <= 1 || t.in_token == t.out_token) &&
+                           (t.heads <= 1 || t.in_head == t.out_head));
+}
+
 sf::RopeHeads take_heads(const sf_heads& t, const float* gain) {
   return sf::RopeHeads{(const char*)t.in, (char*)t.out, gain,       t.in_row,  t.in_token,
                        t.in_head,         t.out_row,    t.out_token, t.out_head};
@@ -67,8 +74,10 @@ int rope_call(const sf_heads* q, const sf_heads* k, const float* q_gain, const f
   a.heads = q->heads + (k ? k->heads : 0);
   if (rows == 0 || tokens == 0 || a.heads == 0) return SF_OK;
   if (rope && !pos) return SF_E_INVAL;
-  if (q->heads > 0 && (!q->in || !q->out || !own_places(*q, rows, tokens))) return SF_E_INVAL;
-  if (k && k->heads > 0 && (!k->in || !k->out || !own_places(*k, rows, tokens))) return SF_E_INVAL;
+  for (const sf_heads* t : {q, k})
+    if (t && t->heads > 0 && (!t->in || !t->out || !own_places(*t, rows, tokens) || !apart_or_in_place(*t, rows, tokens)))
+      return SF_E_INVAL;
+  if (k && q->heads > 0 && k->heads > 0 && (q->out == k->out || q->out == k->in || k->out == q->in)) return SF_E_INVAL;
   a.t[0] = take_heads(*q, q_gain);
   if (k) a.t[1] = take_heads(*k, k_gain);
   a.dh = dh;

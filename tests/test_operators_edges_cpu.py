@@ -148,3 +148,29 @@ def test_gpu_cases_of_equal_bits_compare_different_tiles(tmp_path):
     whole = tiles(sizes)
     assert set(whole) == {2, 3, 4, 5, 6}
     assert max(tiles([s for M, N, K in sizes for s in ((64, N, K), (M, 64, K))])) <= 1
+
+
+def heads(at, out, n=4, tokens=8, dh=64, row=None, token=None, head=None):
+    from paper_2511_22009_amd import binding
+    s = (tokens * n * dh, n * dh, dh)
+    return binding._Heads(at, out, n, *s, s[0] if row is None else row, s[1] if token is None else token, s[2] if head is None else head)
+
+
+def turned(q, k=None, rows=2, tokens=8):
+    """The status of a call that is refused (addresses are never read): without a GPU one that is not ends at its launch."""
+    from paper_2511_22009_amd import load_library
+    return load_library().sf_qk_norm_rotate(ctypes.byref(q), None if k is None else ctypes.byref(k), None, None, 1e-6, 0, rows, tokens,
+                                            64, None, None, 0, None)
+
+
+@pytest.mark.parametrize("other", [dict(row=1 << 20), dict(token=64, head=512), dict(head=128)])
+def test_results_over_their_inputs_with_other_strides_are_refused(other):
+    """A head would be written over one that is still to be read."""
+    assert turned(heads(4096, 4096, **other)) == -1
+    assert turned(heads(4096, 8192), heads(1 << 20, 1 << 20, **other)) == -1
+
+
+def test_results_over_the_other_tensors_are_refused():
+    a, b, c, d = (1 << 20) * 1, (1 << 20) * 2, (1 << 20) * 3, (1 << 20) * 4
+    for q, k in (((a, b), (b, a)), ((a, c), (b, c)), ((a, b), (b, c)), ((a, c), (b, a)), ((a, a), (a, a)), ((a, a), (a, d))):
+        assert turned(heads(*q), heads(*k)) == -1
