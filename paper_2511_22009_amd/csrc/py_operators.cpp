@@ -117,10 +117,6 @@ auto unlocked(F f) {
   return f();
 }
 
-at::Tensor made(at::IntArrayRef sizes, at::IntArrayRef strides, const at::TensorOptions& options) {
-  return unlocked([&] { return at::empty_strided(sizes, strides, options); });
-}
-
 PyObject* pair(PyObject* a, PyObject* b) {
   PyObject* const r = a && b ? PyTuple_Pack(2, a, b) : nullptr;
   Py_XDECREF(a);
@@ -151,29 +147,27 @@ PyObject* quantize_rows(PyObject* const* args) {
     bad_value("x: expected rows of adjacent values, got shape ", x.sizes(), ", strides ", x.strides());
   const int64_t rows = x.size(0), cols = x.size(1), need = up16(cols);
   const int device = x.get_device();
-  const c10::DeviceGuard guard(x.device());
+  const int width = as_int(cols, "x");
   at::Tensor codes, scale;
-  int64_t ldc;
-  if (args[1] == Py_None) {
-    ldc = cols < 1024 ? need : (cols + 127) / 128 * 128;  // whole cache lines
-    codes = made({rows, ldc}, {ldc, 1}, x.options().dtype(at::kChar));
-    if (ldc != cols) codes = codes.narrow(1, 0, cols);
-  } else {
+  int64_t ldc = cols < 1024 ? need : (cols + 127) / 128 * 128;  // whole cache lines
+  if (args[1] != Py_None) {
     codes = tensor(args[1], "out", kCodes);
     if (codes.sizes() != x.sizes() || codes.get_device() != device)
       bad_value("out: expected ", x.sizes(), " on ", x.device(), ", got ", codes.sizes(), " on ", codes.device());
     ldc = pitch_of(codes, "out", need);
   }
-  float* to;
-  if (args[2] == Py_None) {
-    scale = made({rows}, {1}, x.options().dtype(at::kFloat));
-    to = (float*)scale.data_ptr();
-  } else {
-    to = const_cast<float*>(vector(args[2], "scale", rows, device));
-  }
-  const int width = as_int(cols, "x");
+  float* to = const_cast<float*>(vector(args[2], "scale", rows, device, true));
+  const c10::DeviceGuard guard(x.device());
   void* const stream = stream_of(device);
   const int rc = unlocked([&] {
+    if (!codes.defined()) {
+      codes = at::empty_strided({rows, ldc}, {ldc, 1}, x.options().dtype(at::kChar));
+      if (ldc != cols) codes = codes.narrow(1, 0, cols);
+    }
+    if (args[2] == Py_None) {
+      scale = at::empty_strided({rows}, {1}, x.options().dtype(at::kFloat));
+      to = (float*)scale.data_ptr();
+    }
     return g_quantize_rows(x.data_ptr(), type_of(x), rows, width, x.stride(0), (signed char*)codes.data_ptr(), ldc, to, stream);
   });
   check(rc, "sf_quantize_rows");
@@ -201,13 +195,13 @@ PyObject* matmul_i8(PyObject* const* args) {
   const float* const sa = vector(args[1], "a_scale", M, device);
   const float* const sb = vector(args[3], "b_scale", N, device);
   const float* const bias = vector(args[4], "bias", N, device, true);
-  const c10::DeviceGuard guard(a.device());
+  const int m = as_int(M, "a"), n = as_int(N, "b"), k = as_int(K, "a");
   at::Tensor out;
   int64_t ldo = N;
+  long type = 0;
   if (args[6] == Py_None) {
-    const long type = PyLong_AsLong(args[5]);
+    type = PyLong_AsLong(args[5]);
     if (type == -1 && PyErr_Occurred()) throw Raised{};
-    out = made({M, N}, {N, 1}, a.options().dtype(type == SF_PREC_BF16 ? at::kBFloat16 : at::kFloat));
   } else {
     out = tensor(args[6], "out", kReals);
     if (out.dim() != 2 || out.size(0) != M || out.size(1) != N || out.get_device() != device || (N > 1 && out.stride(1) != 1) ||
@@ -216,9 +210,10 @@ PyObject* matmul_i8(PyObject* const* args) {
                 out.strides(), " on ", out.device());
     if (M > 1) ldo = out.stride(0);
   }
-  const int m = as_int(M, "a"), n = as_int(N, "b"), k = as_int(K, "a");
+  const c10::DeviceGuard guard(a.device());
   void* const stream = stream_of(device);
   const int rc = unlocked([&] {
+    if (!out.defined()) out = at::empty_strided({M, N}, {N, 1}, a.options().dtype(type == SF_PREC_BF16 ? at::kBFloat16 : at::kFloat));
     return g_matmul_i8((const signed char*)a.data_ptr(), lda, sa, (const signed char*)b.data_ptr(), ldb, sb, bias, m, n, k,
                        out.data_ptr(), ldo, type_of(out), stream);
   });
@@ -233,22 +228,25 @@ const at::Tensor& heads_in(PyObject* o, const char* what) {
   return t;
 }
 
-// The output for x (allocated into `out` where none is given), and both as the library takes them.
-sf_heads heads_of(const at::Tensor& x, const char* what, PyObject* given, at::Tensor& out) {
-  if (given == Py_None) {
-    out = unlocked([&] {
-      const at::Tensor like = at::empty_like(x);
-      // an x whose entries overlap (windows): its strides' order is not the output's
-      return like.stride(3) == 1 ? like : at::empty_like(x, at::MemoryFormat::Contiguous);
-    });
-  } else {
-    out = tensor(given, what, {x.scalar_type()});
-    if (out.sizes() != x.sizes() || out.get_device() != x.get_device() || (x.size(3) > 1 && out.stride(3) != 1))
-      bad_value(what, " out: expected ", x.sizes(), " with adjacent dims on ", x.device(), ", got ", out.sizes(), ", strides ",
-                out.strides(), " on ", out.device());
+// The output that is given for x, or an undefined tensor.
+at::Tensor heads_out(const at::Tensor& x, const char* what, PyObject* given) {
+  if (given == Py_None) return {};
+  const at::Tensor& out = tensor(given, what, {x.scalar_type()});
+  if (out.sizes() != x.sizes() || out.get_device() != x.get_device() || (x.size(3) > 1 && out.stride(3) != 1))
+    bad_value(what, " out: expected ", x.sizes(), " with adjacent dims on ", x.device(), ", got ", out.sizes(), ", strides ",
+              out.strides(), " on ", out.device());
+  return out;
+}
+
+// x and its output, allocated where none is given, as the library takes them.
+sf_heads heads_of(const at::Tensor& x, int heads, at::Tensor& out) {
+  if (!out.defined()) {
+    out = at::empty_like(x);
+    // an x whose entries overlap (windows): its strides' order is not the output's
+    if (out.stride(3) != 1) out = at::empty_like(x, at::MemoryFormat::Contiguous);
   }
-  return sf_heads{x.data_ptr(), out.data_ptr(), as_int(x.size(2), what), x.stride(0),   x.stride(1),
-                  x.stride(2),  out.stride(0),  out.stride(1),           out.stride(2)};
+  return sf_heads{x.data_ptr(), out.data_ptr(), heads,         x.stride(0),  x.stride(1),
+                  x.stride(2),  out.stride(0),  out.stride(1), out.stride(2)};
 }
 
 struct Positions {
@@ -281,12 +279,14 @@ PyObject* rotate(PyObject* const* args) {
   const Positions pos = positions(args[1], *rope, x);
   const int inverse = PyObject_IsTrue(args[3]);
   if (inverse < 0) throw Raised{};
+  at::Tensor out = heads_out(x, "x", args[4]);
+  const int rows = as_int(x.size(0), "x"), tokens = as_int(x.size(1), "x"), heads = as_int(x.size(2), "x"), dims = as_int(x.size(3), "x");
   const c10::DeviceGuard guard(x.device());
-  at::Tensor out;
-  const sf_heads h = heads_of(x, "x", args[4], out);
-  const int rows = as_int(x.size(0), "x"), tokens = as_int(x.size(1), "x"), dims = as_int(x.size(3), "x");
   void* const stream = stream_of(x.get_device());
-  const int rc = unlocked([&] { return g_rotate(&h, type_of(x), rows, tokens, dims, rope, pos.at, pos.row, inverse, stream); });
+  const int rc = unlocked([&] {
+    const sf_heads h = heads_of(x, heads, out);
+    return g_rotate(&h, type_of(x), rows, tokens, dims, rope, pos.at, pos.row, inverse, stream);
+  });
   check(rc, "sf_rotate");
   return given_or(args[4], out);
 }
@@ -315,15 +315,16 @@ PyObject* qk_norm_rotate(PyObject* const* args) {
   }
   const double eps = PyFloat_AsDouble(args[6]);
   if (eps == -1.0 && PyErr_Occurred()) throw Raised{};
-  const c10::DeviceGuard guard(q.device());
-  at::Tensor q_out, k_out;
-  const sf_heads hq = heads_of(q, "q", args[7], q_out);
-  sf_heads hk{};
-  if (has_k) hk = heads_of(THPVariable_Unpack(args[1]), "k", args[8], k_out);
+  at::Tensor q_out = heads_out(q, "q", args[7]), k_out;
+  const at::Tensor* const k = has_k ? &THPVariable_Unpack(args[1]) : nullptr;
+  if (k) k_out = heads_out(*k, "k", args[8]);
   const int rows = as_int(q.size(0), "q"), tokens = as_int(q.size(1), "q"), dh = as_int(dims, "q");
+  const int q_heads = as_int(q.size(2), "q"), k_heads = k ? as_int(k->size(2), "k") : 0;
+  const c10::DeviceGuard guard(q.device());
   void* const stream = stream_of(device);
   const int rc = unlocked([&] {
-    return g_qk_norm_rotate(&hq, has_k ? &hk : nullptr, q_gain, k_gain, (float)eps, type_of(q), rows, tokens, dh, rope, pos.at,
+    const sf_heads hq = heads_of(q, q_heads, q_out), hk = k ? heads_of(*k, k_heads, k_out) : sf_heads{};
+    return g_qk_norm_rotate(&hq, k ? &hk : nullptr, q_gain, k_gain, (float)eps, type_of(q), rows, tokens, dh, rope, pos.at,
                             pos.row, stream);
   });
   check(rc, "sf_qk_norm_rotate");
