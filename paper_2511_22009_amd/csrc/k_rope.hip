@@ -14,6 +14,7 @@
 // packed; pieces of 16 bytes, eight pairs to a lane, nothing for 128 dims and 4.5 instead of 3.6 us
 // for a single token; 12 pairs to a lane, wavefronts by tokens throughout and angles per wavefront
 // lost 3 to 10 %.)
+#include <algorithm>
 #include <cmath>
 
 #include "sf_ops_device.h"
@@ -134,6 +135,8 @@ struct Pairs<T, E, true> {
 // head of several tokens, through the L2 or past it, or several heads of one token, past it.
 enum RopeOut { ROPE_PLAIN, ROPE_PAST, ROPE_BY_HEADS };
 
+constexpr int kMostHeads = 32;  // of a lane's in a run, which has a bit for each
+
 // A workgroup of four wavefronts takes 64 / G tokens (by heads: four); its first threads form a
 // pair's angle of a token each and leave cosine and sine in LDS, under the wavefronts' first loads.
 // A wavefront takes a run of heads of q or of k.
@@ -141,9 +144,10 @@ enum RopeOut { ROPE_PLAIN, ROPE_PAST, ROPE_BY_HEADS };
 // memory, or two of one pair each (an element at a time: 98 dims 2.4 to 3.1 TB/s, 36 dims 2.3).
 // ADJ: the layout of adjacent pairs. PART: some dims stay as they are.
 // One pass over a workgroup's heads; FAR: over those alone that the first pass leaves, whose squares fp32
-// does not hold. Returns whether it left a head of the lane's.
+// does not hold. Returns which of the lane's heads it left, a bit each (what memory holds does not
+// tell: results over their inputs may be such heads).
 template <typename T, int E, int U, bool ADJ, bool NORM, bool ROT, bool PART, RopeOut OUT, bool FAR>
-__device__ __forceinline__ bool rope_pass(const RopeArgs& a, int tid, float2* angles) {
+__device__ __forceinline__ uint32_t rope_pass(const RopeArgs& a, int tid, float2* angles, uint32_t far) {
   constexpr int HB = 2;  // heads (of each lane) whose loads are in flight together
   constexpr bool kByHeads = OUT == ROPE_BY_HEADS;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -216,7 +220,7 @@ __device__ __forceinline__ bool rope_pass(const RopeArgs& a, int tid, float2* an
     }
     __syncthreads();
   }
-  if (h0 >= h1) return false;
+  if (h0 >= h1) return 0;
 
   // what takes a pair (x, y) to (x xx + y xy, x yx + y yy): the gains and the turn
   float xx[U][E], xy[U][E], yx[U][E], yy[U][E];
@@ -243,8 +247,8 @@ __device__ __forceinline__ bool rope_pass(const RopeArgs& a, int tid, float2* an
       if (PART && !turns[u]) xy[u][e] = yx[u][e] = 0.0f;
     }
   const float inv_dh = 1.0f / (float)a.dh;
-  bool left = false;
-  for (int hb = h0; hb < h1; hb += HB * abreast) {
+  uint32_t left = 0, bit = 1;
+  for (int hb = h0; hb < h1; hb += HB * abreast, bit <<= HB) {
     float x[HB][U][E], y[HB][U][E];
 #pragma unroll
     for (int b = 0; b < HB; ++b)
@@ -292,17 +296,17 @@ __device__ __forceinline__ bool rope_pass(const RopeArgs& a, int tid, float2* an
       for (int b = 0; b < HB; ++b) {
         // no root: 0, of a sum that overflows, or infinity, of 0 and of subnormal numbers, which the
         // instruction takes for 0
-        put[b] = __builtin_amdgcn_classf(r[b], 0x240) == FAR;
-        left = left || !put[b];
+        put[b] = FAR ? (far & (bit << b)) != 0 : !__builtin_amdgcn_classf(r[b], 0x240);
+        left |= put[b] ? 0 : bit << b;
       }
       if constexpr (FAR) {
-        // Times a power of two, which rounds nothing. A sum that overflows has a mean of 2^120 and more:
+        // Times a power of two, which rounds nothing. What overflows has a mean (with eps) of 2^120 and more:
         // times 2^-70, that is a normal number, and every square is below 2^116. A mean below 2^-126
         // has elements below 2^-59: times 2^100, every square is a normal number. (A mean that is
         // one has lost at most 2^-150 to subnormal squares, half a step of itself.) Heads of zeros with
         // eps 0 and heads that hold an infinity keep a root of infinity and 0: 0 / 0, inf / inf.
         constexpr float kDown = 0x1p-70f, kUp = 0x1p100f;
-        const bool down[HB] = {r[0] == 0.0f, r[1] == 0.0f};
+        const bool down[HB] = {r[0] < 1.0f, r[1] < 1.0f};  // 0, not infinity
         roots([&](int b) { return down[b] ? kDown : kUp; });
 #pragma unroll
         for (int b = 0; b < HB; ++b) {
@@ -351,22 +355,22 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   __shared__ __attribute__((aligned(16))) float2 angles[ROT ? (OUT == ROPE_BY_HEADS ? 512 : 64 * E * U) : 1];  // [token][pair]
   typedef const __attribute__((address_space(4))) RopeArgs* Kernarg;  // where `a` lies
   Kernarg args = (Kernarg)__builtin_amdgcn_kernarg_segment_ptr();
-  bool left;
+  uint32_t left;
   // Through the pointer the arguments are loaded where they are used, as `a` all at the start: by heads
   // 31.4 and 32.8 us (q and k of 16384 tokens in packed rows, 16 heads of 72 dims), the others 6.2 and
   // 6.0 (the same of 4096 tokens, 12 heads of 64).
   if constexpr (OUT == ROPE_BY_HEADS)
-    left = rope_pass<T, E, U, ADJ, NORM, ROT, PART, OUT, false>(*(const RopeArgs*)args, (int)threadIdx.x, angles);
+    left = rope_pass<T, E, U, ADJ, NORM, ROT, PART, OUT, false>(*(const RopeArgs*)args, (int)threadIdx.x, angles, 0);
   else
-    left = rope_pass<T, E, U, ADJ, NORM, ROT, PART, OUT, false>(a, (int)threadIdx.x, angles);
+    left = rope_pass<T, E, U, ADJ, NORM, ROT, PART, OUT, false>(a, (int)threadIdx.x, angles, 0);
   if constexpr (NORM) {
-    if (!__any(left)) return;
+    if (!__any(left != 0)) return;
     // The heads that were left, in a pass of their own, which finds its places again (the empty asm
     // hides that it has them, so that no register is kept for it): a branch to the scaling within
     // the loop cost 2 to 4 %.
     int tid = (int)threadIdx.x;
     asm volatile("" : "+v"(tid), "+s"(args));
-    rope_pass<T, E, U, ADJ, NORM, ROT, PART, OUT, true>(*(const RopeArgs*)args, tid, angles);
+    rope_pass<T, E, U, ADJ, NORM, ROT, PART, OUT, true>(*(const RopeArgs*)args, tid, angles, left);
   }
 }
 
@@ -443,14 +447,19 @@ hipError_t launch_rope(bool is_bf16, bool norm, bool rotate, RopeArgs a, hipStre
   const int most = (a.heads + 3) / 4;
   if (splits > most) splits = most;
   if (by_heads && a.heads0 > 0 && heads1 > 0 && splits < 2) splits = 2;
-  // q and k share the runs of heads
-  const int chunks = (int)splits * waves;
-  a.chunks0 = (int)(((int64_t)chunks * a.heads0 + a.heads / 2) / a.heads);
-  if (heads1 > 0 && a.chunks0 == chunks) --a.chunks0;
-  if (a.heads0 > 0 && a.chunks0 == 0) a.chunks0 = 1;
   const auto run = [&](int heads, int n) { return n > 0 ? ((heads + n - 1) / n + abreast - 1) / abreast * abreast : 1; };
-  a.step[0] = run(a.heads0, a.chunks0);
-  a.step[1] = run(heads1, chunks - a.chunks0);
+  const int longest = kMostHeads * abreast;
+  splits = std::max(splits, (int64_t)a.heads / (waves * longest));
+  for (;; ++splits) {
+    // q and k share the runs of heads
+    const int chunks = (int)splits * waves;
+    a.chunks0 = (int)(((int64_t)chunks * a.heads0 + a.heads / 2) / a.heads);
+    if (heads1 > 0 && a.chunks0 == chunks) --a.chunks0;
+    if (a.heads0 > 0 && a.chunks0 == 0) a.chunks0 = 1;
+    a.step[0] = run(a.heads0, a.chunks0);
+    a.step[1] = run(heads1, chunks - a.chunks0);
+    if (a.step[0] <= longest && a.step[1] <= longest) break;
+  }
   const dim3 grid((uint32_t)groups, (uint32_t)splits);
   return is_bf16 ? launch_rope_type<bf16>(a, norm, rotate, whole, out, grid, s) : launch_rope_type<float>(a, norm, rotate, whole, out, grid, s);
 }

@@ -244,3 +244,29 @@ def test_long_calls_on_two_streams_at_once():
     for both in got:
         for out, alone in zip(both, want):
             assert all(torch.equal(p, q) for p, q in zip(out, alone))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids)
+@pytest.mark.parametrize("heads", [5, 33, 200, 700])
+def test_norm_in_place_beside_far_heads(heads, dtype):
+    """Results over their inputs, where some heads' squares leave fp32's range and others' results do
+    (gains of 0 and 1e-30): every head is treated once, as with outputs apart."""
+    from paper_2511_22009_amd import Rotary, qk_norm_rotate
+    for dh, layout, T in ((64, "halves", 3), (72, "adjacent", 1500), (36, "halves", 40)):
+        g = gen(109 + dh)
+        if heads * T > 100000:
+            T = 100
+        r, pos = Rotary([16, 16], layout=layout), positions(g, 1, T, 2)
+        size = torch.tensor([1.0, 1e-25, 1e25], device="cuda")[torch.randint(3, (1, T, heads, 1), generator=g, device="cuda")]
+        q = (randn(g, 1, T, heads, dh) * size).to(dtype)
+        for gain in (torch.zeros(dh, device="cuda"), torch.full((dh,), 1e-30, device="cuda"), 1 + 0.2 * randn(g, dh)):
+            for x in (q, q.transpose(1, 2).contiguous().transpose(1, 2)):
+                for rotary in (r, None):
+                    want, _ = qk_norm_rotate(x, None, gain, None, pos, rotary, eps=0.0)
+                    y = x.clone(memory_format=torch.preserve_format)
+                    qk_norm_rotate(y, None, gain, None, pos, rotary, eps=0.0, out=(y, None))
+                    assert torch.isfinite(want).all() and torch.equal(y, want)
+                    both = x.clone(memory_format=torch.preserve_format)
+                    k = torch.ones_like(q)
+                    qk_norm_rotate(both, k, gain, None, pos, rotary, eps=0.0, out=(both, k))
+                    assert torch.equal(both, want)
