@@ -361,7 +361,8 @@ int sf_matmul_i8(const signed char* a, long long lda, const float* a_scale, cons
  *   spread:  0: f = theta^(-2 i / dims[a]) for pair i of axis a (every axis has the whole
  *            range of frequencies); 1: f = theta^(-j / P) for pair j of all P (one
  *            range, shared out over the axes).
- * Angles are formed and reduced in fp64, so far positions keep their digits. */
+ * Angles are formed and reduced in fp64, so far positions keep their digits: an angle of |u|
+ * radians is off by some 2^-50 |u|, 1.5e-8 at positions of 2^24. */
 enum { SF_ROPE_ADJACENT = 0, SF_ROPE_HALVES = 1, SF_ROPE_AXIS_HALVES = 2 };
 #define SF_ROPE_AXES 4
 typedef struct sf_rope {
@@ -419,12 +420,12 @@ typedef struct sf_qk {
 /* Set (p != NULL) or clear (p == NULL, the default) the queries' and keys' treatment in
  * sf_velocity, sf_stream_step and sf_residual. Synchronous: waits for the device, uploads the
  * gains and the tokens' places (one device allocation, kept until the next set, clear or
- * sf_free) and drops cached graphs. SF_E_INVAL for neither norm nor rope, gains without norm, or
- * a rope that sf_rotate would refuse or whose axes are not 2; nothing changes then. On
- * SF_E_OOM or SF_E_HIP the treatment is cleared. The allocation fails when
- * SF_FAIL_ALLOC_AFTER is 0, to exercise that path. A graph that the caller captured from the
- * model's calls keeps the treatment it was captured with only until the next set or clear, which
- * frees what it reads: capture again. */
+ * sf_free) and drops cached graphs. SF_E_INVAL for neither norm nor rope, gains without norm, an
+ * eps that is negative or not finite, or a rope that sf_rotate would refuse or whose axes are
+ * not 2; nothing changes then. On SF_E_OOM or SF_E_HIP the treatment is cleared. The allocation
+ * fails when SF_FAIL_ALLOC_AFTER is 0, to exercise that path. A graph that the caller captured
+ * from the model's calls keeps the treatment it was captured with only until the next set or
+ * clear, which frees what it reads: capture again. */
 int sf_set_qk(sf_model* m, const sf_qk* p);
 
 /* The four projections of every block (QKV, attention output, MLP up and down) in 8 bits:
@@ -433,8 +434,8 @@ int sf_set_qk(sf_model* m, const sf_qk* p);
  * (sf_quantize_rows; LayerNorm + modulate leaves codes itself, from fp32), multiplied as in
  * sf_matmul_i8 with the epilogues of the bf16 projections. Everything else, the
  * cross-attention's projections included, stays as it is. It pays in wide blocks: a velocity of
- * four 1024^2 rows of width 1152 takes 1.65 ms instead of 1.85 (two blocks), of four 512^2 rows of
- * that width 0.77 instead of 0.85 (four blocks), of width 768 1.37 instead of 1.33 (twelve): there
+ * four 1024^2 rows of width 1152 takes 1.70 ms instead of 1.91 (two blocks), of four 512^2 rows of
+ * that width 0.83 instead of 0.89 (four blocks), of width 768 1.47 instead of 1.41 (twelve): there
  * the passes that make codes cost more than the products save. */
 
 /* Enable (nonzero) or disable (0, the default) 8-bit projections in sf_velocity,

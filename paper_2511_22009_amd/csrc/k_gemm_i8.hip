@@ -9,9 +9,12 @@
 // besides its slices. 8192 x 8192 x 8192 takes 440 us (2500 TOP/s), 16384 x 4608 x 1152 102 us
 // (1700), of which the 151 MB of outputs are 23 at the rate of a plain fill. Where a CU has one
 // tile only, the L2 bounds it: 1023 x 777 x 4321 moves 64 x 64 tiles' slices at 75 bytes per ns and
-// CU, 14 us. Outputs that are written while the next tile is under way, by workgroups that stay and
+// CU, 14 us (three sets of operands in turn, rows 4336 bytes apart; 10.4 with 4352, one set 11.2 and
+// 10.0). Outputs that are written while the next tile is under way, by workgroups that stay and
 // fetch across tiles, made a product of K = 128 a fifth faster, but the larger kernel's loop
-// lost as much elsewhere; so did slices of 64, splits of K over wavefronts and more stages.
+// lost as much at 8192 x 8192 x 8192 (other sizes were not measured); slices of 64 and more stages lost,
+// and K split over wavefronts took one row of 3456 x 1152 in 3.5 us instead of 4.3 and lost from 16
+// rows on. K split over workgroups was not tried.
 #include "sf_ops_device.h"
 #include "sf_ops_rules.h"
 

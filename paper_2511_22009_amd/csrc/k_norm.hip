@@ -138,8 +138,8 @@ hipError_t launch_ln(bool out_bf16, const LnArgs& a, hipStream_t s) {
 
 // The same rows as 8-bit codes with a scale per row (sf_ops_device.h), from the fp32 values: no
 // rounding to bf16 in between, and no pass over the rows of its own. One row per wavefront,
-// loads as in ln_mod_kernel. Bandwidth bounds it (5 bytes an element): 4096 rows of 768 5.2 us (3.0
-// TB/s, a third of it launch and drain), 16384 rows of 1152 17.9 us (5.3 TB/s).
+// loads as in ln_mod_kernel. Bandwidth bounds it (5 bytes an element): 4096 rows of 768 5.2 to 5.6
+// us (3.0 TB/s, a third of it launch and drain), 16384 rows of 1152 17.9 to 19 us (5.3 TB/s).
 template <int NV>
 __global__ __launch_bounds__(256) void ln_codes_kernel(LnArgs a, int ldq, float* scale) {
   const int lane = threadIdx.x & 63;

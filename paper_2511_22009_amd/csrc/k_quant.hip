@@ -8,8 +8,9 @@
 namespace sf {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-// Past the L2: 45.4 us otherwise, rows of 1152 13.0 instead of 14.0. (Loads past it as well: 41.8, but
-// 2000 x 20000, read twice, 35.8 instead of 31.1.)
+// Past the L2: 45.4 us otherwise, rows of 1152 13.0 instead of 14.0. (Loads past it as well: 41.8. They
+// are as they are because the kernel of long rows shares them, which reads a row twice and loses, 2000 x
+// 20000 35.8 instead of 31.1; a load of its own for the kernel that reads once was not measured.)
 __device__ __forceinline__ void put_codes(int8_t* q, const uint32_t (&v)[2]) {
   __builtin_nontemporal_store(u32x2{v[0], v[1]}, (u32x2*)q);
 }

@@ -7,9 +7,9 @@
 // lanes hold a head, and its sum of squares is a butterfly over them.
 //
 // Bandwidth bounds it: the 8 x 30 x 52 tokens of a clip with 16 heads of 128 dims (102 MB) take
-// 16 us, 6.3 TB/s; q and k of 16384 tokens with 32 heads of 64 dims (134 MB, adjacent pairs) 23
-// us, 5.8, as halves 29. With 72 dims a head fills 9 of its 16 lanes, and halves move in pieces of
-// 8 bytes: 30 us for 151 MB, 5.0 TB/s; heads of 72 dims next to each other 42. (Groups of 9 lanes,
+// 16 us, 6.4 TB/s; q and k of 16384 tokens with 32 heads of 64 dims (134 MB, adjacent pairs) 22.5
+// us, 6.0, as halves 28. With 72 dims a head fills 9 of its 16 lanes, and halves move in pieces of
+// 8 bytes: 30 us for 151 MB, 5.1 TB/s; heads next to each other in packed rows 43. (Groups of 9 lanes,
 // their sums in thirds through the LDS crossbar, made 4 % there and cost 5 where q and k lie
 // packed; pieces of 16 bytes, eight pairs to a lane, nothing for 128 dims and 4.5 instead of 3.6 us
 // for a single token; 12 pairs to a lane, wavefronts by tokens throughout and angles per wavefront
@@ -141,7 +141,7 @@ constexpr int kMostHeads = 32;  // of a lane's in a run, which has a bit for eac
 // pair's angle of a token each and leave cosine and sine in LDS, under the wavefronts' first loads.
 // A wavefront takes a run of heads of q or of k.
 // E pairs per unit, U units per lane: one unit of four pairs whose elements are adjacent in
-// memory, or two of one pair each (an element at a time: 98 dims 2.4 to 3.1 TB/s, 36 dims 2.3).
+// memory, or two of one pair each (an element at a time: 98 dims 2.4 to 3.2 TB/s, 36 dims 2.3).
 // ADJ: the layout of adjacent pairs. PART: some dims stay as they are.
 // One pass over a workgroup's heads; FAR: over those alone that the first pass leaves, whose squares fp32
 // does not hold. Returns which of the lane's heads it left, a bit each (what memory holds does not
@@ -427,7 +427,7 @@ hipError_t launch_rope(bool is_bf16, bool norm, bool rotate, RopeArgs a, hipStre
   // bytes: q and k of 16384 tokens with 16 heads of 72 dims 30.5 instead of 42.7 us, a clip's 16.2
   // instead of 21. Where a token's heads follow each other instead, and only several of them are whole
   // pieces, a wavefront takes several heads of one token, past the L2 too: q and k of 16384 tokens in
-  // packed rows with 16 heads of 72 dims 42 instead of 47 us, with 28 heads of 40 dims 38 instead of 55
+  // packed rows with 16 heads of 72 dims 43 instead of 47 us, with 28 heads of 40 dims 39 instead of 55
   // (a head of several tokens past the L2, its ends sharing pieces: 52 at 72 dims).
   const int64_t size = is_bf16 ? 2 : 4;
   bool past = true, runs = whole && size * a.dh * slots % 64 == 0;

@@ -55,8 +55,9 @@ def quantize_rows(x, out=None, scale=None, stream=None):
     """8-bit codes of the rows of x [rows, cols] (bfloat16 or float32, cols adjacent) and
     the fp32 scale of each row: (codes, scale) with x = codes * scale[:, None] nearly.
     codes: int8 [rows, cols], its rows a multiple of 16 bytes apart as `matmul_i8` reads
-    them (of 128 from 1024 columns on: products of 4321 columns take 9.4 us then, 11.2 with
-    rows 4336 bytes apart); `out` and `scale` take the results where they are given."""
+    them (of 128 from 1024 columns on: a product of 1023 x 777 x 4321 takes 10.4 us then and
+    13.9 with rows 4336 bytes apart, three sets of operands in turn; 10.0 and 11.2 with
+    one); `out` and `scale` take the results where they are given."""
     if stream is not None:
         return _aside(stream, (x,), _ext.quantize_rows, x, out, scale)
     return _ext.quantize_rows(x, out, scale)
