@@ -197,7 +197,8 @@ def prepare(c, seed):
 def _nearest_f8(q):
     """The e4m3 number nearest to q (64 bits), ties to even: a step is 2^-3 of the binade, 2^-9 at least."""
     e = torch.frexp(q).exponent.clamp_min(-5) - 4
-    return torch.ldexp(torch.round(torch.ldexp(q, -e)), e).float().to(F8)
+    step = ((e + 1023).to(torch.int64) << 52).view(torch.float64)  # 2^e, every bit of it
+    return (torch.round(q / step) * step).float().to(F8)
 
 
 def _to_codes(x, block):
@@ -206,7 +207,7 @@ def _to_codes(x, block):
     M, K = x.shape
     mb, kb = -(-M // block), _blocks(K)
     padded = torch.nn.functional.pad(x, (0, kb * BLOCK - K, 0, mb * block - M)).view(mb, block, kb, BLOCK)
-    scale = padded.abs().amax((1, 3)) / TOP
+    scale = (padded.abs().amax((1, 3)).double() / TOP).float()
     q = padded.double() / torch.where(scale > 0, scale, 1.0).double()[:, None, :, None]
     return _nearest_f8(q).view(mb * block, kb * BLOCK)[:M, :K], scale
 
