@@ -405,6 +405,107 @@ int sf_qk_norm_rotate(const sf_heads* q, const sf_heads* k, const float* q_gain,
                       int rows, int tokens, int dh, const sf_rope* rope, const float* pos, long long pos_row,
                       void* hip_stream);
 
+/* ---- A block's feed-forward half in 8-bit floating point ---------------------------------
+ *
+ * e4m3 codes (sign, 4 bits of exponent, 3 of mantissa; +-448 the largest, no infinity, 0x7f and
+ * 0xff NaN), one scale per block of SF_F8_BLOCK = 128 columns, the last block as long as
+ * what is left: of every single row (a token's activations), or of 128 rows together (weights). A
+ * block's own scale keeps its digits beside channels far larger than it. In the order of use:
+ * sf_residual_norm leaves codes, sf_gated_matmul_f8 reads and leaves them, sf_matmul_f8 reads them and
+ * sf_residual_norm takes its output into the residual and leaves the next block's codes. */
+#define SF_F8_BLOCK 128
+enum { SF_TYPE_F8 = 2 };  /* where a call leaves codes instead of SF_PREC_* values */
+
+/* Codes that a product reads: rows of ld codes, a multiple of 16 (below 2^23) and at least K rounded up to
+ * one, at an address that is one, every row readable to that length (what stands past K is not
+ * used). The scale of row m's block b: scale[m scale_row + b scale_block], of weights scale[(m / 128)
+ * scale_row + b scale_block]; strides in elements, free from 0 on (scale_row below 2^20). */
+typedef struct sf_codes {
+  const unsigned char* codes;
+  long long ld;
+  const float* scale;
+  long long scale_row, scale_block;
+} sf_codes;
+
+/* x to codes: of every block, top = max |x|, scale = top / 448 rounded to fp32, code = the e4m3 number
+ * nearest to x / scale, ties to even (of the exact quotient, at most 448). A block of zeros, or one
+ * whose scale rounds to 0, has codes and scale 0; one that holds a NaN or an infinity has scale
+ * and codes NaN. block_rows: 1 or 128. x: [rows][cols], row length ldx, element type SF_PREC_*; codes:
+ * [rows][cols], row length ldc, a multiple of 16 at an address that is one (the bytes past cols
+ * stay as they are); scale: [ceil(rows / block_rows)][ceil(cols / 128)] with the given strides (1 for
+ * scale_row, so that the scales of adjacent rows are adjacent, is what the products read fastest).
+ * rows 0..2^31 - 1, cols 1..1048576. SF_E_INVAL otherwise. */
+int sf_quantize_f8(const void* x, int type, long long rows, int cols, long long ldx, int block_rows, unsigned char* codes,
+                   long long ldc, float* scale, long long scale_row, long long scale_block, void* hip_stream);
+
+/* out[m][n] = sum_b (sum_{k in b} A[m][k] B[n][k]) sa[m][b] sb[n / 128][b] + bias[n]
+ * a: M rows, a scale per row and block; b: N rows of weights, a scale per 128 rows and block. Sums over
+ * a block on the matrix cores: for fp32 outputs (and outputs that are codes) in fp32; for bf16 eight products of
+ * adjacent k are added to each other first, each cut off below 2^-13 of the largest one's power of two, which is
+ * twice as fast and some 1.5e-5 of a result, and the eights then in fp32. sa sb rounded to fp32 (so beyond its range
+ * it is lost); its product with the block's sum added to the sum over blocks with one rounding to fp32; the
+ * output's type last. bias: fp32 [N] or NULL. out: [M][N], row length ldo >= N, element type out_type
+ * (SF_PREC_*), any alignment of its elements. K 1..1048576, M and N from 0 on. */
+int sf_matmul_f8(const sf_codes* a, const sf_codes* b, const float* bias, int M, int N, int K, void* out, long long ldo,
+                 int out_type, void* hip_stream);
+
+/* The first half of a gated feed-forward in one pass over its rows:
+ *   out[m][n] = act(G[m][n]) U[m][n],  G = A . gate^T + gate_bias, U = A . up^T + up_bias
+ * both as sf_matmul_f8 has them, N rows of weights each, act SF_ACT_SILU (x / (1 + e^-x)) or SF_ACT_GELU_TANH.
+ * out_type SF_PREC_*: values. SF_TYPE_F8: codes as sf_quantize_f8 makes them of the fp32 values, one
+ * scale per row and 128 outputs in out_scale (strides in elements, not 0 over more than one entry);
+ * ldo a multiple of 16 then, at an address that is one. out_scale is not used otherwise. */
+enum { SF_ACT_SILU = 0, SF_ACT_GELU_TANH = 1 };
+int sf_gated_matmul_f8(const sf_codes* a, const sf_codes* gate, const sf_codes* up, const float* gate_bias, const float* up_bias,
+                       int act, int M, int N, int K, void* out, long long ldo, int out_type, float* out_scale,
+                       long long scale_row, long long scale_block, void* hip_stream);
+
+/* A block's output into the residual stream, and the next block's input from it, in one pass over
+ * rows [samples][tokens][dims]:
+ *   u = post(y) post_gain,  h' = residual_scale h + gate u,  a = pre(h') pre_gain (1 + scale) + shift
+ * A norm is SF_NORM_RMS, x / sqrt(mean x^2 + eps), SF_NORM_LAYER, (x - mean) / sqrt(variance + eps)
+ * (biased variance), or SF_NORM_NONE. pre reads h' before its rounding to h's type. Everything in
+ * fp32, one rounding to each output's type; a row whose squares fp32 does not hold is scaled by a power of
+ * two first, so finite rows of every size are normalised.
+ * h, h_out: element type h_type; h_out may be h itself with the same strides. y: y_type. out: out_type (NULL:
+ * h' alone; the fields of a are not read then), SF_TYPE_F8 for codes with a scale per row and block of
+ * 128 dims in out_scale as sf_quantize_f8 makes them (strides of out multiples of 16 then, at an
+ * address that is one). Dims are adjacent; the other strides (in elements) free, those of results not 0 over more
+ * than one entry. gate, scale, shift: fp32, dims adjacent, the given stride from sample to sample (0:
+ * one for all); post_gain, pre_gain: fp32 [dims]; NULL: gate, gains 1, scale, shift 0. eps finite, >= 0;
+ * residual_scale finite; dims 1..16384; samples x tokens below 2^31. Results do not overlap
+ * what is read, but for h_out at h (SF_E_INVAL where the addresses alone tell otherwise). */
+enum { SF_NORM_NONE = 0, SF_NORM_RMS = 1, SF_NORM_LAYER = 2 };
+typedef struct sf_block_rows {
+  int samples, tokens, dims;
+  const void* h;
+  int h_type;
+  long long h_sample, h_token;
+  const void* y;
+  int y_type;
+  long long y_sample, y_token;
+  void* h_out;
+  long long h_out_sample, h_out_token;
+  const float* gate;
+  long long gate_sample;
+  int post;
+  const float* post_gain;
+  float residual_scale;
+  int pre;
+  const float* pre_gain;
+  const float* scale;
+  long long scale_sample;
+  const float* shift;
+  long long shift_sample;
+  float eps;
+  void* out;
+  int out_type;
+  long long out_sample, out_token;
+  float* out_scale;
+  long long out_scale_sample, out_scale_token, out_scale_block;
+} sf_block_rows;
+int sf_residual_norm(const sf_block_rows* rows, void* hip_stream);
+
 /* A network whose self-attention normalises its queries and keys per head and turns them by
  * the token's place, instead of or besides the position table of its embedding (the usual
  * form of rectified-flow transformers for images): between the QKV projection and the

@@ -7,7 +7,8 @@ from .binding import (Buffer, Cond, KernelClass, Model, SFError, Precision, lib_
                       library_symbols)
 
 # the operators on torch tensors; importing the package itself needs no torch
-_OPERATORS = ("Rotary", "matmul_i8", "qk_norm_rotate", "quantize_rows", "rotate")
+_OPERATORS = ("Rotary", "gated_matmul_f8", "matmul_f8", "matmul_i8", "qk_norm_rotate", "quantize_f8", "quantize_rows",
+              "residual_norm", "rotate")
 
 __all__ = ["Buffer", "Cond", "KernelClass", "Model", "SFError", "Precision", "lib_path", "load_library",
            "library_symbols"]

@@ -88,6 +88,25 @@ class _QK(ctypes.Structure):
                 ("rope", ctypes.POINTER(_Rope))]
 
 
+class _Codes(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("ld", ctypes.c_longlong), ("scale", ctypes.c_void_p),
+                ("scale_row", ctypes.c_longlong), ("scale_block", ctypes.c_longlong)]
+
+
+class _BlockRows(ctypes.Structure):
+    _fields_ = [("samples", ctypes.c_int), ("tokens", ctypes.c_int), ("dims", ctypes.c_int),
+                ("h", ctypes.c_void_p), ("h_type", ctypes.c_int), ("h_sample", ctypes.c_longlong), ("h_token", ctypes.c_longlong),
+                ("y", ctypes.c_void_p), ("y_type", ctypes.c_int), ("y_sample", ctypes.c_longlong), ("y_token", ctypes.c_longlong),
+                ("h_out", ctypes.c_void_p), ("h_out_sample", ctypes.c_longlong), ("h_out_token", ctypes.c_longlong),
+                ("gate", ctypes.c_void_p), ("gate_sample", ctypes.c_longlong), ("post", ctypes.c_int), ("post_gain", ctypes.c_void_p),
+                ("residual_scale", ctypes.c_float), ("pre", ctypes.c_int), ("pre_gain", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p), ("scale_sample", ctypes.c_longlong), ("shift", ctypes.c_void_p),
+                ("shift_sample", ctypes.c_longlong), ("eps", ctypes.c_float),
+                ("out", ctypes.c_void_p), ("out_type", ctypes.c_int), ("out_sample", ctypes.c_longlong), ("out_token", ctypes.c_longlong),
+                ("out_scale", ctypes.c_void_p), ("out_scale_sample", ctypes.c_longlong), ("out_scale_token", ctypes.c_longlong),
+                ("out_scale_block", ctypes.c_longlong)]
+
+
 _LIB = None
 _P = ctypes.c_void_p
 _I = ctypes.c_int
@@ -122,6 +141,10 @@ _SIGS = {
     "sf_matmul_i8": (_I, [_P, _J, _P, _P, _J, _P, _P, _I, _I, _I, _P, _J, _I, _P]),
     "sf_rotate": (_I, [_P, _I, _I, _I, _I, _P, _P, _J, _I, _P]),
     "sf_qk_norm_rotate": (_I, [_P, _P, _P, _P, ctypes.c_float, _I, _I, _I, _I, _P, _P, _J, _P]),
+    "sf_quantize_f8": (_I, [_P, _I, _J, _I, _J, _I, _P, _J, _P, _J, _J, _P]),
+    "sf_matmul_f8": (_I, [_P, _P, _P, _I, _I, _I, _P, _J, _I, _P]),
+    "sf_gated_matmul_f8": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _I, _P, _J, _I, _P, _J, _J, _P]),
+    "sf_residual_norm": (_I, [_P, _P]),
 }
 
 

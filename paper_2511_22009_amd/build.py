@@ -18,7 +18,7 @@ INCLUDE = os.path.join(ROOT, "include")
 OUT = os.path.join(HERE, "libstreamflow.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["k_cond.hip", "k_norm.hip", "k_gemm.hip", "k_attn.hip", "k_euler.hip", "k_quant.hip",
-           "k_gemm_i8.hip", "k_rope.hip", "streamflow.cpp", "operators.cpp"]
+           "k_gemm_i8.hip", "k_rope.hip", "k_quant_f8.hip", "k_gemm_f8.hip", "k_residual_norm.hip", "streamflow.cpp", "operators.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 CXX = os.environ.get("CXX", "g++")
 ARCH = "gfx950"
@@ -28,8 +28,9 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
          "-I", INCLUDE, "-I", CSRC]
 # Per-source flags. Attention runs VALU softmax work on the MFMA results (scores and
 # the running output), so their accumulators are kept in architectural VGPRs instead
-# of being copied to and from accumulation registers every key block.
-SOURCE_FLAGS = {"k_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+# of being copied to and from accumulation registers every key block; the products of
+# e4m3 codes take every block's sums up in the same way.
+SOURCE_FLAGS = {s: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for s in ("k_attn.hip", "k_gemm_f8.hip")}
 
 
 def _compile(src):

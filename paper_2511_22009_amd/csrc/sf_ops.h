@@ -43,6 +43,65 @@ enum I8Kind {
 };
 hipError_t launch_gemm_i8(I8Kind kind, const GemmI8Args& a, hipStream_t s);
 
+// ---- rows and weights to e4m3 codes with a scale per block ---------------------------
+constexpr int kF8Block = 128;  // columns of a block (and rows, of a weight's)
+struct QuantF8Args {
+  const void* x;        // [M][K], row length ldx, bf16 or fp32
+  int64_t ldx;
+  int M, K;
+  uint8_t* q;           // [M][K], row length ldq (a multiple of 16, 16-byte aligned)
+  int64_t ldq;
+  float* scale;         // [blocks of rows][blocks of columns]
+  int64_t s_row, s_block;
+};
+hipError_t launch_quantize_f8(bool x_bf16, bool square, const QuantF8Args& a, hipStream_t s);
+
+// ---- products of e4m3 codes ----------------------------------------------------------
+// Codes [rows][K], row length ld (a multiple of 16, 16-byte aligned), and the scales of their
+// blocks: of one row for the first operand, of 128 rows for weights.
+struct F8Codes {
+  const uint8_t* q;
+  int ld;
+  const float* scale;
+  int64_t s_row, s_block;
+};
+struct GemmF8Args {
+  F8Codes a, b, up;     // up: of gated products only, b is the gate then
+  int M, N, K;          // N: outputs, columns of b
+  const float* bias;    // [N] or nullptr
+  const float* up_bias;
+  void* out;            // [M][N], row length ldo
+  int64_t ldo;
+  float* out_scale;     // of outputs that are codes: [M][blocks of N]
+  int64_t os_row, os_block;
+};
+enum F8Out { F8_BF16 = 0, F8_F32, F8_CODES };             // F8_CODES of gated products only
+enum F8Act { F8_NONE = 0, F8_SILU, F8_GELU };             // F8_NONE: out = a . b^T + bias
+hipError_t launch_gemm_f8(F8Out kind, F8Act act, const GemmF8Args& a, hipStream_t s);
+
+// ---- a block's output into the residual, and the next block's input ------------------
+enum NormKind { NORM_NONE = 0, NORM_RMS, NORM_LAYER };
+struct ResidualNormArgs {
+  const char* h;        // [samples][tokens][D]; strides in elements, also below
+  const char* y;
+  char* h_out;
+  char* out;            // nullptr: none
+  int64_t h_sample, h_token, y_sample, y_token, ho_sample, ho_token, out_sample, out_token;
+  float* out_scale;     // of codes: a scale per row and block of 128
+  int64_t os_sample, os_token, os_block;
+  const float* gate;    // [samples][D] or nullptr, as shift and scale
+  const float* scale;
+  const float* shift;
+  int64_t gate_sample, scale_sample, shift_sample;
+  const float* post_gain;  // [D] or nullptr
+  const float* pre_gain;
+  int post, pre;        // NormKind
+  float r, eps;
+  int samples, tokens, D;
+};
+enum NormOut { NORM_BF16 = 0, NORM_F32, NORM_CODES };
+hipError_t launch_residual_norm(bool h_bf16, bool y_bf16, NormOut out, const ResidualNormArgs& a, hipStream_t s);
+
 // ---- per-head norm and rotation of heads ---------------------------------------------
 constexpr int kRopeAxes = 4;  // equals SF_ROPE_AXES
 struct RopeHeads {

@@ -65,4 +65,16 @@ inline I8Tile choose_gemm_i8_tile(long M, long N, long K, bool heavy, bool resid
   return best;
 }
 
+// Tiles of the products of e4m3 codes. N counts columns of the weights (gated: both projections).
+// Outputs that are codes need a tile that holds whole blocks of 128 outputs.
+enum F8Tile { kF8Few, kF8Deep64, kF8Tile128, kF8Tile128x256, kF8Tile256x256 };
+inline F8Tile choose_gemm_f8_tile(long M, long N, long K, bool codes, bool exact) {
+  (void)K;
+  if (codes) return kF8Tile128x256;
+  if (M <= 64) return kF8Few;
+  const int64_t large = (((int64_t)M + 255) / 256) * (((int64_t)N + 255) / 256);
+  const int64_t mid = (((int64_t)M + 127) / 128) * (((int64_t)N + 127) / 128);
+  return large >= 128 && !exact ? kF8Tile256x256 : mid >= 128 ? kF8Tile128 : kF8Deep64;
+}
+
 }  // namespace sf

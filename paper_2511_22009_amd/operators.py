@@ -1,6 +1,7 @@
 """Operators on torch tensors that need no model: 8-bit row quantisation and products,
-rotary positions with several axes, and the norm of queries and keys with the rotation
-(the calls without a model in include/streamflow.h, which states their formulas).
+rotary positions with several axes, the norm of queries and keys with the rotation, and a
+block's feed-forward half in 8-bit floating point: codes with a scale per block, their
+products, gated projections, and the norms around a block with its residual (the calls without a model in include/streamflow.h, which states their formulas).
 
 As in the rest of the binding, tensors give device memory and streams, and shapes, types
 and devices are checked before a call: TypeError for what is no fitting tensor, ValueError
@@ -24,6 +25,9 @@ except ImportError as e:
                       "(or __graft_entry__.build())") from e
 
 _TYPES = {torch.bfloat16: 0, torch.float32: 1}
+_TYPES_OR_CODES = {**_TYPES, torch.float8_e4m3fn: 2}
+_ACTS = {"silu": 0, "gelu_tanh": 1}
+_NORMS = {None: 0, "none": 0, "rms": 1, "layer": 2}
 _LAYOUTS = {"adjacent": 0, "halves": 1, "axis_halves": 2}
 
 
@@ -33,7 +37,8 @@ def _raw_stream(index):
 
 _ext.bind(_check, getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream),
           *(ctypes.cast(getattr(load_library(), "sf_" + n), ctypes.c_void_p).value
-            for n in ("quantize_rows", "matmul_i8", "rotate", "qk_norm_rotate")))
+            for n in ("quantize_rows", "matmul_i8", "rotate", "qk_norm_rotate", "quantize_f8", "matmul_f8", "gated_matmul_f8",
+                      "residual_norm")))
 
 
 def _aside(stream, tensors, call, *args):
@@ -43,8 +48,12 @@ def _aside(stream, tensors, call, *args):
         raise ValueError(f"stream of {stream.device}, tensors on {first.device}")
     with torch.cuda.stream(stream):
         result = call(*args)
-    for t in (*tensors, *(result if isinstance(result, tuple) else (result,))):
-        if t is not None:
+    pending = [*tensors, result]
+    while pending:
+        t = pending.pop()
+        if isinstance(t, tuple):
+            pending += t
+        elif t is not None:
             t.record_stream(stream)
     return result
 
@@ -123,3 +132,72 @@ def qk_norm_rotate(q, k, q_gain=None, k_gain=None, positions=None, rotary=None, 
         return _aside(stream, (q, k, q_gain, k_gain, positions), _ext.qk_norm_rotate, q, k, q_gain, k_gain, positions, address, eps,
                       q_out, k_out)
     return _ext.qk_norm_rotate(q, k, q_gain, k_gain, positions, address, eps, q_out, k_out)
+
+
+# ----------------------------------------- a block's feed-forward half in 8-bit floating point
+
+def _of(table, key, what):
+    try:
+        return table[key]
+    except (KeyError, TypeError):
+        names = ", ".join(str(k) for k in table)
+        raise (TypeError if what == "dtype" else ValueError)(f"{what}: expected one of {names}, got {key!r}") from None
+
+
+def quantize_f8(x, block_rows=1, out=None, scale=None, stream=None):
+    """e4m3 codes of x [rows, cols] (bfloat16 or float32, cols adjacent) with an fp32 scale
+    for each block of 128 columns, of every row (block_rows=1: activations) or of 128 rows
+    together (128: weights): (codes, scale), codes float8_e4m3fn [rows, cols], scale
+    [rows, blocks] or [blocks of rows, blocks]; a block's value is its code times its scale
+    nearly. Rows of codes start at multiples of 16 bytes (of 128 from 1024 columns on), and
+    the scales of adjacent rows are adjacent, as the products read them fastest; `out` and
+    `scale` take the results where they are given, the scales with any strides."""
+    if stream is not None:
+        return _aside(stream, (x,), _ext.quantize_f8, x, block_rows, out, scale)
+    return _ext.quantize_f8(x, block_rows, out, scale)
+
+
+def matmul_f8(a, a_scale, b, b_scale, bias=None, dtype=torch.bfloat16, out=None, stream=None):
+    """a [M, K] (codes of `quantize_f8`, a scale per row and block) times b [N, K] transposed
+    (a scale per 128 rows and block), plus bias [N] (fp32): [M, N] in `dtype` (bfloat16 or
+    float32), or in `out`, whose columns are adjacent and whose type then holds."""
+    kind = _of(_TYPES, dtype, "dtype")
+    if stream is not None:
+        return _aside(stream, (a, a_scale, b, b_scale, bias), _ext.matmul_f8, a, a_scale, b, b_scale, bias, kind, out)
+    return _ext.matmul_f8(a, a_scale, b, b_scale, bias, kind, out)
+
+
+def gated_matmul_f8(a, a_scale, gate, gate_scale, up, up_scale, gate_bias=None, up_bias=None, activation="silu",
+                    dtype=torch.bfloat16, out=None, out_scale=None, stream=None):
+    """act(a gate^T + gate_bias) * (a up^T + up_bias), the first half of a gated feed-forward,
+    operands as in `matmul_f8`; activation "silu" or "gelu_tanh". [M, N] in `dtype`
+    (bfloat16 or float32) or, for float8_e4m3fn, (codes, scale) as `quantize_f8` makes them
+    of the fp32 values, for the projection that follows. `out` and `out_scale` take the
+    results where they are given; out's type then holds."""
+    kind, act = _of(_TYPES_OR_CODES, dtype, "dtype"), _of(_ACTS, activation, "activation")
+    if stream is not None:
+        return _aside(stream, (a, a_scale, gate, gate_scale, up, up_scale, gate_bias, up_bias), _ext.gated_matmul_f8, a, a_scale, gate,
+                      gate_scale, up, up_scale, gate_bias, up_bias, act, kind, out, out_scale)
+    return _ext.gated_matmul_f8(a, a_scale, gate, gate_scale, up, up_scale, gate_bias, up_bias, act, kind, out, out_scale)
+
+
+def residual_norm(h, y, gate=None, post=None, post_gain=None, residual_scale=1.0, pre=None, pre_gain=None, scale=None, shift=None,
+                  eps=1e-6, dtype=torch.bfloat16, h_out=None, out=None, out_scale=None, stream=None):
+    """A block's output y into the residual stream h, and the next block's input from it:
+
+        h' = residual_scale * h + gate * post(y) * post_gain
+        a  = pre(h') * pre_gain * (1 + scale) + shift
+
+    h, y: [samples, tokens, dims] or [tokens, dims] (bfloat16 or float32, dims adjacent, other
+    strides free). post, pre: "rms", "layer" or "none"; post None is none, pre None leaves a
+    out. gate, scale, shift: fp32 [samples, dims], or [dims] for all; gains fp32 [dims]; None:
+    not there. Returns (h', a), h' of h's type, a in `dtype` (bfloat16 or float32) or, for
+    float8_e4m3fn, as (codes, scale) like `quantize_f8`'s, or None. `h_out` (which may be
+    h), `out` and `out_scale` take the results where they are given."""
+    kind = _of(_TYPES_OR_CODES, dtype, "dtype")
+    after, before = _of(_NORMS, post, "post"), -1 if pre is None else _of(_NORMS, pre, "pre")
+    if stream is not None:
+        return _aside(stream, (h, y, gate, post_gain, pre_gain, scale, shift), _ext.residual_norm, h, y, gate, after, post_gain,
+                      residual_scale, before, pre_gain, scale, shift, eps, kind, h_out, out, out_scale)
+    return _ext.residual_norm(h, y, gate, after, post_gain, residual_scale, before, pre_gain, scale, shift, eps, kind, h_out, out,
+                              out_scale)
