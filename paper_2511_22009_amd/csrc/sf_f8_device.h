@@ -22,22 +22,19 @@ __device__ __forceinline__ uint32_t pack_f8(float a, float b, float c, float d) 
 // A block's scale, top / 448, and what takes its values to codes.
 struct BlockF8 {
   float scale;  // NaN for a block that is not finite
-  float inv;    // 1 / scale; 0 where fp32 does not hold it to full precision, or scale is 0 or NaN
+  float inv;    // 1 / scale, NaN too, 0 for a scale of 0, and -1 for one so small that differences are lost
 };
 __device__ __forceinline__ BlockF8 block_f8(uint32_t top_bits) {
-  const float s = __uint_as_float(top_bits) / kF8Top;
   BlockF8 b;
-  b.scale = top_bits < 0x7f800000u ? s : __uint_as_float(0x7fc00000u);
-  b.inv = s >= 0x1p-126f && top_bits < 0x7f800000u ? 1.0f / s : 0.0f;
+  b.scale = top_bits < 0x7f800000u ? __uint_as_float(top_bits) / kF8Top : __uint_as_float(0x7fc00000u);
+  b.inv = b.scale == 0.0f ? 0.0f : b.scale < 0x1p-100f ? -1.0f : 1.0f / b.scale;
   return b;
 }
 
-// The code of x in a block of scale s: the exact quotient's. The fp64 quotient of two fp32 numbers
+// The code of x in a block of scale s > 0: the exact quotient's. The fp64 quotient of two fp32 numbers
 // lies on the exact one's side of every tie: it is a tie only where that is one, since the quotient of
 // two 24-bit significands that is not a number of five bits differs from one by over 2^-30 of itself.
 __device__ __forceinline__ uint32_t code_f8_exact(float x, float s) {
-  if (s != s) return 0x7f;
-  if (s == 0.0f) return 0;
   const uint32_t sign = __float_as_uint(x) >> 31 << 7;
   const double q = fmin(fabs((double)x) / (double)s, 448.0);
   if (q < 0x1p-6) return sign | (uint32_t)(int)rint(q * 512.0);
@@ -46,25 +43,43 @@ __device__ __forceinline__ uint32_t code_f8_exact(float x, float s) {
   return sign | ((uint32_t)(r >> 49) - (1016u << 3));
 }
 
+// Which of two adjacent codes, byte E of lo and of hi, is x's in a block of scale s >= 2^-100: the sign of
+// |x| - tie s is the exact one's, as one fma rounds it, and where that is 0 the even code has it.
+template <int E>
+__device__ __forceinline__ uint32_t nearer_f8(uint32_t lo, uint32_t hi, float x, float s) {
+  const float tie = 0.5f * (fabsf(__builtin_amdgcn_cvt_f32_fp8((int)lo, E)) + fabsf(__builtin_amdgcn_cvt_f32_fp8((int)hi, E)));
+  const float over = __builtin_fmaf(-tie, s, fabsf(x));
+  const uint32_t l = lo & (0xffu << (8 * E)), h = hi & (0xffu << (8 * E));
+  return over > 0.0f || (over == 0.0f && !(h >> (8 * E) & 1)) ? h : l;
+}
+
 // Codes of N values of a block. x inv (1 -+ 2^-22) lie on both sides of the exact quotient (inv and the
 // two products add less than 2^-22 of it), and rounding is monotone, so where both give the same code
-// it is the quotient's. Elsewhere, one value in some 2^16, the exact quotient decides.
+// it is the quotient's. Elsewhere, one value in some 2^17 and one in 16 where the scale is a power of
+// two and the values are bf16, the exact quotient decides. (In fp64 it took 16384 x 1152 bf16
+// from 13 to 19 us.)
 template <int N>
 __device__ __forceinline__ void codes_f8(const float (&x)[N], const BlockF8& b, uint32_t (&out)[N / 4]) {
-  const float lo = b.inv * (1.0f - 0x1p-22f), hi = b.inv * (1.0f + 0x1p-22f);
-  uint32_t differ = 0;
+  const float less = b.inv * (1.0f - 0x1p-22f), more = b.inv * (1.0f + 0x1p-22f);
+  uint32_t hi[N / 4], differ = 0;
 #pragma unroll
   for (int i = 0; i < N / 4; ++i) {
-    out[i] = pack_f8(x[4 * i] * lo, x[4 * i + 1] * lo, x[4 * i + 2] * lo, x[4 * i + 3] * lo);
-    differ |= out[i] ^ pack_f8(x[4 * i] * hi, x[4 * i + 1] * hi, x[4 * i + 2] * hi, x[4 * i + 3] * hi);
+    out[i] = pack_f8(x[4 * i] * less, x[4 * i + 1] * less, x[4 * i + 2] * less, x[4 * i + 3] * less);
+    hi[i] = pack_f8(x[4 * i] * more, x[4 * i + 1] * more, x[4 * i + 2] * more, x[4 * i + 3] * more);
+    differ |= out[i] ^ hi[i];
   }
-  if (differ != 0 || b.inv == 0.0f) {
+  if (b.inv < 0.0f) {
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
       out[i] = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) out[i] |= code_f8_exact(x[4 * i + e], b.scale) << (8 * e);
     }
+  } else if (differ != 0) {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i)
+      out[i] = nearer_f8<0>(out[i], hi[i], x[4 * i], b.scale) | nearer_f8<1>(out[i], hi[i], x[4 * i + 1], b.scale) |
+               nearer_f8<2>(out[i], hi[i], x[4 * i + 2], b.scale) | nearer_f8<3>(out[i], hi[i], x[4 * i + 3], b.scale);
   }
 }
 
