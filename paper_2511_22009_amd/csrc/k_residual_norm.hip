@@ -3,6 +3,8 @@
 // each norm the division by the root mean square, or that of what the mean leaves, or none. Bandwidth
 // bounds it: h and y are read once, h' and a written once, and a row stays in registers between its
 // two norms.
+#include <algorithm>
+
 #include "sf_f8_device.h"
 
 namespace sf {
@@ -13,7 +15,7 @@ template <> struct Out4<float> {
   typedef float V __attribute__((ext_vector_type(4), aligned(4)));
   __device__ static void run(float* p, const float (&x)[4], int left) {
     if (left >= 4) {
-      *(V*)p = V{x[0], x[1], x[2], x[3]};
+      __builtin_nontemporal_store(V{x[0], x[1], x[2], x[3]}, (V*)p);
     } else {
       for (int e = 0; e < 4; ++e)
         if (e < left) p[e] = x[e];
@@ -24,7 +26,7 @@ template <> struct Out4<bf16> {
   typedef uint32_t V __attribute__((ext_vector_type(2), aligned(2)));
   __device__ static void run(bf16* p, const float (&x)[4], int left) {
     if (left >= 4) {
-      *(V*)p = V{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+      __builtin_nontemporal_store(V{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])}, (V*)p);
     } else {
       for (int e = 0; e < 4; ++e)
         if (e < left) p[e] = (bf16)x[e];
@@ -112,129 +114,194 @@ __device__ __forceinline__ void normalise(float (&x)[NV][4], int kind, const Res
   }
 }
 
-// WAVES wavefronts per row, NV pieces of four per lane (D <= 256 WAVES NV).
-template <typename TH, typename TY, NormOut OUT, int NV, int WAVES>
-__global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNormArgs a, FastDiv div_tokens, int64_t row0, int rows) {
-  __shared__ float lds[4];
-  constexpr int STEP = WAVES * 256;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int part = blockIdx.x * (4 / WAVES) + wave / WAVES;
-  if (part >= rows) return;  // whole wavefronts, and with several to a row whole workgroups
-  const uint32_t row = (uint32_t)(row0 + part);
-  const uint32_t sample = fdiv(row, div_tokens), token = row - sample * div_tokens.d;
-  const int first = 4 * ((wave % WAVES) * 64 + (threadIdx.x & 63));
-  const TH* const h = (const TH*)a.h + sample * a.h_sample + token * a.h_token;
-  const TY* const y = (const TY*)a.y + sample * a.y_sample + token * a.y_token;
-  Piece<TH, 4> hp[NV];
-  Piece<TY, 4> yp[NV];
+// A piece of four of a row from column c on. WHOLE (D is a multiple of four): a lane past the row reads its last piece,
+// unconditionally, since a load under a lane's condition is waited for at once; what is past D is cleared
+// in use. Otherwise it is read element by element where D ends in it, and is 0 past D.
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void load_piece(Piece<T, 4>& p, const T* row, int c, int D) {
+  if constexpr (WHOLE)
+    p.load(row + min(c, D - 4), 4);
+  else
+    p.load(row + c, D - c);
+}
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void take_piece(float (&x)[4], const Piece<T, 4>& p, int c, int D) {
+  p.unpack(x);
+  if constexpr (WHOLE) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = c < D ? x[e] : 0.0f;
+  }
+}
+
+// A vector's pieces of a lane, `other` where there is none.
+template <bool WHOLE, int NV, int STEP>
+__device__ __forceinline__ void load_vector(float (&v)[NV][4], const float* p, int first, int D, float other) {
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = first + i * STEP;
-    yp[i].load(y + c, a.D - c);
-    hp[i].load(h + c, a.D - c);
-  }
-  float x[NV][4];
+    if (p) {
+      Piece<float, 4> q;
+      load_piece<WHOLE>(q, p, c, D);
+      q.unpack(v[i]);
+    } else {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) yp[i].unpack(x[i]);
-  if (a.post != NORM_NONE) normalise<NV, WAVES>(x, a.post, a, first, lds);
+      for (int e = 0; e < 4; ++e) v[i][e] = other;
+    }
+  }
+}
+
+constexpr int threads_of(int waves) { return waves > 4 ? waves * 64 : 256; }
+
+// WAVES wavefronts per row, NV pieces of four per lane (D <= 256 WAVES NV). A workgroup takes `span` rows of one
+// sample in turn, fetches the next before it works on one, and keeps the sample's vectors, folded into
+// three, in registers, fetched with its first row.
+template <typename TH, typename TY, NormOut OUT, int NV, int WAVES, bool WHOLE>
+__global__ __launch_bounds__(threads_of(WAVES)) void residual_norm_kernel(ResidualNormArgs a, FastDiv div_spans, int span) {
+  __shared__ float lds[WAVES];
+  constexpr int STEP = WAVES * 256, ROWS = threads_of(WAVES) / 64 / WAVES;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t sample = fdiv(blockIdx.x, div_spans);
+  const int start = (int)(blockIdx.x - sample * div_spans.d) * span, end = min(start + span, a.tokens);
+  int token = start + wave / WAVES;
+  if (token >= end) return;  // whole wavefronts, and with several to a row whole workgroups
+  const int first = 4 * ((wave % WAVES) * 64 + (threadIdx.x & 63));
+  const TH* const h = (const TH*)a.h + sample * a.h_sample;
+  const TY* const y = (const TY*)a.y + sample * a.y_sample;
+  Piece<TH, 4> hp[NV];
+  Piece<TY, 4> yp[NV];
+  auto fetch_y = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) load_piece<WHOLE>(yp[i], y + (int64_t)t * a.y_token, first + i * STEP, a.D);
+  };
+  auto fetch_h = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) load_piece<WHOLE>(hp[i], h + (int64_t)t * a.h_token, first + i * STEP, a.D);
+  };
+  // gate post_gain, pre_gain (1 + scale) and shift
   const float* const gate = a.gate ? a.gate + sample * a.gate_sample : nullptr;
-  TH* const h_out = (TH*)a.h_out + sample * a.ho_sample + token * a.ho_token;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = first + i * STEP, left = a.D - c;
-    Piece<float, 4> p;
-    float v[4];
-    if (a.post_gain) {
-      p.load(a.post_gain + c, left);
-      p.unpack(v);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[i][e] *= v[e];
-    }
-    if (gate) {
-      p.load(gate + c, left);
-      p.unpack(v);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[i][e] *= v[e];
-    }
-    float hv[4];
-    hp[i].unpack(hv);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[i][e] = __builtin_fmaf(a.r, hv[e], x[i][e]);
-    Out4<TH>::run(h_out + c, x[i], left);
-  }
-  if (!a.out) return;
-  if (a.pre != NORM_NONE) normalise<NV, WAVES>(x, a.pre, a, first, lds);
   const float* const scale = a.scale ? a.scale + sample * a.scale_sample : nullptr;
   const float* const shift = a.shift ? a.shift + sample * a.shift_sample : nullptr;
+  float vg[NV][4], vs[NV][4], vb[NV][4];
+  fetch_y(token);
+  fetch_h(token);
+  {
+    float w[NV][4];
+    load_vector<WHOLE, NV, STEP>(vg, gate, first, a.D, 1.0f);
+    load_vector<WHOLE, NV, STEP>(w, a.post_gain, first, a.D, 1.0f);
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = first + i * STEP, left = a.D - c;
-    Piece<float, 4> p;
-    float v[4];
-    if (a.pre_gain) {
-      p.load(a.pre_gain + c, left);
-      p.unpack(v);
+    for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[i][e] *= v[e];
+      for (int e = 0; e < 4; ++e) vg[i][e] *= w[i][e];
+    if (a.out) {
+      load_vector<WHOLE, NV, STEP>(vs, scale, first, a.D, 0.0f);
+      load_vector<WHOLE, NV, STEP>(w, a.pre_gain, first, a.D, 1.0f);
+      load_vector<WHOLE, NV, STEP>(vb, shift, first, a.D, 0.0f);
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vs[i][e] = w[i][e] * (1.0f + vs[i][e]);
     }
-    if (scale) {
-      p.load(scale + c, left);
-      p.unpack(v);
+  }
+  for (;;) {
+    float x[NV][4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[i][e] = __builtin_fmaf(x[i][e], v[e], x[i][e]);
+    for (int i = 0; i < NV; ++i) take_piece<WHOLE>(x[i], yp[i], first + i * STEP, a.D);
+    const int next = token + ROWS, ahead = min(next, end - 1);
+    fetch_y(ahead);
+    if (a.post != NORM_NONE) normalise<NV, WAVES>(x, a.post, a, first, lds);
+    TH* const h_out = (TH*)a.h_out + sample * a.ho_sample + (int64_t)token * a.ho_token + first;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      float hv[4];
+      take_piece<WHOLE>(hv, hp[i], first + i * STEP, a.D);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[i][e] = __builtin_fmaf(a.r, hv[e], x[i][e] * vg[i][e]);
     }
-    if (shift) {
-      p.load(shift + c, left);
-      p.unpack(v);
+    // before this row's h' leaves: over h itself, the last row is read again
+    if (next < end) fetch_h(next);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[i][e] += v[e];
-    }
-    const int64_t at = sample * a.out_sample + token * a.out_token + c;
-    if constexpr (OUT == NORM_CODES) {
-      // 32 lanes hold a block
-      uint32_t top = 0;
+    for (int i = 0; i < NV; ++i) Out4<TH>::run(h_out + i * STEP, x[i], a.D - first - i * STEP);
+    if (a.out) {
+      if (a.pre != NORM_NONE) normalise<NV, WAVES>(x, a.pre, a, first, lds);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) top = max(top, e < left ? abs_bits(x[i][e]) : 0u);
-      const BlockF8 b = block_f8(max_of_32(top));
-      uint32_t q[1];
-      codes_f8(x[i], b, q);
-      uint8_t* const to = (uint8_t*)a.out + at;
-      if (left >= 4) {
-        *(uint32_t*)to = q[0];
-      } else {
-        for (int e = 0; e < 4; ++e)
-          if (e < left) to[e] = (uint8_t)(q[0] >> (8 * e));
+      for (int i = 0; i < NV; ++i) {
+        const int c = first + i * STEP, left = a.D - c;
+        const int64_t at = sample * a.out_sample + (int64_t)token * a.out_token + c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i][e] = __builtin_fmaf(x[i][e], vs[i][e], vb[i][e]);
+        if constexpr (OUT == NORM_CODES) {
+          // 32 lanes hold a block
+          uint32_t top = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = max(top, e < left ? abs_bits(x[i][e]) : 0u);
+          const BlockF8 b = block_f8(max_of_32(top));
+          uint32_t q[1];
+          codes_f8(x[i], b, q);
+          uint8_t* const to = (uint8_t*)a.out + at;
+          if (left >= 4) {
+            __builtin_nontemporal_store(q[0], (uint32_t*)to);
+          } else {
+            for (int e = 0; e < 4; ++e)
+              if (e < left) to[e] = (uint8_t)(q[0] >> (8 * e));
+          }
+          if ((threadIdx.x & 31) == 0 && left > 0)
+            a.out_scale[sample * a.os_sample + (int64_t)token * a.os_token + (int64_t)(c / kF8Block) * a.os_block] = b.scale;
+        } else if constexpr (OUT == NORM_F32) {
+          Out4<float>::run((float*)a.out + at, x[i], left);
+        } else {
+          Out4<bf16>::run((bf16*)a.out + at, x[i], left);
+        }
       }
-      if ((threadIdx.x & 31) == 0 && left > 0)
-        a.out_scale[sample * a.os_sample + token * a.os_token + (int64_t)(c / kF8Block) * a.os_block] = b.scale;
-    } else if constexpr (OUT == NORM_F32) {
-      Out4<float>::run((float*)a.out + at, x[i], left);
-    } else {
-      Out4<bf16>::run((bf16*)a.out + at, x[i], left);
     }
+    token = next;
+    if (token >= end) break;
   }
 }
 
-template <typename TH, typename TY, NormOut OUT, int NV, int WAVES>
-static void launch_rows(const ResidualNormArgs& a, hipStream_t s) {
-  const FastDiv div = make_fastdiv((uint32_t)a.tokens);
-  constexpr int64_t kMost = 1 << 23;  // a grid holds less than 2^32 threads
+template <typename TH, typename TY, NormOut OUT, int NV, int WAVES, bool WHOLE>
+static void launch_rows(ResidualNormArgs a, hipStream_t s) {
+  constexpr int ROWS = threads_of(WAVES) / 64 / WAVES;
+  // four workgroups to a CU, each as many rows of its sample as that takes
   const int64_t rows = (int64_t)a.samples * a.tokens;
-  for (int64_t r = 0; r < rows; r += kMost) {
-    const int n = (int)(rows - r < kMost ? rows - r : kMost);
-    launch(residual_norm_kernel<TH, TY, OUT, NV, WAVES>, dim3((uint32_t)((n + 4 / WAVES - 1) / (4 / WAVES))), dim3(256), 0, s, a, div, r, n);
+  const int turns = (int)std::min<int64_t>((rows + 1024 * ROWS - 1) / (1024 * ROWS), (a.tokens + ROWS - 1) / ROWS);
+  const int span = turns * ROWS;
+  const uint32_t spans = (uint32_t)((a.tokens + (int64_t)span - 1) / span);
+  const FastDiv div = make_fastdiv(spans);
+  const int most = std::max((int)((1 << 21) / spans), 1);  // a grid holds less than 2^32 threads
+  const int samples = a.samples;
+  for (int from = 0; from < samples; from += most) {
+    launch(residual_norm_kernel<TH, TY, OUT, NV, WAVES, WHOLE>, dim3((uint32_t)std::min(most, samples - from) * spans), dim3(threads_of(WAVES)), 0, s, a, div, span);
+    a.h += (int64_t)most * a.h_sample * (int64_t)sizeof(TH);
+    a.y += (int64_t)most * a.y_sample * (int64_t)sizeof(TY);
+    a.h_out += (int64_t)most * a.ho_sample * (int64_t)sizeof(TH);
+    if (a.out) a.out += (int64_t)most * a.out_sample * (OUT == NORM_CODES ? 1 : OUT == NORM_F32 ? 4 : 2);
+    if (a.out_scale) a.out_scale += (int64_t)most * a.os_sample;
+    if (a.gate) a.gate += (int64_t)most * a.gate_sample;
+    if (a.scale) a.scale += (int64_t)most * a.scale_sample;
+    if (a.shift) a.shift += (int64_t)most * a.shift_sample;
   }
 }
 
+// A wavefront per row where there are many, else a workgroup, whose lanes each wait for less.
 template <typename TH, typename TY, NormOut OUT>
 static hipError_t launch_t(const ResidualNormArgs& a, hipStream_t s) {
-  if (a.D <= 256) launch_rows<TH, TY, OUT, 1, 1>(a, s);
-  else if (a.D <= 768) launch_rows<TH, TY, OUT, 3, 1>(a, s);
-  else if (a.D <= 1280) launch_rows<TH, TY, OUT, 5, 1>(a, s);
-  else if (a.D <= 2048) launch_rows<TH, TY, OUT, 8, 1>(a, s);
-  else if (a.D <= 4096) launch_rows<TH, TY, OUT, 4, 4>(a, s);
-  else if (a.D <= 8192) launch_rows<TH, TY, OUT, 8, 4>(a, s);
-  else launch_rows<TH, TY, OUT, 16, 4>(a, s);
+  const bool many = (int64_t)a.samples * a.tokens >= 2048;
+  if (a.D % 4 == 0) {
+    if (a.D <= 256) launch_rows<TH, TY, OUT, 1, 1, true>(a, s);
+    else if (a.D <= 768 && many) launch_rows<TH, TY, OUT, 3, 1, true>(a, s);
+    else if (a.D <= 1280 && many) launch_rows<TH, TY, OUT, 5, 1, true>(a, s);
+    else if (a.D <= 1024) launch_rows<TH, TY, OUT, 1, 4, true>(a, s);
+    else if (a.D <= 2048) launch_rows<TH, TY, OUT, 2, 4, true>(a, s);
+    else if (a.D <= 4096) launch_rows<TH, TY, OUT, 4, 4, true>(a, s);
+    else if (a.D <= 8192) launch_rows<TH, TY, OUT, 2, 16, true>(a, s);
+    else launch_rows<TH, TY, OUT, 4, 16, true>(a, s);
+  } else {
+    if (a.D <= 256) launch_rows<TH, TY, OUT, 1, 1, false>(a, s);
+    else if (a.D <= 1024) launch_rows<TH, TY, OUT, 1, 4, false>(a, s);
+    else if (a.D <= 2048) launch_rows<TH, TY, OUT, 2, 4, false>(a, s);
+    else if (a.D <= 8192) launch_rows<TH, TY, OUT, 2, 16, false>(a, s);
+    else launch_rows<TH, TY, OUT, 4, 16, false>(a, s);
+  }
   return hipGetLastError();
 }
 
