@@ -122,53 +122,56 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_f8_kernel(GemmF8Args 
   const int m0 = mt * BM, n0 = nt * ON;
   const int nk = (a.K + BK - 1) / BK;
 
-  // LDS row r of the weights' part holds this column of the tile: gated, a wavefront's run of
-  // TN / 2 blocks of the gate is followed by the same run of up
-  auto column = [&](int r) -> int { return GATED ? r / (2 * WON) * WON + r % WON : r; };
-  auto is_up = [&](int r) -> bool { return GATED && r / WON % 2 == 1; };
-
-  // A load of a wavefront takes eight rows, R apart from round to round; R is a multiple of 16, so one
-  // chunk and its swizzle serve every round of a lane. Each load's resource starts at its eight rows
-  // and ends with the tile's last row, so rows past it read as zeros; its address is scalar work.
+  // LDS row r of the weights' part holds, gated, column r / (2 WON) * WON + r % WON of the tile, of the gate where r / WON
+  // is even, else of up: a wavefront's run of TN / 2 blocks of the gate is followed by the same run of up. A load of a
+  // wavefront takes eight rows, R apart from round to round, so which of the two it reads goes by the
+  // round, or by the wavefront where a round holds both.
   constexpr int R = NT / CPR;
-  static_assert(R % 16 == 0 && (!GATED || WON % 8 == 0), "rounds share the swizzle");
+  constexpr bool BY_WAVE = GATED && R % (2 * WON) == 0;
+  static_assert(R % 16 == 0, "one swizzle for a lane's rows of every round");
+  static_assert(!GATED || BY_WAVE || WON % R == 0, "a round holds rows of one, or whole runs of both");
+  auto round_up = [](int i) constexpr { return GATED && !BY_WAVE && i * R / WON % 2 == 1; };
+  auto round_column = [](int i) constexpr { return !GATED ? i * R : BY_WAVE ? i * R / 2 : i * R / (2 * WON) * WON + i * R % WON; };
+  const bool wave_up = BY_WAVE && wave * 8 / WON % 2 == 1;
+  const int wave_column = BY_WAVE ? wave * 8 / (2 * WON) * WON + wave * 8 % WON : wave * 8;
   const int kc = ((lane % CPR) ^ dma_swz<CPR>(wave * 8 + lane / CPR)) * 16;
-  const int a_off = (lane / CPR) * a.a.ld + kc, b_off = (lane / CPR) * a.b.ld + kc;
-  const int u_off = GATED ? (lane / CPR) * a.up.ld + kc : 0;
-  const int kend = (a.K + 15) & ~15;
-  const uint8_t* const A0 = a.a.q + (int64_t)m0 * a.a.ld;
-  const uint8_t* const B0 = a.b.q + (int64_t)n0 * a.b.ld;
-  const uint8_t* const U0 = GATED ? a.up.q + (int64_t)n0 * a.up.ld : nullptr;
-  const int a_bytes = (min(a.M - m0, BM) - 1) * a.a.ld + kend;
-  const int b_bytes = (min(a.N - n0, ON) - 1) * a.b.ld + kend;
-  const int u_bytes = GATED ? (min(a.N - n0, ON) - 1) * a.up.ld + kend : 0;
-  const float* const SA0 = a.a.scale + (int64_t)m0 * a.a.s_row;
+  const int a_off = (wave * 8 + lane / CPR) * a.a.ld + kc;
+  const int b_ld = wave_up ? a.up.ld : a.b.ld;
+  const int b_off = (wave_column + lane / CPR) * b_ld + kc;
+  const int u_off = GATED ? (wave_column + lane / CPR) * a.up.ld + kc : 0;
+  // resources from the tile's first row to the end of the chunk that K ends in of its last: rows past it read as zeros
+  const int kend = (a.K + 15) & ~15, o_rows = min(a.N - n0, ON) - 1;
+  const __amdgpu_buffer_rsrc_t ra = buffer_rsrc(a.a.q + (int64_t)m0 * a.a.ld, (uint32_t)((min(a.M - m0, BM) - 1) * a.a.ld + kend));
+  const __amdgpu_buffer_rsrc_t rb = buffer_rsrc((wave_up ? a.up.q : a.b.q) + (int64_t)n0 * b_ld, (uint32_t)(o_rows * b_ld + kend));
+  const __amdgpu_buffer_rsrc_t ru = GATED && !BY_WAVE ? buffer_rsrc(a.up.q + (int64_t)n0 * a.up.ld, (uint32_t)(o_rows * a.up.ld + kend)) : rb;
+  const float* sa_at = a.a.scale + (int64_t)m0 * a.a.s_row;  // of the next slice to be fetched
   const uint32_t s_bytes = (uint32_t)(min(a.M - m0, BM) - 1) * (uint32_t)a.a.s_row * 4 + 4;
   const int s_wave = wave % SROWS;
   const int s_off = m0 + s_wave * 64 + lane < a.M && s_wave * 64 + lane < BM ? (s_wave * 64 + lane) * (int)a.a.s_row * 4 : kOffOOB;
-  auto issue = [&](char* sb, int kt) __attribute__((always_inline)) {
-    const int k0 = kt * BK;
-    const bool live = k0 < a.K;
-    const bool in = k0 + kc < a.K;
-    auto load = [&](const uint8_t* base, int bytes, int from, char* to, int off) __attribute__((always_inline)) {
-      from += k0;
-      buffer_load16_lds(buffer_rsrc(base + from, live && from < bytes ? (uint32_t)(bytes - from) : 0u), to, in ? off : kOffOOB);
-    };
+  // Loads number n of slice kt; n runs from 0 to LPT. An offset past K stays past every resource
+  // with the rounds' rows added (kOffOOB and those are below 2^31 each).
+  int a_now, b_now, u_now;
+  auto issue = [&](char* sb, int kt, int from, int to) __attribute__((always_inline)) {
+    if (from == 0) {
+      const bool in = kt * BK + kc < a.K;
+      a_now = in ? a_off + kt * BK : kOffOOB;
+      b_now = in ? b_off + kt * BK : kOffOOB;
+      if constexpr (GATED && !BY_WAVE) u_now = in ? u_off + kt * BK : kOffOOB;
+    }
 #pragma unroll
-    for (int i = 0; i < ACH; ++i) load(A0, a_bytes, (wave * 8 + i * R) * a.a.ld, sb + (i * NT + wave * 64) * 16, a_off);
-#pragma unroll
-    for (int i = 0; i < BCH; ++i) {
-      char* const to = sb + (ATOT + i * NT + wave * 64) * 16;
-      const int r = wave * 8 + i * R;
-      if constexpr (GATED) {
-        const bool up = is_up(r);
-        load(up ? U0 : B0, up ? u_bytes : b_bytes, column(r) * (up ? a.up.ld : a.b.ld), to, up ? u_off : b_off);
+    for (int n = from; n < to; ++n) {
+      if (n < ACH) {
+        buffer_load16_lds(ra, sb + (n * NT + wave * 64) * 16, (int)((uint32_t)a_now + (uint32_t)(n * R * a.a.ld)));
+      } else if (n < ACH + BCH) {
+        const int i = n - ACH;
+        const bool up = round_up(i);
+        buffer_load16_lds(up ? ru : rb, sb + (ATOT + i * NT + wave * 64) * 16,
+                          (int)((uint32_t)(up ? u_now : b_now) + (uint32_t)(round_column(i) * (up ? a.up.ld : b_ld))));
       } else {
-        load(B0, b_bytes, r * a.b.ld, to, b_off);
+        buffer_load4_lds(buffer_rsrc(sa_at, kt < nk ? s_bytes : 0u), sb + SCALES + s_wave * 256, s_off);
+        sa_at += kt + 1 < nk ? a.a.s_block : 0;
       }
     }
-    const __amdgpu_buffer_rsrc_t rs = buffer_rsrc(SA0 + (int64_t)(live ? kt : 0) * a.a.s_block, live ? s_bytes : 0u);
-    buffer_load4_lds(rs, sb + SCALES + s_wave * 256, s_off);
   };
   // clears the bytes past K in the last slice
   auto clear_tail = [&](char* sb) {
@@ -267,7 +270,6 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_f8_kernel(GemmF8Args 
         __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0<(STAGES - 2) * LPT>());
         bare_barrier();
         if (a.K % 16 != 0 && kt + 2 == nk) clear_tail(stage(std::integral_constant<int, S + 1>{}));
-        issue(stage(std::integral_constant<int, S>{}), kt + STAGES);
         load_s(next, sa_next);
       }
       // reads into registers that the MFMAs before have taken
@@ -275,12 +277,16 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_f8_kernel(GemmF8Args 
       if (i == 0) load_b(j + 1 < TN ? cur : next, j + 1);
       if (j == TN - 1 && i > 0) load_a(next, i - 1);
       __builtin_amdgcn_sched_barrier(0);
-      d[p & 1] = mfma_f8<EXACT>(bf[j & 1][0], af[i][0], zero);
-      fmas((p + NP - 1) % NP, 0, pending);
-      __builtin_amdgcn_sched_barrier(0);
-      d[p & 1] = mfma_f8<EXACT>(bf[j & 1][1], af[i][1], d[p & 1]);
-      fmas((p + NP - 1) % NP, 1, pending);
-      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        d[p & 1] = mfma_f8<EXACT>(bf[j & 1][half], af[i][half], half ? d[p & 1] : zero);
+        __builtin_amdgcn_sched_barrier(0);
+        fmas((p + NP - 1) % NP, half, pending);
+        // the stage's refill, spread over the last column's MFMAs
+        if (j == TN - 1)
+          issue(stage(std::integral_constant<int, S>{}), kt + STAGES, (2 * i + half) * LPT / (2 * TM), (2 * i + half + 1) * LPT / (2 * TM));
+        __builtin_amdgcn_sched_barrier(0);
+      }
       pending = GATED && j >= TN / 2 ? s_up[i] : s_gate[i];
     }
     if (TM == 1) load_a(next, 0);
@@ -293,10 +299,10 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_f8_kernel(GemmF8Args 
     if constexpr (STAGES > 2) step(std::integral_constant<int, 2>{}, kt + 2);
     if constexpr (STAGES > 3) step(std::integral_constant<int, 3>{}, kt + 3);
   };
-  issue(stage(std::integral_constant<int, 0>{}), 0);
-  issue(stage(std::integral_constant<int, 1>{}), 1);
-  if constexpr (STAGES > 2) issue(stage(std::integral_constant<int, 2>{}), 2);
-  if constexpr (STAGES > 3) issue(stage(std::integral_constant<int, 3>{}), 3);
+  issue(stage(std::integral_constant<int, 0>{}), 0, 0, LPT);
+  issue(stage(std::integral_constant<int, 1>{}), 1, 0, LPT);
+  if constexpr (STAGES > 2) issue(stage(std::integral_constant<int, 2>{}), 2, 0, LPT);
+  if constexpr (STAGES > 3) issue(stage(std::integral_constant<int, 3>{}), 3, 0, LPT);
   __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0<(STAGES - 1) * LPT>());
   bare_barrier();
   if (a.K % 16 != 0 && nk == 1) clear_tail(st0);
