@@ -2,9 +2,9 @@
 //   out[m][n] = sum_b (sum_{k in b} A[m][k] B[n][k]) sa[m][b] sb[n / 128][b] + bias[n],
 // and of gated projections act(gate) up, both such products of the same rows.
 //
-// A block's products are summed by two v_mfma_f32_32x32x64_f8f6f4 from zero, then one fma per output
+// A block's products are summed by one v_mfma_f32_16x16x128_f8f6f4 from zero, then one fma per output
 // multiplies by sa sb (rounded once) and adds to the sum over blocks, in fp32. The weights are the first
-// operand, so a lane holds sixteen columns of ONE row: one scale per lane and block of rows, and the
+// operand, so a lane holds four adjacent columns of ONE row: one scale per lane and group of rows, and the
 // scale of the weights' block is the same for the whole wavefront.
 //
 // That instruction adds eight products of adjacent k to each other first, and cuts each off below 2^-13 of the
@@ -38,33 +38,30 @@ __device__ __forceinline__ void buffer_load4_lds(__amdgpu_buffer_rsrc_t r, char*
 }
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-// Eight codes in two words as fp16.
-__device__ __forceinline__ f16x8 f16_of(uint32_t lo, uint32_t hi) {
+// Words 2 w and 2 w + 1 of 32 codes as fp16.
+__device__ __forceinline__ f16x8 f16_of(const i32x8& v, int w) {
+  const uint32_t lo = v[2 * w], hi = v[2 * w + 1];
   const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
   const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
   return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-// c plus the products of 64 k (32 in each half of the wavefront).
-template <bool EXACT>
-__device__ __forceinline__ f32x16 mfma_f8(const i32x8& n, const i32x8& m, f32x16 c) {
-  if constexpr (EXACT) {
-#pragma unroll
-    for (int w = 0; w < 8; w += 2) c = __builtin_amdgcn_mfma_f32_32x32x16_f16(f16_of(n[w], n[w + 1]), f16_of(m[w], m[w + 1]), c, 0, 0, 0);
-    return c;
-  } else {
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(n, m, c, 0, 0, 0, 0, 0, 0);
-  }
+// 16 x 16 sums over 128 k (of which a quarter of the wavefront holds 32): at once, or over 32 k (eight a quarter) more.
+__device__ __forceinline__ f32x4 mfma_f8(const i32x8& n, const i32x8& m) {
+  const f32x4 zero = {};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(n, m, zero, 0, 0, 0, 0, 0, 0);
 }
-// Of 16 x 16 outputs: the products of 128 k, 32 in each quarter.
+__device__ __forceinline__ f32x4 mfma_f16(const f16x8& n, const f16x8& m, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(n, m, c, 0, 0, 0);
+}
 template <bool EXACT>
-__device__ __forceinline__ f32x4 mfma16_f8(const i32x8& n, const i32x8& m) {
-  f32x4 c = {};
+__device__ __forceinline__ f32x4 sum_of_block(const i32x8& n, const i32x8& m) {
   if constexpr (EXACT) {
+    f32x4 c = {};
 #pragma unroll
-    for (int w = 0; w < 8; w += 2) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16_of(n[w], n[w + 1]), f16_of(m[w], m[w + 1]), c, 0, 0, 0);
+    for (int w = 0; w < 4; ++w) c = mfma_f16(f16_of(n, w), f16_of(m, w), c);
     return c;
   } else {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(n, m, c, 0, 0, 0, 0, 0, 0);
+    return mfma_f8(n, m);
   }
 }
 
@@ -77,17 +74,20 @@ __device__ __forceinline__ float act_f8(float g) {
 
 // Slices of one block of 128 columns go global -> LDS directly into a ring of STAGES buffers (rows of eight
 // 16-byte chunks, swizzled by dma_swz; the rows' scales behind them). A wavefront owns TM x TN blocks of
-// 32 x 32; it holds its rows' codes of a slice, takes the weights' a block of 32 columns at a time, and
+// 32 x 32 outputs; it holds its rows' codes of a slice, takes the weights' a block of 32 columns at a time, and
 // meets the others once it has read the last of them, so that the stage can be filled again under the
 // MFMAs of that last block. Gated: the first half of a wavefront's TN blocks are the gate's columns,
 // the other half the same columns of up.
 //
 // Codes past K: whole chunks read as zeros (an offset past the resource); in a chunk that K ends in, the
 // bytes past K of both operands are cleared in LDS before the last slice is read.
-template <int BM, int BN, int WM, int WN, int STAGES, int MINW, F8Out OUT, F8Act ACT>
-__global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_f8_kernel(GemmF8Args a) {
+//
+// WK > 1, for few tiles: as many groups of WM WN wavefronts share a tile, group g takes slices g, g + WK, ... (a stage holds one
+// of each), and the first adds the others' sums to its own, in order, through LDS.
+template <int BM, int BN, int WM, int WN, int WK, int STAGES, int MINW, F8Out OUT, F8Act ACT>
+__global__ __launch_bounds__(WM * WN * WK * 64, MINW) void gemm_f8_kernel(GemmF8Args a) {
   constexpr bool GATED = ACT != F8_NONE, EXACT = OUT != F8_BF16;
-  constexpr int NT = WM * WN * 64, BK = 128, CPR = 8;
+  constexpr int NT = WM * WN * 64, BK = 128, CPR = 8;  // NT: of a group
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
   static_assert(TM * WM * 32 == BM && TN * WN * 32 == BN, "wave grid must tile the block");
   constexpr int ATOT = BM * CPR, BTOT = BN * CPR;
@@ -97,14 +97,15 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_f8_kernel(GemmF8Args 
   constexpr int SCALES = (ATOT + BTOT) * 16, SROWS = (BM + 63) / 64;
   constexpr int SLICE = SCALES + SROWS * 256;
   static_assert(SROWS <= WM * WN, "a wavefront per 64 scales");
-  static_assert(STAGES * SLICE <= 160 * 1024, "stages do not fit in LDS");
+  static_assert(STAGES * WK * SLICE <= 160 * 1024, "stages do not fit in LDS");
+  static_assert(WK == 1 || OUT != F8_CODES, "the scales of codes are joined over a tile's only group");
   // output columns of the tile and of a wavefront; those of a wavefront lie in one block of weights' rows
   constexpr int ON = GATED ? BN / 2 : BN, WON = ON / WN;
   static_assert(WON <= kF8Block && kF8Block % WON == 0, "a wavefront's columns share a scale");
-  __shared__ __attribute__((aligned(16))) char st0[SLICE];
-  __shared__ __attribute__((aligned(16))) char st1[SLICE];
-  __shared__ __attribute__((aligned(16))) char st2[STAGES > 2 ? SLICE : 16];
-  __shared__ __attribute__((aligned(16))) char st3[STAGES > 3 ? SLICE : 16];
+  __shared__ __attribute__((aligned(16))) char st0[WK * SLICE];
+  __shared__ __attribute__((aligned(16))) char st1[WK * SLICE];
+  __shared__ __attribute__((aligned(16))) char st2[STAGES > 2 ? WK * SLICE : 16];
+  __shared__ __attribute__((aligned(16))) char st3[STAGES > 3 ? WK * SLICE : 16];
   auto stage = [&](auto s) -> char* {
     constexpr int S = decltype(s)::value % STAGES;
     if constexpr (S == 0) return st0;
@@ -112,15 +113,16 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_f8_kernel(GemmF8Args 
     else if constexpr (S == 2) return st2;
     else return st3;
   };
-  const int tid = threadIdx.x;
-  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = threadIdx.x & 63, all_wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = all_wave / (WM * WN), wave = all_wave % (WM * WN), tid = wave * 64 + lane;  // tid: in the group
   const int wm = wave / WN, wn = wave % WN;
-  const int l32 = lane & 31, g = lane >> 5;
+  const int l16 = lane & 15, g = lane >> 4;
   int mt, nt;
   const int nbm = (a.M + BM - 1) / BM, nbn = (a.N + ON - 1) / ON;
   f8_tile(nbm, nbn, mt, nt);
   const int m0 = mt * BM, n0 = nt * ON;
-  const int nk = (a.K + BK - 1) / BK;
+  const int nk = (a.K + BK - 1) / BK, turns = (nk + WK - 1) / WK;
+  const int mine = group * SLICE;  // of a stage
 
   // LDS row r of the weights' part holds, gated, column r / (2 WON) * WON + r % WON of the tile, of the gate where r / WON
   // is even, else of up: a wavefront's run of TN / 2 blocks of the gate is followed by the same run of up. A load of a
@@ -128,56 +130,61 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_f8_kernel(GemmF8Args 
   // round, or by the wavefront where a round holds both.
   constexpr int R = NT / CPR;
   constexpr bool BY_WAVE = GATED && R % (2 * WON) == 0;
-  static_assert(R % 16 == 0, "one swizzle for a lane's rows of every round");
+  constexpr int SWZ = R % 16 == 0 ? 1 : 2;  // rounds of eight rows alternate between two swizzles, a chunk apart
+  static_assert(R % 8 == 0, "a lane's rows have one swizzle or two");
   static_assert(!GATED || BY_WAVE || WON % R == 0, "a round holds rows of one, or whole runs of both");
   auto round_up = [](int i) constexpr { return GATED && !BY_WAVE && i * R / WON % 2 == 1; };
   auto round_column = [](int i) constexpr { return !GATED ? i * R : BY_WAVE ? i * R / 2 : i * R / (2 * WON) * WON + i * R % WON; };
   const bool wave_up = BY_WAVE && wave * 8 / WON % 2 == 1;
   const int wave_column = BY_WAVE ? wave * 8 / (2 * WON) * WON + wave * 8 % WON : wave * 8;
   const int kc = ((lane % CPR) ^ dma_swz<CPR>(wave * 8 + lane / CPR)) * 16;
-  const int a_off = (wave * 8 + lane / CPR) * a.a.ld + kc;
+  const int a_off = (wave * 8 + lane / CPR) * a.a.ld;
   const int b_ld = wave_up ? a.up.ld : a.b.ld;
-  const int b_off = (wave_column + lane / CPR) * b_ld + kc;
-  const int u_off = GATED ? (wave_column + lane / CPR) * a.up.ld + kc : 0;
+  const int b_off = (wave_column + lane / CPR) * b_ld;
+  const int u_off = GATED ? (wave_column + lane / CPR) * a.up.ld : 0;
   // resources from the tile's first row to the end of the chunk that K ends in of its last: rows past it read as zeros
   const int kend = (a.K + 15) & ~15, o_rows = min(a.N - n0, ON) - 1;
   const __amdgpu_buffer_rsrc_t ra = buffer_rsrc(a.a.q + (int64_t)m0 * a.a.ld, (uint32_t)((min(a.M - m0, BM) - 1) * a.a.ld + kend));
   const __amdgpu_buffer_rsrc_t rb = buffer_rsrc((wave_up ? a.up.q : a.b.q) + (int64_t)n0 * b_ld, (uint32_t)(o_rows * b_ld + kend));
   const __amdgpu_buffer_rsrc_t ru = GATED && !BY_WAVE ? buffer_rsrc(a.up.q + (int64_t)n0 * a.up.ld, (uint32_t)(o_rows * a.up.ld + kend)) : rb;
-  const float* sa_at = a.a.scale + (int64_t)m0 * a.a.s_row;  // of the next slice to be fetched
+  const float* sa_at = a.a.scale + (int64_t)m0 * a.a.s_row + min(group, nk - 1) * a.a.s_block;  // of the next slice to be fetched
   const uint32_t s_bytes = (uint32_t)(min(a.M - m0, BM) - 1) * (uint32_t)a.a.s_row * 4 + 4;
   const int s_wave = wave % SROWS;
   const int s_off = m0 + s_wave * 64 + lane < a.M && s_wave * 64 + lane < BM ? (s_wave * 64 + lane) * (int)a.a.s_row * 4 : kOffOOB;
-  // Loads number n of slice kt; n runs from 0 to LPT. An offset past K stays past every resource
-  // with the rounds' rows added (kOffOOB and those are below 2^31 each).
-  int a_now, b_now, u_now;
-  auto issue = [&](char* sb, int kt, int from, int to) __attribute__((always_inline)) {
+  // Loads number `from` to `to` of the group's slice of a turn, LPT in all. An offset past K stays past every
+  // resource with the rounds' rows added (kOffOOB and those are below 2^31 each).
+  int a_now[SWZ], b_now[SWZ], u_now[SWZ];
+  auto issue = [&](char* sb, int turn, int from, int to) __attribute__((always_inline)) {
+    const int k0 = (turn * WK + group) * BK;
     if (from == 0) {
-      const bool in = kt * BK + kc < a.K;
-      a_now = in ? a_off + kt * BK : kOffOOB;
-      b_now = in ? b_off + kt * BK : kOffOOB;
-      if constexpr (GATED && !BY_WAVE) u_now = in ? u_off + kt * BK : kOffOOB;
+#pragma unroll
+      for (int z = 0; z < SWZ; ++z) {
+        const int k = k0 + (kc ^ (16 * z));
+        a_now[z] = k < a.K ? a_off + k : kOffOOB;
+        b_now[z] = k < a.K ? b_off + k : kOffOOB;
+        if constexpr (GATED && !BY_WAVE) u_now[z] = k < a.K ? u_off + k : kOffOOB;
+      }
     }
 #pragma unroll
     for (int n = from; n < to; ++n) {
       if (n < ACH) {
-        buffer_load16_lds(ra, sb + (n * NT + wave * 64) * 16, (int)((uint32_t)a_now + (uint32_t)(n * R * a.a.ld)));
+        buffer_load16_lds(ra, sb + mine + (n * NT + wave * 64) * 16, (int)((uint32_t)a_now[n % SWZ] + (uint32_t)(n * R * a.a.ld)));
       } else if (n < ACH + BCH) {
         const int i = n - ACH;
         const bool up = round_up(i);
-        buffer_load16_lds(up ? ru : rb, sb + (ATOT + i * NT + wave * 64) * 16,
-                          (int)((uint32_t)(up ? u_now : b_now) + (uint32_t)(round_column(i) * (up ? a.up.ld : b_ld))));
+        buffer_load16_lds(up ? ru : rb, sb + mine + (ATOT + i * NT + wave * 64) * 16,
+                          (int)((uint32_t)(up ? u_now : b_now)[i % SWZ] + (uint32_t)(round_column(i) * (up ? a.up.ld : b_ld))));
       } else {
-        buffer_load4_lds(buffer_rsrc(sa_at, kt < nk ? s_bytes : 0u), sb + SCALES + s_wave * 256, s_off);
-        sa_at += kt + 1 < nk ? a.a.s_block : 0;
+        buffer_load4_lds(buffer_rsrc(sa_at, k0 < a.K ? s_bytes : 0u), sb + mine + SCALES + s_wave * 256, s_off);
+        sa_at += k0 + WK * BK < a.K ? WK * a.a.s_block : 0;
       }
     }
   };
   // clears the bytes past K in the last slice
   auto clear_tail = [&](char* sb) {
     const int c = (a.K % BK) / 16;
-    for (int r = tid; r < BM + BN; r += NT) {
-      char* p = sb + (r * CPR + (c ^ dma_swz<CPR>(r))) * 16;
+    for (int r = tid; r < BM + BN && group == (nk - 1) % WK; r += NT) {
+      char* p = sb + mine + (r * CPR + (c ^ dma_swz<CPR>(r))) * 16;
       i32x4 v = *(i32x4*)p;
       const int left = a.K % 16;
 #pragma unroll
@@ -191,113 +198,119 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_f8_kernel(GemmF8Args 
   };
   static_assert(BM % 16 == 0, "the weights' rows start at a multiple of 16, as their swizzle has it");
 
-  // scales of the wavefront's block of weights, lane l those of slices l, 64 + l, ...
+  // scales of the wavefront's block of weights, lane l those of turns l, 64 + l, ...
   const int sb_row = min(n0 + wn * WON, a.N - 1) / kF8Block;
-  auto weights_scale = [&](const F8Codes& w, int kt) -> float {
-    return w.scale[(int64_t)sb_row * w.s_row + (int64_t)min(kt + lane, nk - 1) * w.s_block];
+  auto weights_scale = [&](const F8Codes& w, int turn) -> float {
+    return w.scale[(int64_t)sb_row * w.s_row + (int64_t)min((turn + lane) * WK + group, nk - 1) * w.s_block];
   };
   float sb_v = weights_scale(a.b, 0), su_v = GATED ? weights_scale(a.up, 0) : 0.0f;
 
-  f32x16 acc[TM][TN];
+  // Units of 16 rows x 32 columns: unit u = j IB + i is rows i of column block j.
+  constexpr int IB = TM * 2, NU = IB * TN, PARTS = EXACT ? 4 : 1;
+  f32x4 acc[IB][TN][2];
 #pragma unroll
-  for (int i = 0; i < TM; ++i)
+  for (int i = 0; i < IB; ++i)
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-  const int sw = dma_swz<CPR>(l32);  // row blocks are 32 apart: every row of a lane shares it
-  // chunk g + c of a lane's first row (c even, so that g + c is g ^ c); the other chunks and blocks are
-  // an exclusive or and a constant away, formed where they are used: kept, they cost 16 registers
-  const int a_at = ((wm * TM * 32 + l32) * CPR + (g ^ sw)) * 16;
-  const int b_at = (ATOT + (wn * TN * 32 + l32) * CPR + (g ^ sw)) * 16;
-  // Blocks of a slice in the order p = j TM + i. The two MFMAs of block p + 1 are issued around the fmas of
-  // block p, which are VALU work in the matrix core's shadow; block NP - 1's wait for the next slice.
-  constexpr int NP = TM * TN;
-  i32x8 af[TM][2], bf[2][2];
-  float s_gate[TM], s_up[TM], pending = 0.0f;
-  f32x16 d[2] = {};
-  auto frag = [&](const char* cur, int at, int s) __attribute__((always_inline)) -> i32x8 {
-    const i32x4 lo = *(const i32x4*)(cur + (at ^ (64 * s)));
-    const i32x4 hi = *(const i32x4*)(cur + (at ^ (64 * s + 32)));
+    for (int j = 0; j < TN; ++j) acc[i][j][0] = acc[i][j][1] = f32x4{};
+  const int sw = dma_swz<CPR>(l16);  // groups of rows are 16 apart: every row of a lane shares it
+  // chunks 2 g and 2 g + 1 of a lane's first row: the quarter's 32 codes; other groups are a constant away
+  const int a_at = mine + ((wm * TM * 32 + l16) * CPR + ((2 * g) ^ sw)) * 16;
+  const int b_at = mine + (ATOT + (wn * TN * 32 + l16) * CPR + ((2 * g) ^ sw)) * 16;
+  // The MFMAs of unit u + 1 are issued between the fmas of unit u, which are VALU work in the matrix core's shadow; the
+  // last unit's wait for the next slice. EXACT: so are the conversions to fp16, each operand's once per slice.
+  i32x8 af[IB], bf[EXACT ? 1 : 2][2];
+  f16x8 a16[EXACT ? IB : 1][4], b16[2][4];
+  f32x4 d[2][2] = {};
+  float sa[IB], sa_next[IB], s_gate[IB], s_up[IB], pending = 0.0f;
+  auto frag = [&](const char* cur, int at) __attribute__((always_inline)) -> i32x8 {
+    const i32x4 lo = *(const i32x4*)(cur + at), hi = *(const i32x4*)(cur + (at ^ 16));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  auto load_a = [&](const char* cur, int i) __attribute__((always_inline)) {
-    int at = a_at;
-    asm volatile("" : "+v"(at));
-    af[i][0] = frag(cur + i * 32 * CPR * 16, at, 0);
-    af[i][1] = frag(cur + i * 32 * CPR * 16, at, 1);
-  };
+  auto load_a = [&](const char* cur, int i) __attribute__((always_inline)) { af[i] = frag(cur + i * 16 * CPR * 16, a_at); };
   auto load_b = [&](const char* cur, int j) __attribute__((always_inline)) {
-    int at = b_at;
-    asm volatile("" : "+v"(at));
-    bf[j & 1][0] = frag(cur + (j % TN) * 32 * CPR * 16, at, 0);
-    bf[j & 1][1] = frag(cur + (j % TN) * 32 * CPR * 16, at, 1);
-  };
-  auto load_s = [&](const char* cur, float (&s)[TM]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) s[i] = *(const float*)(cur + SCALES + ((wm * TM + i) * 32 + l32) * 4);
+    for (int c = 0; c < 2; ++c) bf[EXACT ? 0 : j & 1][c] = frag(cur + (j % TN * 2 + c) * 16 * CPR * 16, b_at);
   };
-  auto fmas = [&](int p, int half, float s) __attribute__((always_inline)) {
+  auto load_s = [&](const char* cur, float (&s)[IB]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 8 * half; r < 8 * half + 8; ++r) acc[p % TM][p / TM][r] = __builtin_fmaf(d[p & 1][r], s, acc[p % TM][p / TM][r]);
+    for (int i = 0; i < IB; ++i) s[i] = *(const float*)(cur + mine + SCALES + (wm * TM * 32 + i * 16 + l16) * 4);
+  };
+  auto fmas = [&](int u, int c, int part, float s) __attribute__((always_inline)) {
+    f32x4& to = acc[u % IB][u / IB][c];
+#pragma unroll
+    for (int r = 4 / PARTS * part; r < 4 / PARTS * (part + 1); ++r) to[r] = __builtin_fmaf(d[u & 1][c][r], s, to[r]);
     // computed here: moved behind later MFMAs they would keep those's results alive as well
-    asm volatile("" : "+v"(acc[p % TM][p / TM]));
+    asm volatile("" : "+v"(to));
   };
-  const f32x16 zero = {};
-  static_assert(TN % 2 == 0 && NP % 2 == 0, "the next slice starts with the buffers that this one started with");
-  float sa[TM], sa_next[TM];
-  auto step = [&](auto st, int kt) __attribute__((always_inline)) {
+  static_assert(TN % 2 == 0 && NU % 2 == 0, "the next slice starts with the buffers that this one started with");
+  auto step = [&](auto st, int turn) __attribute__((always_inline)) {
     constexpr int S = decltype(st)::value;
     const char* const cur = stage(std::integral_constant<int, S>{});
     const char* const next = stage(std::integral_constant<int, S + 1>{});
-    if ((kt & 63) == 0 && kt > 0) {
-      sb_v = weights_scale(a.b, kt);
-      if constexpr (GATED) su_v = weights_scale(a.up, kt);
+    if ((turn & 63) == 0 && turn > 0) {
+      sb_v = weights_scale(a.b, turn);
+      if constexpr (GATED) su_v = weights_scale(a.up, turn);
       __builtin_amdgcn_s_waitcnt(0);
     }
-    const float sb = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sb_v), kt & 63));
-    const float su = GATED ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(su_v), kt & 63)) : 0.0f;
+    const bool live = WK == 1 || turn * WK + group < nk;  // past K, codes and the rows' scales are 0
+    const float sb = live ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sb_v), turn & 63)) : 0.0f;
+    const float su = GATED && live ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(su_v), turn & 63)) : 0.0f;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
+    for (int i = 0; i < IB; ++i) {
       s_gate[i] = sa[i] * sb;
       s_up[i] = sa[i] * su;
     }
 #pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      const int i = p % TM, j = p / TM;
-      if (p == NP - TM) {
+    for (int u = 0; u < NU; ++u) {
+      const int i = u % IB, j = u / IB;
+      if (u == NU - IB) {
         // every read of this stage has arrived: the MFMAs below take the last of them
         __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0<(STAGES - 2) * LPT>());
         bare_barrier();
-        if (a.K % 16 != 0 && kt + 2 == nk) clear_tail(stage(std::integral_constant<int, S + 1>{}));
+        if (a.K % 16 != 0 && turn + 2 == turns) clear_tail(stage(std::integral_constant<int, S + 1>{}));
         load_s(next, sa_next);
       }
-      // reads into registers that the MFMAs before have taken
-      if (p == 0 && TM > 1) load_a(cur, TM - 1);
-      if (i == 0) load_b(j + 1 < TN ? cur : next, j + 1);
-      if (j == TN - 1 && i > 0) load_a(next, i - 1);
+      // reads into registers that the MFMAs (EXACT: the conversions) before have taken
+      if (i == (EXACT ? 1 : 0)) load_b(j + 1 < TN ? cur : next, j + 1);
+      if constexpr (EXACT) {
+        if (u == NU - IB) {
+#pragma unroll
+          for (int n = 0; n < IB; ++n) load_a(next, n);
+        }
+      } else {
+        if (u == 0) load_a(cur, IB - 1);
+        if (j == TN - 1 && i > 0) load_a(next, i - 1);
+      }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        d[p & 1] = mfma_f8<EXACT>(bf[j & 1][half], af[i][half], half ? d[p & 1] : zero);
-        __builtin_amdgcn_sched_barrier(0);
-        fmas((p + NP - 1) % NP, half, pending);
-        // the stage's refill, spread over the last column's MFMAs
-        if (j == TN - 1)
-          issue(stage(std::integral_constant<int, S>{}), kt + STAGES, (2 * i + half) * LPT / (2 * TM), (2 * i + half + 1) * LPT / (2 * TM));
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      for (int w = 0; w < PARTS; ++w)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          if constexpr (EXACT) {
+            if (i == 0) b16[c][w] = f16_of(bf[0][c], w);
+            if (j == 0 && c == 0) a16[i][w] = f16_of(af[i], w);
+            d[u & 1][c] = mfma_f16(b16[c][w], a16[i][w], w ? d[u & 1][c] : f32x4{});
+          } else {
+            d[u & 1][c] = mfma_f8(bf[j & 1][c], af[i]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          fmas((u + NU - 1) % NU, c, w, pending);
+          // the stage's refill, spread over the last column's MFMAs
+          constexpr int N = PARTS * 2 * IB;
+          const int n = (i * PARTS + w) * 2 + c;
+          if (j == TN - 1) issue(stage(std::integral_constant<int, S>{}), turn + STAGES, n * LPT / N, (n + 1) * LPT / N);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       pending = GATED && j >= TN / 2 ? s_up[i] : s_gate[i];
     }
-    if (TM == 1) load_a(next, 0);
 #pragma unroll
-    for (int i = 0; i < TM; ++i) sa[i] = sa_next[i];
+    for (int i = 0; i < IB; ++i) sa[i] = sa_next[i];
   };
-  auto round = [&](int kt) __attribute__((always_inline)) {
-    step(std::integral_constant<int, 0>{}, kt);
-    step(std::integral_constant<int, 1>{}, kt + 1);
-    if constexpr (STAGES > 2) step(std::integral_constant<int, 2>{}, kt + 2);
-    if constexpr (STAGES > 3) step(std::integral_constant<int, 3>{}, kt + 3);
+  auto round = [&](int turn) __attribute__((always_inline)) {
+    step(std::integral_constant<int, 0>{}, turn);
+    step(std::integral_constant<int, 1>{}, turn + 1);
+    if constexpr (STAGES > 2) step(std::integral_constant<int, 2>{}, turn + 2);
+    if constexpr (STAGES > 3) step(std::integral_constant<int, 3>{}, turn + 3);
   };
   issue(stage(std::integral_constant<int, 0>{}), 0, 0, LPT);
   issue(stage(std::integral_constant<int, 1>{}), 1, 0, LPT);
@@ -305,55 +318,83 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_f8_kernel(GemmF8Args 
   if constexpr (STAGES > 3) issue(stage(std::integral_constant<int, 3>{}), 3, 0, LPT);
   __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0<(STAGES - 1) * LPT>());
   bare_barrier();
-  if (a.K % 16 != 0 && nk == 1) clear_tail(st0);
+  if (a.K % 16 != 0 && turns == 1) clear_tail(st0);
 #pragma unroll
-  for (int i = 0; i < TM - 1 || i == 0; ++i) load_a(st0, i);
+  for (int i = 0; i < (EXACT ? IB : IB - 1); ++i) load_a(st0, i);
   load_b(st0, 0);
   load_s(st0, sa);
-  int kt = 0;
-  for (; kt + STAGES <= nk; kt += STAGES) round(kt);
-  if (kt < nk) step(std::integral_constant<int, 0>{}, kt);
+  int turn = 0;
+  for (; turn + STAGES <= turns; turn += STAGES) round(turn);
+  if (turn < turns) step(std::integral_constant<int, 0>{}, turn);
   if constexpr (STAGES > 2)
-    if (kt + 1 < nk) step(std::integral_constant<int, 1>{}, kt + 1);
+    if (turn + 1 < turns) step(std::integral_constant<int, 1>{}, turn + 1);
   if constexpr (STAGES > 3)
-    if (kt + 2 < nk) step(std::integral_constant<int, 2>{}, kt + 2);
-  fmas(NP - 1, 0, pending);
-  fmas(NP - 1, 1, pending);
+    if (turn + 2 < turns) step(std::integral_constant<int, 2>{}, turn + 2);
+#pragma unroll
+  for (int w = 0; w < PARTS; ++w) {
+    fmas(NU - 1, 0, w, pending);
+    fmas(NU - 1, 1, w, pending);
+  }
   __builtin_amdgcn_s_waitcnt(0);  // the loads past K land before the LDS is used again or given up
-
-  // Lane (l32, g) holds row l32 of each block and the columns 8 q + 4 g + 0..3. Values and bias first;
-  // a gated wavefront has its outputs in the gate's blocks then.
-  constexpr int TO = GATED ? TN / 2 : TN;
+  if constexpr (WK > 1) {
+    static_assert((WK - 1) * BM * BN * 4 <= WK * SLICE, "the other groups' sums fit a stage");
+    f32x4* const sums = (f32x4*)st0 + wave * NU * 2 * 64 + lane;
+    constexpr int GROUP = BM * BN / 4;
+    __syncthreads();
+    if (group > 0) {
 #pragma unroll
-  for (int j = 0; j < TO; ++j) {
-    const int nb = n0 + wn * WON + j * 32;
-    const int n = min(nb + l32, a.N - 1);
-    const float bias_v = a.bias ? a.bias[n] : 0.0f, up_v = GATED && a.up_bias ? a.up_bias[n] : 0.0f;
+      for (int u = 0; u < 2 * NU; ++u) sums[(group - 1) * GROUP + u * 64] = acc[u / 2 % IB][u / 2 / IB][u & 1];
+    }
+    __syncthreads();
+    if (group == 0) {
+      for (int o = 0; o < WK - 1; ++o)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int from = 8 * (r >> 2) + 4 * g + (r & 3);
-      const float b = __shfl(bias_v, from);
-      const float u = GATED ? __shfl(up_v, from) : 0.0f;
-#pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const float v = acc[i][j][r] + b;
-        if constexpr (GATED)
-          acc[i][j][r] = act_f8<ACT>(v) * (acc[i][j + TO][r] + u);
-        else
-          acc[i][j][r] = v;
-      }
+        for (int u = 0; u < 2 * NU; ++u) acc[u / 2 % IB][u / 2 / IB][u & 1] += sums[o * GROUP + u * 64];
     }
   }
+
+  // Lane (l16, g) holds row l16 of each group of rows and the columns 16 c + 4 g + 0..3 of each block. Values and bias first;
+  // a gated wavefront has its outputs in the gate's blocks then.
+  constexpr int TO = GATED ? TN / 2 : TN;
+  typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+  auto bias4 = [&](const float* p, int n) __attribute__((always_inline)) -> f32x4 {
+    if (n + 4 <= a.N) return *(const f32x4_any*)(p + n);
+    f32x4 v = {};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (n + e < a.N) v[e] = p[n + e];
+    return v;
+  };
+#pragma unroll
+  for (int j = 0; j < TO; ++j)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int n = n0 + wn * WON + j * 32 + 16 * c + 4 * g;
+      f32x4 b = {}, u = {};
+      if (a.bias) b = bias4(a.bias, n);
+      if (GATED && a.up_bias) u = bias4(a.up_bias, n);
+#pragma unroll
+      for (int i = 0; i < IB; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v = acc[i][j][c][e] + b[e];
+          if constexpr (GATED)
+            acc[i][j][c][e] = act_f8<ACT>(v) * (acc[i][j + TO][c][e] + u[e]);
+          else
+            acc[i][j][c][e] = v;
+        }
+    }
   // Every wavefront passes its part of the tile through LDS of its own, 32 rows at a time, so that
   // stores leave in whole rows of the part
   typedef uint32_t out16 __attribute__((ext_vector_type(4), aligned(1)));
   constexpr int ES = OUT == F8_F32 ? 4 : OUT == F8_BF16 ? 2 : 1;
   constexpr int E = 16 / ES, JG = OUT == F8_F32 ? 1 : TO;
   constexpr int PITCH = JG * 32 * ES + 16, CPW = JG * 32 / E, HALF = (WM * WN + 1) / 2;
-  static_assert(HALF * 32 * PITCH <= SCALES, "the parts of half the wavefronts fit a stage");
+  static_assert(HALF * 32 * PITCH <= WK * SLICE, "the parts of half the wavefronts fit a stage");
   char* const part = (wave < HALF ? st0 + wave * 32 * PITCH : st1 + (wave - HALF) * 32 * PITCH);
   __syncthreads();
-  BlockF8 bq[OUT == F8_CODES ? TM : 1];
+  if (WK > 1 && group > 0) return;  // no barrier follows: codes have one group
+  BlockF8 bq[OUT == F8_CODES ? IB : 1];
   if constexpr (OUT == F8_CODES) {
     // the scale of a row's 128 columns: every wavefront's largest, joined in LDS
     static_assert(ON == kF8Block, "a tile holds whole blocks of outputs");
@@ -362,27 +403,27 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_f8_kernel(GemmF8Args 
     uint32_t* const tops = (uint32_t*)(STAGES > 2 ? st2 : st1 + HALF * 32 * PITCH);
     static_assert(STAGES > 2 || HALF * 32 * PITCH + BM * CP * 4 <= SLICE, "tops fit behind the parts");
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
+    for (int i = 0; i < IB; ++i) {
       uint32_t t = 0;
 #pragma unroll
       for (int j = 0; j < TO; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int n = n0 + wn * WON + j * 32 + 8 * (r >> 2) + 4 * g + (r & 3);
-          if (n < a.N) t = max(t, abs_bits(acc[i][j][r]));
+        for (int e = 0; e < 8; ++e) {
+          const int n = n0 + wn * WON + j * 32 + 16 * (e >> 2) + 4 * g + (e & 3);
+          if (n < a.N) t = max(t, abs_bits(acc[i][j][e >> 2][e & 3]));
         }
-      t = xor_max<32>(t);
-      if (g == 0) tops[((wm * TM + i) * 32 + l32) * CP + wn] = t;
+      t = xor_max<32>(xor_max<16>(t));
+      if (g == 0) tops[(wm * TM * 32 + i * 16 + l16) * CP + wn] = t;
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const uint32_t* const p = tops + ((wm * TM + i) * 32 + l32) * CP;
+    for (int i = 0; i < IB; ++i) {
+      const uint32_t* const p = tops + (wm * TM * 32 + i * 16 + l16) * CP;
       uint32_t t = p[0];
 #pragma unroll
       for (int w = 1; w < WN; ++w) t = max(t, p[w]);
       bq[i] = block_f8(t);
-      const int m = m0 + (wm * TM + i) * 32 + l32;
+      const int m = m0 + wm * TM * 32 + i * 16 + l16;
       if (wn == 0 && g == 0 && m < a.M) a.out_scale[(int64_t)m * a.os_row + (int64_t)(n0 / kF8Block) * a.os_block] = bq[i].scale;
     }
   }
@@ -391,24 +432,26 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_f8_kernel(GemmF8Args 
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
 #pragma unroll
-      for (int j = 0; j < JG; ++j) {
-        uint32_t c[4];
+      for (int h = 0; h < 2; ++h) {
+        const auto& rows = acc[2 * i + h];
+        char* const p = part + (16 * h + l16) * PITCH + 4 * g * ES;
+        uint32_t q[2 * JG];
         if constexpr (OUT == F8_CODES) {
-          float v[16];
+          float v[8 * JG];
 #pragma unroll
-          for (int r = 0; r < 16; ++r) v[r] = acc[i][j0 + j][r];
-          codes_f8(v, bq[i], c);
+          for (int e = 0; e < 8 * JG; ++e) v[e] = rows[j0 + e / 8][e / 4 % 2][e % 4];
+          codes_f8(v, bq[2 * i + h], q);
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          char* const p = part + l32 * PITCH + (j * 32 + q * 8 + g * 4) * ES;
-          const f32x16& v = acc[i][j0 + j];
+        for (int c = 0; c < 2 * JG; ++c) {
+          const f32x4 v = rows[j0 + c / 2][c % 2];
+          char* const to = p + c * 16 * ES;
           if constexpr (OUT == F8_F32)
-            *(f32x4*)p = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+            *(f32x4*)to = v;
           else if constexpr (OUT == F8_BF16)
-            *(uint2*)p = uint2{pack_bf16(v[4 * q], v[4 * q + 1]), pack_bf16(v[4 * q + 2], v[4 * q + 3])};
+            *(uint2*)to = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
           else
-            *(uint32_t*)p = c[q];
+            *(uint32_t*)to = q[c];
         }
       }
       __builtin_amdgcn_wave_barrier();
@@ -439,17 +482,19 @@ __global__ __launch_bounds__(WM * WN * 64, MINW) void gemm_f8_kernel(GemmF8Args 
   }
 }
 
-// Few rows, up to 16 MT: the weights are read once and bound it, so a workgroup takes only sixteen columns (gated:
-// of both projections), its W wavefronts share the blocks of K among them, each straight from memory to
-// v_mfma_f32_16x16x128_f8f6f4, and the sums are joined in LDS in a fixed order.
-template <int MT, int W, F8Out OUT, F8Act ACT>
-__global__ __launch_bounds__(W * 64) void few_f8_kernel(GemmF8Args a) {
+// Few rows, up to 16 MT: the weights are read once and bound it, so a wavefront takes only sixteen columns (gated:
+// of both projections) and a KS-th of the blocks of K, straight from memory to the matrix cores, and the sums
+// are joined in LDS in a fixed order. A workgroup has CG such columns: one, so that there are many
+// workgroups, and eight, the 128 outputs that share a scale, where the outputs are codes.
+template <int MT, int CG, int KS, F8Out OUT, F8Act ACT>
+__global__ __launch_bounds__(CG * KS * 64) void few_f8_kernel(GemmF8Args a) {
   constexpr bool GATED = ACT != F8_NONE;
-  constexpr int P = GATED ? 2 : 1, AHEAD = MT == 1 ? 4 : 2;
-  __shared__ __attribute__((aligned(16))) f32x4 sums[W][P][MT][64];
+  constexpr int P = GATED ? 2 : 1, AHEAD = MT * P * CG > 2 ? 2 : 4;
+  static_assert(OUT != F8_CODES || CG * 16 == kF8Block, "a workgroup holds a block of outputs");
+  __shared__ __attribute__((aligned(16))) f32x4 sums[KS][CG][P][MT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int l16 = lane & 15, g = lane >> 4;
-  const int n0 = blockIdx.x * 16;
+  const int l16 = lane & 15, g = lane >> 4, cg = wave % CG, ks = wave / CG;
+  const int n0 = min((int)blockIdx.x * CG + cg, (a.N - 1) / 16) * 16;  // past the last column: the last ones again
   const int nk = (a.K + kF8Block - 1) / kF8Block;
   // the resources hold the tile's rows to the end of the chunk that K ends in; rows past the last are it
   const int kend = (a.K + 15) & ~15;
@@ -482,12 +527,12 @@ __global__ __launch_bounds__(W * 64) void few_f8_kernel(GemmF8Args a) {
     }
   };
   f32x4 acc[P][MT] = {};
-  for (int kb0 = wave; kb0 < nk; kb0 += AHEAD * W) {
+  for (int kb0 = ks; kb0 < nk; kb0 += AHEAD * KS) {
     i32x8 b[AHEAD][P], x[AHEAD][MT];
     float s[AHEAD][MT], w[AHEAD][P];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-      const int kb = kb0 + u * W, k = kb * kF8Block + 32 * g, sk = min(kb, nk - 1);
+      const int kb = kb0 + u * KS, k = kb * kF8Block + 32 * g, sk = min(kb, nk - 1);
       b[u][0] = load(rb, b_off, k);
       if constexpr (GATED) b[u][P - 1] = load(ru, u_off, k);
 #pragma unroll
@@ -500,7 +545,7 @@ __global__ __launch_bounds__(W * 64) void few_f8_kernel(GemmF8Args a) {
     }
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-      const int kb = kb0 + u * W, k = kb * kF8Block + 32 * g;
+      const int kb = kb0 + u * KS, k = kb * kF8Block + 32 * g;
       if (kb >= nk) break;
       if (kb + 1 == nk && a.K % 16 != 0) {
 #pragma unroll
@@ -512,7 +557,7 @@ __global__ __launch_bounds__(W * 64) void few_f8_kernel(GemmF8Args a) {
       for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-          const f32x4 d = mfma16_f8<OUT != F8_BF16>(b[u][p], x[u][t]);
+          const f32x4 d = sum_of_block<OUT != F8_BF16>(b[u][p], x[u][t]);
           const float f = s[u][t] * w[u][p];
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[p][t][e] = __builtin_fmaf(d[e], f, acc[p][t][e]);
@@ -522,45 +567,76 @@ __global__ __launch_bounds__(W * 64) void few_f8_kernel(GemmF8Args a) {
 #pragma unroll
   for (int p = 0; p < P; ++p)
 #pragma unroll
-    for (int t = 0; t < MT; ++t) sums[wave][p][t][lane] = acc[p][t];
+    for (int t = 0; t < MT; ++t) sums[ks][cg][p][t][lane] = acc[p][t];
   __syncthreads();
-  for (int e = threadIdx.x; e < MT * 256; e += W * 64) {
-    const int t = e >> 8, m = (e >> 4) & 15, c = e & 15, n = n0 + c;
-    float v[P];
+  // four adjacent columns of a row to a thread
+  for (int e = threadIdx.x; e < MT * 16 * CG * 4; e += CG * KS * 64) {
+    const int c = e % (CG * 4), m = e / (CG * 4) % 16, t = e / (CG * 64);
+    const int row = t * 16 + m, n = (int)blockIdx.x * CG * 16 + c * 4, left = a.N - n;
+    f32x4 v[P];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      v[p] = 0.0f;
+      v[p] = sums[0][c >> 2][p][t][(c & 3) * 16 + m];
 #pragma unroll
-      for (int k = 0; k < W; ++k) v[p] += ((const float*)&sums[k][p][t][(c >> 2) * 16 + m])[c & 3];
+      for (int k = 1; k < KS; ++k) v[p] += sums[k][c >> 2][p][t][(c & 3) * 16 + m];
     }
-    if (t * 16 + m >= a.M || n >= a.N) continue;
-    v[0] += a.bias ? a.bias[n] : 0.0f;
-    if constexpr (GATED) v[0] = act_f8<ACT>(v[0]) * (v[P - 1] + (a.up_bias ? a.up_bias[n] : 0.0f));
-    const int64_t at = (int64_t)(t * 16 + m) * a.ldo + n;
-    if constexpr (OUT == F8_F32)
-      ((float*)a.out)[at] = v[0];
-    else
-      ((bf16*)a.out)[at] = (bf16)v[0];
+    float x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = v[0][i];
+      if (a.bias && i < left) x[i] += a.bias[n + i];
+      if constexpr (GATED) {
+        float u = v[P - 1][i];
+        if (a.up_bias && i < left) u += a.up_bias[n + i];
+        x[i] = act_f8<ACT>(x[i]) * u;
+      }
+    }
+    if constexpr (OUT == F8_CODES) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max(top, i < left ? abs_bits(x[i]) : 0u);
+      const BlockF8 b = block_f8(max_of_32(top));  // of 32 threads, which share a row
+      uint32_t q[1];
+      codes_f8(x, b, q);
+      if (row >= a.M) continue;
+      if (c == 0) a.out_scale[(int64_t)row * a.os_row + (int64_t)blockIdx.x * a.os_block] = b.scale;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < left) ((uint8_t*)a.out)[(int64_t)row * a.ldo + n + i] = (uint8_t)(q[0] >> (8 * i));
+    } else {
+      if (row >= a.M) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < left) {
+          if constexpr (OUT == F8_F32)
+            ((float*)a.out)[(int64_t)row * a.ldo + n + i] = x[i];
+          else
+            ((bf16*)a.out)[(int64_t)row * a.ldo + n + i] = (bf16)x[i];
+        }
+    }
   }
 }
 
 template <F8Out OUT, F8Act ACT>
 static void launch_few(const GemmF8Args& a, hipStream_t s) {
-  const dim3 grid((uint32_t)((a.N + 15) / 16));
+  constexpr int CG = OUT == F8_CODES ? 8 : 1, KS = OUT == F8_CODES ? 2 : 4;
+  const dim3 grid((uint32_t)((a.N + CG * 16 - 1) / (CG * 16)));
   if (a.M <= 16)
-    launch(few_f8_kernel<1, 8, OUT, ACT>, grid, dim3(512), 0, s, a);
-  else if (a.M <= 32)
-    launch(few_f8_kernel<2, 8, OUT, ACT>, grid, dim3(512), 0, s, a);
+    launch(few_f8_kernel<1, CG, KS, OUT, ACT>, grid, dim3(CG * KS * 64), 0, s, a);
   else
-    launch(few_f8_kernel<4, 8, OUT, ACT>, grid, dim3(512), 0, s, a);
+    launch(few_f8_kernel<2, CG, KS, OUT, ACT>, grid, dim3(CG * KS * 64), 0, s, a);
 }
 
-// Tiles: BM x BN, wave grid, LDS stages, wavefronts per SIMD.
-#define SF_F8_TILES(X)                    \
-  X(kF8Deep64, 64, 64, 2, 1, 4, 2)        \
-  X(kF8Tile128, 128, 128, 2, 2, 2, 2)     \
-  X(kF8Tile128x256, 128, 256, 2, 4, 2, 2) \
-  X(kF8Tile256x256, 256, 256, 4, 2, 2, 2)
+// Tiles: BM x BN, wave grid, groups of it, LDS stages, wavefronts per SIMD.
+#define SF_F8_TILES(X)                       \
+  X(kF8Split64, 64, 64, 2, 1, 2, 4, 1)       \
+  X(kF8Split64x4, 64, 64, 2, 1, 4, 2, 1)     \
+  X(kF8Deep128, 128, 128, 4, 2, 1, 4, 2)     \
+  X(kF8Tile128, 128, 128, 2, 2, 1, 2, 2)     \
+  X(kF8Codes64, 64, 256, 2, 4, 1, 3, 2)      \
+  X(kF8Codes128, 128, 256, 2, 4, 1, 2, 2)    \
+  X(kF8Tile128x256, 128, 256, 2, 4, 1, 3, 2) \
+  X(kF8Tile256x256, 256, 256, 4, 2, 1, 2, 2)
 
 template <F8Out OUT, F8Act ACT>
 static hipError_t launch_f8(const GemmF8Args& a, hipStream_t s) {
@@ -568,15 +644,15 @@ static hipError_t launch_f8(const GemmF8Args& a, hipStream_t s) {
   F8Tile tile = choose_gemm_f8_tile(a.M, (long)a.N * (kGated ? 2 : 1), a.K, OUT == F8_CODES, OUT == F8_F32);
   switch (tile) {
     case kF8Few:
-      if constexpr (OUT != F8_CODES) launch_few<OUT, ACT>(a, s);
+      launch_few<OUT, ACT>(a, s);
       break;
-#define SF_F8_CASE(id, bm, bn, wm, wn, st, mw)                                                                \
+#define SF_F8_CASE(id, bm, bn, wm, wn, wk, st, mw)                                                              \
   case id: {                                                                                                  \
     constexpr int on = kGated ? bn / 2 : bn;                                                                  \
     const int64_t tiles = (((int64_t)a.M + bm - 1) / bm) * (((int64_t)a.N + on - 1) / on);                    \
     if (tiles > 0x7fffffff) return hipErrorInvalidValue;                                                      \
-    if constexpr ((OUT != F8_CODES || on == kF8Block) && (OUT == F8_BF16 || bm < 256)) /* never chosen otherwise */                             \
-      launch(gemm_f8_kernel<bm, bn, wm, wn, st, mw, OUT, ACT>, dim3((uint32_t)tiles), dim3(wm * wn * 64), 0, s, a); \
+    if constexpr (f8_has_tile(id, OUT == F8_CODES, OUT != F8_BF16))                              \
+      launch(gemm_f8_kernel<bm, bn, wm, wn, wk, st, mw, OUT, ACT>, dim3((uint32_t)tiles), dim3(wm * wn * wk * 64), 0, s, a); \
     break;                                                                                                    \
   }
     SF_F8_TILES(SF_F8_CASE)

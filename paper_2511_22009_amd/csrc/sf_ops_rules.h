@@ -65,16 +65,58 @@ inline I8Tile choose_gemm_i8_tile(long M, long N, long K, bool heavy, bool resid
   return best;
 }
 
-// Tiles of the products of e4m3 codes. N counts columns of the weights (gated: both projections).
-// Outputs that are codes need a tile that holds whole blocks of 128 outputs.
-enum F8Tile { kF8Few, kF8Deep64, kF8Tile128, kF8Tile128x256, kF8Tile256x256 };
+// Tiles of the products of e4m3 codes. Outputs that are codes need a tile that holds whole blocks of 128
+// outputs, gated: 256 columns of both projections. `exact`: sums in fp32 (outputs in fp32, or codes).
+enum F8Tile { kF8Few, kF8Split64, kF8Split64x4, kF8Deep128, kF8Tile128, kF8Tile128x256, kF8Tile256x256, kF8Codes64, kF8Codes128 };
+constexpr bool f8_has_tile(F8Tile t, bool codes, bool exact) {
+  return codes   ? t == kF8Codes64 || t == kF8Codes128
+         : exact ? t == kF8Split64x4 || t == kF8Tile128
+                 : t == kF8Split64 || t == kF8Deep128 || t == kF8Tile128 || t == kF8Tile128x256 || t == kF8Tile256x256;
+}
+
+// What the workgroups of a tile cost that a CU runs side by side (`per` of them, or one alone), in ns: so much per
+// 128-wide slice of K and so much once.
+struct F8Cost {
+  F8Tile tile;
+  int bm, bn, per, slice, once, alone_slice, alone_once;
+};
+
+// Which tile: the one with the least work on its busiest CU. N counts columns of the weights (gated: both
+// projections). Costs from launches of one and of two rounds of each tile at K = 1024 and 4096. Some times (us):
+//   * 256 x 256, of large outputs: 16384 x 4608 x 1152 115, 128 x 256 129, 128 x 128 in pairs 136; 8192^3 492, 535
+//     and 585.
+//   * 128 x 128 in pairs where rounds of the large tiles are left half empty: 16384 x 1152 x 4608 123, 256 x 256 129.
+//   * 128 x 128 with four stages, eight wavefronts, one per CU, for single rounds of it: 2048 x 2048 x 4096 23, in pairs
+//     31, 128 x 256 37.
+//   * 64 x 64 with K split over two groups of wavefronts for the smallest grids: 512 x 1024 x 4352 11.6, over four
+//     13.3, not split 13.9, 128 x 128 30; in fp32 517 x 1001 x 4321 over four 16.0, not split 25.
+// Up to 32 rows the weights' bytes count, which more and smaller workgroups fetch sooner: 32 x 3456 x 1152 4.4,
+// 64 x 64 6.1; but long weights that a tile's stages fetch faster: 32 x 8192 x 8192 25.8 and 17.7 (16 rows 18.2 and 17.0).
 inline F8Tile choose_gemm_f8_tile(long M, long N, long K, bool codes, bool exact) {
-  (void)K;
-  if (codes) return kF8Tile128x256;
-  if (M <= 64) return kF8Few;
-  const int64_t large = (((int64_t)M + 255) / 256) * (((int64_t)N + 255) / 256);
-  const int64_t mid = (((int64_t)M + 127) / 128) * (((int64_t)N + 127) / 128);
-  return large >= 128 && !exact ? kF8Tile256x256 : mid >= 128 ? kF8Tile128 : kF8Deep64;
+  constexpr F8Cost kTiles[] = {{kF8Split64, 64, 64, 1, 242, 3700, 242, 3700},
+                               {kF8Deep128, 128, 128, 1, 600, 4300, 600, 4300},
+                               {kF8Tile128, 128, 128, 2, 1265, 2600, 834, 4000},
+                               {kF8Tile128x256, 128, 256, 1, 1000, 5200, 1000, 5200},
+                               {kF8Tile256x256, 256, 256, 1, 1900, 7300, 1900, 7300}};
+  constexpr F8Cost kExact[] = {{kF8Split64x4, 64, 64, 1, 311, 4800, 311, 4800}, {kF8Tile128, 128, 128, 2, 1930, 4900, 1165, 5560}};
+  constexpr F8Cost kCodes[] = {{kF8Codes64, 64, 256, 1, 1160, 5400, 1160, 5400}, {kF8Codes128, 128, 256, 1, 1950, 6800, 1950, 6800}};
+  if (M <= 32 && (double)N * (double)K <= (M <= 16 ? 4e7 : 1.6e7)) return kF8Few;
+  const F8Cost* const from = codes ? kCodes : exact ? kExact : kTiles;
+  const F8Cost* const to = codes ? kCodes + 2 : exact ? kExact + 2 : kTiles + 5;
+  const int64_t slices = ((int64_t)K + 127) / 128;
+  double least = -1.0;
+  F8Tile best = from->tile;
+  for (const F8Cost* t = from; t != to; ++t) {
+    const int64_t tiles = (((int64_t)M + t->bm - 1) / t->bm) * (((int64_t)N + t->bn - 1) / t->bn);
+    const int64_t k = (tiles + 255) / 256, rest = k % t->per;
+    const double cost = (double)(k / t->per) * ((double)t->slice * (double)slices + t->once) +
+                        (rest ? (double)t->alone_slice * (double)slices + t->alone_once : 0.0);
+    if (least < 0.0 || cost < least) {
+      best = t->tile;
+      least = cost;
+    }
+  }
+  return best;
 }
 
 }  // namespace sf
