@@ -242,6 +242,13 @@ __global__ __launch_bounds__(WM * WN * WK * 64, MINW) void gemm_f8_kernel(GemmF8
     // computed here: moved behind later MFMAs they would keep those's results alive as well
     asm volatile("" : "+v"(to));
   };
+  // EXACT: what part w of unit u is the first to multiply, one part ahead of it, so that no MFMA waits for a conversion:
+  // the rows' codes in the first column block, the columns' in the first rows. c: the half of it.
+  auto convert = [&](int u, int w, int c) __attribute__((always_inline)) {
+    const int i = u % IB, j = u / IB;
+    if (i == 0) b16[c][w] = f16_of(bf[0][c], w);
+    if (j == 0 && c == 0) a16[i][w] = f16_of(af[i], w);
+  };
   static_assert(TN % 2 == 0 && NU % 2 == 0, "the next slice starts with the buffers that this one started with");
   auto step = [&](auto st, int turn) __attribute__((always_inline)) {
     constexpr int S = decltype(st)::value;
@@ -287,13 +294,12 @@ __global__ __launch_bounds__(WM * WN * WK * 64, MINW) void gemm_f8_kernel(GemmF8
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           if constexpr (EXACT) {
-            if (i == 0) b16[c][w] = f16_of(bf[0][c], w);
-            if (j == 0 && c == 0) a16[i][w] = f16_of(af[i], w);
             d[u & 1][c] = mfma_f16(b16[c][w], a16[i][w], w ? d[u & 1][c] : f32x4{});
           } else {
             d[u & 1][c] = mfma_f8(bf[j & 1][c], af[i]);
           }
           __builtin_amdgcn_sched_barrier(0);
+          if constexpr (EXACT) convert((u + (w + 1) / PARTS) % NU, (w + 1) % PARTS, c);
           fmas((u + NU - 1) % NU, c, w, pending);
           // the stage's refill, spread over the last column's MFMAs
           constexpr int N = PARTS * 2 * IB;
@@ -323,6 +329,10 @@ __global__ __launch_bounds__(WM * WN * WK * 64, MINW) void gemm_f8_kernel(GemmF8
   for (int i = 0; i < (EXACT ? IB : IB - 1); ++i) load_a(st0, i);
   load_b(st0, 0);
   load_s(st0, sa);
+  if constexpr (EXACT) {
+    convert(0, 0, 0);
+    convert(0, 0, 1);
+  }
   int turn = 0;
   for (; turn + STAGES <= turns; turn += STAGES) round(turn);
   if (turn < turns) step(std::integral_constant<int, 0>{}, turn);

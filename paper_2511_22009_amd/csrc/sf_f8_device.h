@@ -22,12 +22,20 @@ __device__ __forceinline__ uint32_t pack_f8(float a, float b, float c, float d) 
 // A block's scale, top / 448, and what takes its values to codes.
 struct BlockF8 {
   float scale;  // NaN for a block that is not finite
-  float inv;    // 1 / scale, NaN too, 0 for a scale of 0, and -1 for one so small that differences are lost
+  float inv;    // 1 / scale to a step, NaN too, 0 for a scale of 0, and -1 for one so small that differences are lost
 };
+// The quotient by the reciprocal of 448, corrected once by its remainder: correctly rounded, as the
+// reciprocal is, wherever no part of it is below fp32's normal numbers. (With two divisions, 16384 x
+// 1152 rows leave their norms as codes after 54 us instead of 50.)
 __device__ __forceinline__ BlockF8 block_f8(uint32_t top_bits) {
-  BlockF8 b;
-  b.scale = top_bits < 0x7f800000u ? __uint_as_float(top_bits) / kF8Top : __uint_as_float(0x7fc00000u);
-  b.inv = b.scale == 0.0f ? 0.0f : b.scale < 0x1p-100f ? -1.0f : 1.0f / b.scale;
+  const float top = __uint_as_float(top_bits);
+  constexpr float r = 1.0f / kF8Top;
+  const float q = top * r, s = __builtin_fmaf(__builtin_fmaf(-q, kF8Top, top), r, q);
+  BlockF8 b{s, __builtin_amdgcn_rcpf(s)};
+  if (!(s >= 0x1p-90f && top_bits < 0x7f800000u)) {
+    b.scale = top_bits < 0x7f800000u ? top / kF8Top : __uint_as_float(0x7fc00000u);
+    b.inv = b.scale == 0.0f ? 0.0f : b.scale < 0x1p-90f ? -1.0f : b.scale;
+  }
   return b;
 }
 
@@ -43,7 +51,7 @@ __device__ __forceinline__ uint32_t code_f8_exact(float x, float s) {
   return sign | ((uint32_t)(r >> 49) - (1016u << 3));
 }
 
-// Which of two adjacent codes, byte E of lo and of hi, is x's in a block of scale s >= 2^-100: the sign of
+// Which of two adjacent codes, byte E of lo and of hi, is x's in a block of scale s >= 2^-90: the sign of
 // |x| - tie s is the exact one's, as one fma rounds it, and where that is 0 the even code has it.
 template <int E>
 __device__ __forceinline__ uint32_t nearer_f8(uint32_t lo, uint32_t hi, float x, float s) {
@@ -53,14 +61,14 @@ __device__ __forceinline__ uint32_t nearer_f8(uint32_t lo, uint32_t hi, float x,
   return over > 0.0f || (over == 0.0f && !(h >> (8 * E) & 1)) ? h : l;
 }
 
-// Codes of N values of a block. x inv (1 -+ 2^-22) lie on both sides of the exact quotient (inv and the
-// two products add less than 2^-22 of it), and rounding is monotone, so where both give the same code
-// it is the quotient's. Elsewhere, one value in some 2^17 and one in 16 where the scale is a power of
+// Codes of N values of a block. x inv (1 -+ 2^-21) lie on both sides of the exact quotient (inv, a step off at most, and
+// the two products add up to 2^-22 of it), and rounding is monotone, so where both give the same code
+// it is the quotient's. Elsewhere, one value in some 2^16 and one in 16 where the scale is a power of
 // two and the values are bf16, the exact quotient decides. (In fp64 it took 16384 x 1152 bf16
 // from 13 to 19 us.)
 template <int N>
 __device__ __forceinline__ void codes_f8(const float (&x)[N], const BlockF8& b, uint32_t (&out)[N / 4]) {
-  const float less = b.inv * (1.0f - 0x1p-22f), more = b.inv * (1.0f + 0x1p-22f);
+  const float less = b.inv * (1.0f - 0x1p-21f), more = b.inv * (1.0f + 0x1p-21f);
   uint32_t hi[N / 4], differ = 0;
 #pragma unroll
   for (int i = 0; i < N / 4; ++i) {
