@@ -116,7 +116,8 @@ __device__ __forceinline__ void normalise(float (&x)[NV][4], int kind, const Res
 
 // A piece of four of a row from column c on. WHOLE (D is a multiple of four): a lane past the row reads its last piece,
 // unconditionally, since a load under a lane's condition is waited for at once; what is past D is cleared
-// in use. Otherwise it is read element by element where D ends in it, and is 0 past D.
+// in use. Otherwise it is read element by element where D ends in it, and is 0 past D (reading the row's last
+// four there and moving them to their places took 2760 x 771 from 9.8 to 12.9 us).
 template <bool WHOLE, typename T>
 __device__ __forceinline__ void load_piece(Piece<T, 4>& p, const T* row, int c, int D) {
   if constexpr (WHOLE)
@@ -263,7 +264,7 @@ static void launch_rows(ResidualNormArgs a, hipStream_t s) {
   constexpr int ROWS = threads_of(WAVES) / 64 / WAVES;
   // as many workgroups as a CU holds at once, each as many rows of its sample as that takes (4096 x 1152 to codes: two
   // 17.9 us, four, which take turns, 21.3; 16384 x 768: three 32.6, four 27.9)
-  constexpr int64_t kGroups = NV > 4 ? 512 : 1024;
+  constexpr int64_t kGroups = NV > 4 ? 512 : NV > 3 && WAVES == 1 ? 768 : 1024;
   const int64_t rows = (int64_t)a.samples * a.tokens;
   const int turns = (int)std::min<int64_t>((rows + kGroups * ROWS - 1) / (kGroups * ROWS), (a.tokens + ROWS - 1) / ROWS);
   const int span = turns * ROWS;
@@ -291,6 +292,7 @@ static hipError_t launch_t(const ResidualNormArgs& a, hipStream_t s) {
   if (a.D % 4 == 0) {
     if (a.D <= 256) launch_rows<TH, TY, OUT, 1, 1, true>(a, s);
     else if (a.D <= 768 && many) launch_rows<TH, TY, OUT, 3, 1, true>(a, s);
+    else if (a.D <= 1024 && many) launch_rows<TH, TY, OUT, 4, 1, true>(a, s);
     else if (a.D <= 1280 && many) launch_rows<TH, TY, OUT, 5, 1, true>(a, s);
     else if (a.D <= 1024) launch_rows<TH, TY, OUT, 1, 4, true>(a, s);
     else if (a.D <= 2048) launch_rows<TH, TY, OUT, 2, 4, true>(a, s);
