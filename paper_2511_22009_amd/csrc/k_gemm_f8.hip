@@ -409,9 +409,8 @@ __global__ __launch_bounds__(WM * WN * WK * 64, MINW) void gemm_f8_kernel(GemmF8
     // the scale of a row's 128 columns: every wavefront's largest, joined in LDS
     static_assert(ON == kF8Block, "a tile holds whole blocks of outputs");
     constexpr int CP = WN + 1;
-    static_assert(BM * CP * 4 <= SROWS * 256 * CP, "tops");
-    uint32_t* const tops = (uint32_t*)(STAGES > 2 ? st2 : st1 + HALF * 32 * PITCH);
-    static_assert(STAGES > 2 || HALF * 32 * PITCH + BM * CP * 4 <= SLICE, "tops fit behind the parts");
+    uint32_t* const tops = (uint32_t*)(st1 + HALF * 32 * PITCH);
+    static_assert(HALF * 32 * PITCH + BM * CP * 4 <= SLICE, "the rows' largest fit behind the parts");
 #pragma unroll
     for (int i = 0; i < IB; ++i) {
       uint32_t t = 0;

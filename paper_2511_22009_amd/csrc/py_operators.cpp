@@ -620,23 +620,35 @@ PyObject* residual_norm(PyObject* const* args) {
   return pair(given_or(args[12], h_out), second);
 }
 
-// check, raw_stream and the addresses of the entry points
-PyObject* bind(PyObject* const* args) {
-  void* at[8];
-  for (int i = 0; i < 8; ++i) {
-    at[i] = PyLong_AsVoidPtr(args[2 + i]);
+template <int N>
+void addresses(PyObject* const* args, void* (&at)[N]) {
+  for (int i = 0; i < N; ++i) {
+    at[i] = PyLong_AsVoidPtr(args[i]);
     if (!at[i] && PyErr_Occurred()) throw Raised{};
   }
+}
+
+// check, raw_stream and the addresses of the first four entry points
+PyObject* bind(PyObject* const* args) {
+  void* at[4];
+  addresses(args + 2, at);
   g_quantize_rows = (decltype(g_quantize_rows))at[0];
   g_matmul_i8 = (decltype(g_matmul_i8))at[1];
   g_rotate = (decltype(g_rotate))at[2];
   g_qk_norm_rotate = (decltype(g_qk_norm_rotate))at[3];
-  g_quantize_f8 = (decltype(g_quantize_f8))at[4];
-  g_matmul_f8 = (decltype(g_matmul_f8))at[5];
-  g_gated_matmul_f8 = (decltype(g_gated_matmul_f8))at[6];
-  g_residual_norm = (decltype(g_residual_norm))at[7];
   g_check = Py_NewRef(args[0]);
   g_raw_stream = Py_NewRef(args[1]);
+  return Py_NewRef(Py_None);
+}
+
+// The addresses of those in 8-bit floating point, after bind().
+PyObject* bind_f8(PyObject* const* args) {
+  void* at[4];
+  addresses(args, at);
+  g_quantize_f8 = (decltype(g_quantize_f8))at[0];
+  g_matmul_f8 = (decltype(g_matmul_f8))at[1];
+  g_gated_matmul_f8 = (decltype(g_gated_matmul_f8))at[2];
+  g_residual_norm = (decltype(g_residual_norm))at[3];
   return Py_NewRef(Py_None);
 }
 
@@ -657,7 +669,8 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-PyMethodDef kMethods[] = {{"bind", (PyCFunction)(void (*)(void))call<bind, 10>, METH_FASTCALL, nullptr},
+PyMethodDef kMethods[] = {{"bind", (PyCFunction)(void (*)(void))call<bind, 6>, METH_FASTCALL, nullptr},
+                          {"bind_f8", (PyCFunction)(void (*)(void))call<bind_f8, 4>, METH_FASTCALL, nullptr},
                           {"quantize_rows", (PyCFunction)(void (*)(void))call<quantize_rows, 3>, METH_FASTCALL, nullptr},
                           {"matmul_i8", (PyCFunction)(void (*)(void))call<matmul_i8, 7>, METH_FASTCALL, nullptr},
                           {"rotate", (PyCFunction)(void (*)(void))call<rotate, 5>, METH_FASTCALL, nullptr},

@@ -35,10 +35,13 @@ def _raw_stream(index):
     return torch.cuda.current_stream(index).cuda_stream
 
 
+def _entries(*names):
+    return (ctypes.cast(getattr(load_library(), "sf_" + n), ctypes.c_void_p).value for n in names)
+
+
 _ext.bind(_check, getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream),
-          *(ctypes.cast(getattr(load_library(), "sf_" + n), ctypes.c_void_p).value
-            for n in ("quantize_rows", "matmul_i8", "rotate", "qk_norm_rotate", "quantize_f8", "matmul_f8", "gated_matmul_f8",
-                      "residual_norm")))
+          *_entries("quantize_rows", "matmul_i8", "rotate", "qk_norm_rotate"))
+_ext.bind_f8(*_entries("quantize_f8", "matmul_f8", "gated_matmul_f8", "residual_norm"))
 
 
 def _aside(stream, tensors, call, *args):

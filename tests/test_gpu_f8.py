@@ -245,7 +245,7 @@ def check_gated(M, N, K, dtype, name, bias, narrow=False):
 @pytest.mark.parametrize("name", ["silu", "gelu_tanh"])
 @pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 2048, 768), (16, 17, 33), (20, 130, 129), (64, 300, 128), (65, 33, 300), (200, 129, 144),
                                    (300, 700, 1000), (513, 64, 8320), (1025, 2100, 260), (2304, 2176, 768), (32, 1000, 1152), (800, 600, 140),
-                                   (4699, 393, 1300), (646, 2750, 260)])
+                                   (4699, 393, 1300), (646, 2750, 260), (1610, 303, 520)])
 def test_gated(M, N, K, name, dtype):
     check_gated(M, N, K, dtype, name, bias=(M + N) % 2 == 1)
     check_gated(M, N, K, dtype, name, bias=(M + N) % 2 == 0, narrow=True)
@@ -468,6 +468,25 @@ def test_feed_forward_in_a_graph(S, T):
             assert torch.equal(a, b)
 
 
+def test_two_streams_at_once():
+    """The same chain on two streams, its calls in turn, many times over: the bits of one alone."""
+    g = gen(42)
+    blocks = [make_block(g, 2, 300, 256, 640), make_block(g, 1, 900, 384, 1000)]
+    want = [[t.clone() for t in flat(feed_forward(*b, F8))] for b in blocks]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(6):
+        for n, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[n].append(feed_forward(*blocks[n], F8))
+    torch.cuda.synchronize()
+    for n in range(2):
+        for result in got[n]:
+            for a, b in zip(flat(result), want[n]):
+                assert torch.equal(a, b)
+
+
 def test_feed_forward_on_a_stream():
     """Every call on a stream that is not the current one, its inputs dropped at once."""
     from paper_2511_22009_amd import gated_matmul_f8, matmul_f8, quantize_f8, residual_norm
@@ -557,3 +576,38 @@ def test_empty_calls():
     assert q.shape == (2, 0) and s.shape == (2, 0)
     h, out = residual_norm(torch.zeros((3, 0, 8), device="cuda"), torch.zeros((3, 0, 8), device="cuda"), pre="rms")
     assert h.shape == (3, 0, 8) and out.shape == (3, 0, 8)
+
+
+def test_other_threads_run_while_a_call_is_under_way(tmp_path):
+    """In the place of the library's entry points stands a function that waits (5 s at most) for what
+    another Python thread does. Nothing is launched."""
+    import ctypes
+    import subprocess
+    import threading
+
+    from paper_2511_22009_amd import operators
+    from test_gpu_operators_edges import WAITS
+    src, lib = str(tmp_path / "w.cpp"), str(tmp_path / "w.so")
+    with open(src, "w") as f:
+        f.write(WAITS)
+    subprocess.run(["g++", "-shared", "-fPIC", "-O1", src, "-o", lib], check=True)
+    w = ctypes.CDLL(lib)
+    flag = ctypes.c_int.in_dll(w, "flag")
+    x = randn(gen(107), 4, 256)
+    a, sa = operators.quantize_f8(x)
+    b, sb = operators.quantize_f8(x, block_rows=128)
+    address = ctypes.cast(w.wait_for_flag, ctypes.c_void_p).value
+    names = ("quantize_f8", "matmul_f8", "gated_matmul_f8", "residual_norm")
+    entries = [ctypes.cast(getattr(operators.load_library(), "sf_" + n), ctypes.c_void_p).value for n in names]
+    try:
+        operators._ext.bind_f8(*[address] * 4)
+        for call in (lambda: operators.quantize_f8(x), lambda: operators.matmul_f8(a, sa, b, sb),
+                     lambda: operators.gated_matmul_f8(a, sa, b, sb, b, sb, dtype=F8), lambda: operators.residual_norm(x, x, pre="rms")):
+            flag.value = 0
+            setter = threading.Timer(0.02, lambda: setattr(flag, "value", 1))
+            setter.start()
+            call()                                     # SFError after 5 s if no other thread could run
+            setter.join()
+    finally:
+        operators._ext.bind_f8(*entries)
+    check_quantize(x, 1)                               # the library's own again
