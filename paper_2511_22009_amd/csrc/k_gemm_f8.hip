@@ -396,8 +396,8 @@ __global__ __launch_bounds__(WM * WN * WK * 64, MINW) void gemm_f8_kernel(GemmF8
     }
   // Every wavefront passes its part of the tile through LDS of its own, 32 rows at a time, so that
   // stores leave in whole rows of the part
-  typedef uint32_t out16 __attribute__((ext_vector_type(4), aligned(1)));
-  constexpr int ES = OUT == F8_F32 ? 4 : OUT == F8_BF16 ? 2 : 1;
+  typedef uint32_t out16 __attribute__((ext_vector_type(4), aligned(2)));
+  constexpr int ES = OUT == F8_F32 ? 4 : 2;
   constexpr int E = 16 / ES, JG = OUT == F8_F32 ? 1 : TO;
   constexpr int PITCH = JG * 32 * ES + 16, CPW = JG * 32 / E, HALF = (WM * WN + 1) / 2;
   static_assert(HALF * 32 * PITCH <= WK * SLICE, "the parts of half the wavefronts fit a stage");
@@ -409,8 +409,8 @@ __global__ __launch_bounds__(WM * WN * WK * 64, MINW) void gemm_f8_kernel(GemmF8
     // the scale of a row's 128 columns: every wavefront's largest, joined in LDS
     static_assert(ON == kF8Block, "a tile holds whole blocks of outputs");
     constexpr int CP = WN + 1;
-    uint32_t* const tops = (uint32_t*)(st1 + HALF * 32 * PITCH);
-    static_assert(HALF * 32 * PITCH + BM * CP * 4 <= SLICE, "the rows' largest fit behind the parts");
+    uint32_t* const tops = (uint32_t*)st1;
+    static_assert(BM * CP * 4 <= SLICE, "the rows' largest fit a stage");
 #pragma unroll
     for (int i = 0; i < IB; ++i) {
       uint32_t t = 0;
@@ -436,6 +436,37 @@ __global__ __launch_bounds__(WM * WN * WK * 64, MINW) void gemm_f8_kernel(GemmF8
       if (wn == 0 && g == 0 && m < a.M) a.out_scale[(int64_t)m * a.os_row + (int64_t)(n0 / kF8Block) * a.os_block] = bq[i].scale;
     }
   }
+  if constexpr (OUT == F8_CODES) {
+    // the wavefronts' pieces of a row join in LDS, so that its 128 codes leave as one line (in pieces of
+    // 32 bytes, 16384 x 4608 codes took 99 MB of writes instead of 78)
+    constexpr int ROW = ON + 16;
+    static_assert(BM * ROW <= SLICE, "the tile's codes fit a stage");
+#pragma unroll
+    for (int i = 0; i < IB; ++i) {
+      float v[8 * TO];
+#pragma unroll
+      for (int e = 0; e < 8 * TO; ++e) v[e] = acc[i][e / 8][e / 4 % 2][e % 4];
+      uint32_t q[2 * TO];
+      codes_f8(v, bq[i], q);
+      char* const p = st0 + (wm * TM * 32 + i * 16 + l16) * ROW + wn * WON + 4 * g;
+#pragma unroll
+      for (int c = 0; c < 2 * TO; ++c) *(uint32_t*)(p + c * 16) = q[c];
+    }
+    __syncthreads();
+    for (int c = tid; c < BM * ON / 16; c += NT) {
+      const int r = c / (ON / 16), m = m0 + r, n = n0 + c % (ON / 16) * 16;
+      const u32x4 o = *(const u32x4*)(st0 + r * ROW + c % (ON / 16) * 16);
+      uint8_t* const to = (uint8_t*)a.out + (int64_t)m * a.ldo + n;
+      if (m < a.M && n + 16 <= a.N) {
+        __builtin_nontemporal_store(o, (u32x4*)to);  // rows of codes start at multiples of 16
+      } else if (m < a.M) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (n + e < a.N) to[e] = (uint8_t)(o[e >> 2] >> (8 * (e & 3)));
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int j0 = 0; j0 < TO; j0 += JG) {
 #pragma unroll
@@ -444,23 +475,14 @@ __global__ __launch_bounds__(WM * WN * WK * 64, MINW) void gemm_f8_kernel(GemmF8
       for (int h = 0; h < 2; ++h) {
         const auto& rows = acc[2 * i + h];
         char* const p = part + (16 * h + l16) * PITCH + 4 * g * ES;
-        uint32_t q[2 * JG];
-        if constexpr (OUT == F8_CODES) {
-          float v[8 * JG];
-#pragma unroll
-          for (int e = 0; e < 8 * JG; ++e) v[e] = rows[j0 + e / 8][e / 4 % 2][e % 4];
-          codes_f8(v, bq[2 * i + h], q);
-        }
 #pragma unroll
         for (int c = 0; c < 2 * JG; ++c) {
           const f32x4 v = rows[j0 + c / 2][c % 2];
           char* const to = p + c * 16 * ES;
           if constexpr (OUT == F8_F32)
             *(f32x4*)to = v;
-          else if constexpr (OUT == F8_BF16)
-            *(uint2*)to = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
           else
-            *(uint32_t*)to = q[c];
+            *(uint2*)to = uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
         }
       }
       __builtin_amdgcn_wave_barrier();
@@ -479,10 +501,8 @@ __global__ __launch_bounds__(WM * WN * WK * 64, MINW) void gemm_f8_kernel(GemmF8
             if (n + e < a.N) {
               if constexpr (OUT == F8_F32)
                 ((float*)to)[e] = __uint_as_float(o[e]);
-              else if constexpr (OUT == F8_BF16)
-                ((uint16_t*)to)[e] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
               else
-                ((uint8_t*)to)[e] = (uint8_t)(o[e >> 2] >> (8 * (e & 3)));
+                ((uint16_t*)to)[e] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
             }
         }
       }
