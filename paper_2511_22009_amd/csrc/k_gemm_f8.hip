@@ -92,13 +92,16 @@ __global__ __launch_bounds__(WM * WN * WK * 64, MINW) void gemm_f8_kernel(GemmF8
   static_assert(TM * WM * 32 == BM && TN * WN * 32 == BN, "wave grid must tile the block");
   constexpr int ATOT = BM * CPR, BTOT = BN * CPR;
   static_assert(ATOT % NT == 0 && BTOT % NT == 0, "whole rounds of chunks per slice");
-  constexpr int ACH = ATOT / NT, BCH = BTOT / NT, LPT = ACH + BCH + 1;
   static_assert(STAGES >= 2 && STAGES <= 4, "two to four stages");
+  // Two workgroups of 64 x 256 fill a CU's LDS with codes alone: each lane fetches its rows' scales itself then.
+  constexpr bool OWN_SCALES = 2 * STAGES * WK * (ATOT + BTOT) * 16 == 160 * 1024;
   constexpr int SCALES = (ATOT + BTOT) * 16, SROWS = (BM + 63) / 64;
-  constexpr int SLICE = SCALES + SROWS * 256;
+  constexpr int SLICE = SCALES + (OWN_SCALES ? 0 : SROWS * 256);
+  constexpr int ACH = ATOT / NT, BCH = BTOT / NT, LPT = ACH + BCH + (OWN_SCALES ? 0 : 1);
   static_assert(SROWS <= WM * WN, "a wavefront per 64 scales");
   static_assert(STAGES * WK * SLICE <= 160 * 1024, "stages do not fit in LDS");
   static_assert(WK == 1 || OUT != F8_CODES, "the scales of codes are joined over a tile's only group");
+  static_assert(WK == 1 || !OWN_SCALES, "a lane's own scales go from slice to slice");
   // output columns of the tile and of a wavefront; those of a wavefront lie in one block of weights' rows
   constexpr int ON = GATED ? BN / 2 : BN, WON = ON / WN;
   static_assert(WON <= kF8Block && kF8Block % WON == 0, "a wavefront's columns share a scale");
@@ -147,6 +150,7 @@ __global__ __launch_bounds__(WM * WN * WK * 64, MINW) void gemm_f8_kernel(GemmF8
   const __amdgpu_buffer_rsrc_t ra = buffer_rsrc(a.a.q + (int64_t)m0 * a.a.ld, (uint32_t)((min(a.M - m0, BM) - 1) * a.a.ld + kend));
   const __amdgpu_buffer_rsrc_t rb = buffer_rsrc((wave_up ? a.up.q : a.b.q) + (int64_t)n0 * b_ld, (uint32_t)(o_rows * b_ld + kend));
   const __amdgpu_buffer_rsrc_t ru = GATED && !BY_WAVE ? buffer_rsrc(a.up.q + (int64_t)n0 * a.up.ld, (uint32_t)(o_rows * a.up.ld + kend)) : rb;
+  int sa_left = nk;  // OWN_SCALES: slices whose scales are still to be fetched
   const float* sa_at = a.a.scale + (int64_t)m0 * a.a.s_row + min(group, nk - 1) * a.a.s_block;  // of the next slice to be fetched
   const uint32_t s_bytes = (uint32_t)(min(a.M - m0, BM) - 1) * (uint32_t)a.a.s_row * 4 + 4;
   const int s_wave = wave % SROWS;
@@ -232,6 +236,16 @@ __global__ __launch_bounds__(WM * WN * WK * 64, MINW) void gemm_f8_kernel(GemmF8
     for (int c = 0; c < 2; ++c) bf[EXACT ? 0 : j & 1][c] = frag(cur + (j % TN * 2 + c) * 16 * CPR * 16, b_at);
   };
   auto load_s = [&](const char* cur, float (&s)[IB]) __attribute__((always_inline)) {
+    if constexpr (OWN_SCALES) {
+      const __amdgpu_buffer_rsrc_t r = buffer_rsrc(sa_at, s_bytes);
+#pragma unroll
+      for (int i = 0; i < IB; ++i)
+        s[i] = __uint_as_float(
+            __builtin_amdgcn_raw_buffer_load_b32(r, (wm * TM * 32 + i * 16 + l16) * (int)a.a.s_row * 4, 0, 0));
+      sa_left -= 1;
+      sa_at += sa_left > 0 ? a.a.s_block : 0;
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < IB; ++i) s[i] = *(const float*)(cur + mine + SCALES + (wm * TM * 32 + i * 16 + l16) * 4);
   };
@@ -662,8 +676,7 @@ static void launch_few(const GemmF8Args& a, hipStream_t s) {
   X(kF8Split64x4, 64, 64, 2, 1, 4, 2, 1)     \
   X(kF8Deep128, 128, 128, 4, 2, 1, 4, 2)     \
   X(kF8Tile128, 128, 128, 2, 2, 1, 2, 2)     \
-  X(kF8Codes64, 64, 256, 2, 4, 1, 3, 2)      \
-  X(kF8Codes128, 128, 256, 2, 4, 1, 2, 2)    \
+  X(kF8Codes64, 64, 256, 1, 4, 1, 2, 2)      \
   X(kF8Tile128x256, 128, 256, 2, 4, 1, 3, 2) \
   X(kF8Tile256x256, 256, 256, 4, 2, 1, 2, 2)
 

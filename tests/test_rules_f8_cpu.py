@@ -19,7 +19,7 @@ int main() {
   }
 }
 """
-F8_NAMES = ["few", "split64", "split64x4", "deep128", "tile128", "tile128x256", "tile256x256", "codes64", "codes128"]
+F8_NAMES = ["few", "split64", "split64x4", "deep128", "tile128", "tile128x256", "tile256x256", "codes64"]
 
 
 def _f8_tiles(exe, calls):
@@ -52,4 +52,4 @@ def test_f8_sizes_of_the_gpu_tests_reach_every_tile(tmp_path_factory):
     both = [(m, 2 * n, k) for m, n, k in gated]
     assert set(_f8_tiles(exe, [(*s, 0, 0) for s in both])[0]) == values
     assert set(_f8_tiles(exe, [(*s, 0, 1) for s in both])[0]) == {"few", "split64x4", "tile128"}
-    assert set(_f8_tiles(exe, [(*s, 1, 1) for s in both])[0]) == {"few", "codes64", "codes128"}
+    assert set(_f8_tiles(exe, [(*s, 1, 1) for s in both])[0]) == {"few", "codes64"}
