@@ -672,10 +672,13 @@ static void launch_few(const GemmF8Args& a, hipStream_t s) {
 
 // Tiles: BM x BN, wave grid, groups of it, LDS stages, wavefronts per SIMD.
 #define SF_F8_TILES(X)                       \
+  X(kF8Split32, 32, 64, 1, 1, 2, 3, 1)       \
+  X(kF8Split32x4, 32, 64, 1, 1, 4, 3, 1)     \
   X(kF8Split64, 64, 64, 2, 1, 2, 4, 1)       \
   X(kF8Split64x4, 64, 64, 2, 1, 4, 2, 1)     \
   X(kF8Deep128, 128, 128, 4, 2, 1, 4, 2)     \
   X(kF8Tile128, 128, 128, 2, 2, 1, 2, 2)     \
+  X(kF8Codes32, 32, 256, 1, 4, 1, 2, 2)      \
   X(kF8Codes64, 64, 256, 1, 4, 1, 2, 2)      \
   X(kF8Tile128x256, 128, 256, 2, 4, 1, 3, 2) \
   X(kF8Tile256x256, 256, 256, 4, 2, 1, 2, 2)

@@ -67,11 +67,24 @@ inline I8Tile choose_gemm_i8_tile(long M, long N, long K, bool heavy, bool resid
 
 // Tiles of the products of e4m3 codes. Outputs that are codes need a tile that holds whole blocks of 128
 // outputs, gated: 256 columns of both projections. `exact`: sums in fp32 (outputs in fp32, or codes).
-enum F8Tile { kF8Few, kF8Split64, kF8Split64x4, kF8Deep128, kF8Tile128, kF8Tile128x256, kF8Tile256x256, kF8Codes64 };
+enum F8Tile {
+  kF8Few,
+  kF8Split32,
+  kF8Split32x4,
+  kF8Split64,
+  kF8Split64x4,
+  kF8Deep128,
+  kF8Tile128,
+  kF8Tile128x256,
+  kF8Tile256x256,
+  kF8Codes32,
+  kF8Codes64
+};
 constexpr bool f8_has_tile(F8Tile t, bool codes, bool exact) {
-  return codes   ? t == kF8Codes64
-         : exact ? t == kF8Split64x4 || t == kF8Tile128
-                 : t == kF8Split64 || t == kF8Deep128 || t == kF8Tile128 || t == kF8Tile128x256 || t == kF8Tile256x256;
+  return codes   ? t == kF8Codes32 || t == kF8Codes64
+         : exact ? t == kF8Split32x4 || t == kF8Split64x4 || t == kF8Tile128
+                 : t == kF8Split32 || t == kF8Split64 || t == kF8Deep128 || t == kF8Tile128 || t == kF8Tile128x256 ||
+                       t == kF8Tile256x256;
 }
 
 // What the workgroups of a tile cost that a CU runs side by side (`per` of them, or one alone), in ns: so much per
@@ -88,24 +101,30 @@ struct F8Cost {
 //   * 128 x 128 in pairs where rounds of the large tiles are left half empty: 16384 x 1152 x 4608 123, 256 x 256 129.
 //   * 128 x 128 with four stages, eight wavefronts, one per CU, for single rounds of it: 2048 x 2048 x 4096 23, in pairs
 //     31, 128 x 256 37.
-//   * 64 x 64 with K split over two groups of wavefronts for the smallest grids: 512 x 1024 x 4352 11.6, over four
-//     13.3, not split 13.9, 128 x 128 30; in fp32 517 x 1001 x 4321 over four 16.0, not split 25.
-//   * codes: 64 x 256, two workgroups a CU, at every size: gated 16384 x 2 x 4608 x 1152 388, 1024 x 2 x 4608 x 1152 33,
-//     300 x 2 x 2048 x 768 11.7; 128 x 256 with eight wavefronts, one a CU, 398, 43 and 16.6; 64 x 256 of that kind 489, 42
-//     and 11.6.
+//   * 64 x 64 with K split over two groups of wavefronts for small grids: 1024 x 1024 x 4096 11.5, over four 13.3, 32 x 64
+//     13.5; not split 13.9 at 512 x 1024 x 4352, 128 x 128 there 30; in fp32 517 x 1001 x 4321 over four 16.3, not split 25.
+//   * 32 x 64 with one wavefront to a group, two groups (fp32: four) for the smallest: 512 x 1024 x 4352 10.2, 64 x 64 11.8;
+//     300 x 1152 x 1152 5.6 and 6.3; in fp32 100 x 1152 x 4608 11.7 and 14.3, 300 x 1152 x 1152 7.3 and 8.2. With the
+//     groups of the other type, bf16 9.8 to 10.7, 6.3, fp32 512 x 1024 x 4096 14.7 and not 11.7.
+//   * codes: 64 x 256, two workgroups a CU: gated 16384 x 2 x 4608 x 1152 388, 1024 x 2 x 4608 x 1152 33; 128 x 256 with
+//     eight wavefronts, one a CU, 398 and 43; 64 x 256 of that kind 489 and 42. 32 x 256 while a CU gets one or
+//     two of them: 300 x 2 x 1152 x 1152 11.2, 64 x 256 14.6; 2048 x 2 x 2048 x 1024 28 and 23.
 // Up to 32 rows the weights' bytes count, which more and smaller workgroups fetch sooner: 32 x 3456 x 1152 4.4,
 // 64 x 64 6.1; but long weights that a tile's stages fetch faster: 32 x 8192 x 8192 25.8 and 17.7 (16 rows 18.2 and 17.0).
 inline F8Tile choose_gemm_f8_tile(long M, long N, long K, bool codes, bool exact) {
-  constexpr F8Cost kTiles[] = {{kF8Split64, 64, 64, 1, 242, 3700, 242, 3700},
+  constexpr F8Cost kTiles[] = {{kF8Split32, 32, 64, 2, 279, 4540, 193, 3740},
+                               {kF8Split64, 64, 64, 1, 242, 3700, 242, 3700},
                                {kF8Deep128, 128, 128, 1, 600, 4300, 600, 4300},
                                {kF8Tile128, 128, 128, 2, 1265, 2600, 834, 4000},
                                {kF8Tile128x256, 128, 256, 1, 1000, 5200, 1000, 5200},
                                {kF8Tile256x256, 256, 256, 1, 1900, 7300, 1900, 7300}};
-  constexpr F8Cost kExact[] = {{kF8Split64x4, 64, 64, 1, 311, 4800, 311, 4800}, {kF8Tile128, 128, 128, 2, 1930, 4900, 1165, 5560}};
+  constexpr F8Cost kExact[] = {{kF8Split32x4, 32, 64, 1, 215, 4800, 215, 4800},
+                               {kF8Split64x4, 64, 64, 1, 311, 4800, 311, 4800},
+                               {kF8Tile128, 128, 128, 2, 1930, 4900, 1165, 5560}};
+  constexpr F8Cost kCodes[] = {{kF8Codes32, 32, 256, 2, 1096, 6570, 776, 4510}, {kF8Codes64, 64, 256, 2, 1891, 7940, 1092, 6700}};
   if (M <= 32 && (double)N * (double)K <= (M <= 16 ? 4e7 : 1.6e7)) return kF8Few;
-  if (codes) return kF8Codes64;
-  const F8Cost* const from = exact ? kExact : kTiles;
-  const F8Cost* const to = exact ? kExact + 2 : kTiles + 5;
+  const F8Cost* const from = codes ? kCodes : exact ? kExact : kTiles;
+  const F8Cost* const to = codes ? kCodes + 2 : exact ? kExact + 3 : kTiles + 6;
   const int64_t slices = ((int64_t)K + 127) / 128;
   double least = -1.0;
   F8Tile best = from->tile;

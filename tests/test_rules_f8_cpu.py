@@ -19,7 +19,7 @@ int main() {
   }
 }
 """
-F8_NAMES = ["few", "split64", "split64x4", "deep128", "tile128", "tile128x256", "tile256x256", "codes64"]
+F8_NAMES = ["few", "split32", "split32x4", "split64", "split64x4", "deep128", "tile128", "tile128x256", "tile256x256", "codes32", "codes64"]
 
 
 def _f8_tiles(exe, calls):
@@ -47,9 +47,9 @@ def test_f8_sizes_of_the_gpu_tests_reach_every_tile(tmp_path_factory):
                  for d in f.decorator_list if d.args[0].value == "M,N,K")
     exe = _compiled(tmp_path_factory, "f8_sizes", F8_TILES)
     values = set(_f8_tiles(exe, [(*s, 0, 0) for s in sizes])[0])
-    assert values == {"few", "split64", "deep128", "tile128", "tile128x256", "tile256x256"}
-    assert set(_f8_tiles(exe, [(*s, 0, 1) for s in sizes])[0]) == {"few", "split64x4", "tile128"}
+    assert values == {"few", "split32", "split64", "deep128", "tile128", "tile128x256", "tile256x256"}
+    assert set(_f8_tiles(exe, [(*s, 0, 1) for s in sizes])[0]) == {"few", "split32x4", "split64x4", "tile128"}
     both = [(m, 2 * n, k) for m, n, k in gated]
     assert set(_f8_tiles(exe, [(*s, 0, 0) for s in both])[0]) == values
-    assert set(_f8_tiles(exe, [(*s, 0, 1) for s in both])[0]) == {"few", "split64x4", "tile128"}
-    assert set(_f8_tiles(exe, [(*s, 1, 1) for s in both])[0]) == {"few", "codes64"}
+    assert set(_f8_tiles(exe, [(*s, 0, 1) for s in both])[0]) == {"few", "split32x4", "split64x4", "tile128"}
+    assert set(_f8_tiles(exe, [(*s, 1, 1) for s in both])[0]) == {"few", "codes32", "codes64"}
