@@ -12,7 +12,15 @@
 // lost, 15/8 2^-11 becomes 7/4 2^-11; products eight apart are added in fp32): 1.5e-5 of the result on codes of
 // a bell, a hundredth of what rounding it to bf16 costs. Outputs in fp32, and the fp32 scales of outputs that
 // are codes, are for what comes after to see more than that: the operands' codes are converted to fp16, which holds
-// every one, and multiplied by v_mfma_f32_32x32x16_f16 at half the rate (1e-8 on the same codes).
+// every one, and multiplied by v_mfma_f32_16x16x32_f16 at half the rate (1e-8 on the same codes).
+//
+// What bounds it. Large products in bf16: the matrix cores at the clock that their power leaves, 8192^3 492 us, 2235
+// TFLOP/s (a library's product with one scale per operand, without the fmas, 409). Outputs that are exact: the vector
+// unit, which converts 128 pairs of codes and runs 64 fmas of a wavefront's 64 x 64 outputs a slice beside 1024 cycles of
+// matrix work: gated 16384 x 2 x 4608 x 1152 to codes 333 us, to fp32 335, to bf16 177. Single rounds of tiles:
+// the first slices and the outputs of all at once (gated 4096 x 2 x 2048 x 768 17 us). Few tiles: a turn's latencies and the
+// L2's rate to one CU (517 x 1001 x 4321 fp32 15). Few rows: the weights' bytes and one chain of latencies (8 x 2 x 2048 x 768
+// 4.7, the host's part of a call among them).
 #include "sf_f8_device.h"
 #include "sf_ops_rules.h"
 
@@ -527,17 +535,16 @@ __global__ __launch_bounds__(WM * WN * WK * 64, MINW) void gemm_f8_kernel(GemmF8
 
 // Few rows, up to 16 MT: the weights are read once and bound it, so a wavefront takes only sixteen columns (gated:
 // of both projections) and a KS-th of the blocks of K, straight from memory to the matrix cores, and the sums
-// are joined in LDS in a fixed order. A workgroup has CG such columns: one, so that there are many
-// workgroups, and eight, the 128 outputs that share a scale, where the outputs are codes.
-template <int MT, int CG, int KS, F8Out OUT, F8Act ACT>
-__global__ __launch_bounds__(CG * KS * 64) void few_f8_kernel(GemmF8Args a) {
+// are joined in LDS in a fixed order. Outputs that are codes have no such kernel: eight such runs of columns, the 128
+// outputs that share a scale, in one workgroup took 20.7 us for 32 x 2 x 1152 x 1152, a tile of 32 x 256 9.6.
+template <int MT, int KS, F8Out OUT, F8Act ACT>
+__global__ __launch_bounds__(KS * 64) void few_f8_kernel(GemmF8Args a) {
   constexpr bool GATED = ACT != F8_NONE;
-  constexpr int P = GATED ? 2 : 1, AHEAD = MT * P * CG > 2 ? 2 : 4;
-  static_assert(OUT != F8_CODES || CG * 16 == kF8Block, "a workgroup holds a block of outputs");
-  __shared__ __attribute__((aligned(16))) f32x4 sums[KS][CG][P][MT][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int l16 = lane & 15, g = lane >> 4, cg = wave % CG, ks = wave / CG;
-  const int n0 = min((int)blockIdx.x * CG + cg, (a.N - 1) / 16) * 16;  // past the last column: the last ones again
+  constexpr int P = GATED ? 2 : 1, AHEAD = MT * P > 2 ? 2 : 4;
+  __shared__ __attribute__((aligned(16))) f32x4 sums[KS][P][MT][64];
+  const int lane = threadIdx.x & 63, ks = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const int n0 = (int)blockIdx.x * 16;
   const int nk = (a.K + kF8Block - 1) / kF8Block;
   // the resources hold the tile's rows to the end of the chunk that K ends in; rows past the last are it
   const int kend = (a.K + 15) & ~15;
@@ -610,18 +617,18 @@ __global__ __launch_bounds__(CG * KS * 64) void few_f8_kernel(GemmF8Args a) {
 #pragma unroll
   for (int p = 0; p < P; ++p)
 #pragma unroll
-    for (int t = 0; t < MT; ++t) sums[ks][cg][p][t][lane] = acc[p][t];
+    for (int t = 0; t < MT; ++t) sums[ks][p][t][lane] = acc[p][t];
   __syncthreads();
   // four adjacent columns of a row to a thread
-  for (int e = threadIdx.x; e < MT * 16 * CG * 4; e += CG * KS * 64) {
-    const int c = e % (CG * 4), m = e / (CG * 4) % 16, t = e / (CG * 64);
-    const int row = t * 16 + m, n = (int)blockIdx.x * CG * 16 + c * 4, left = a.N - n;
+  for (int e = threadIdx.x; e < MT * 64; e += KS * 64) {
+    const int c = e % 4, m = e / 4 % 16, t = e / 64;
+    const int row = t * 16 + m, n = n0 + c * 4, left = a.N - n;
     f32x4 v[P];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      v[p] = sums[0][c >> 2][p][t][(c & 3) * 16 + m];
+      v[p] = sums[0][p][t][c * 16 + m];
 #pragma unroll
-      for (int k = 1; k < KS; ++k) v[p] += sums[k][c >> 2][p][t][(c & 3) * 16 + m];
+      for (int k = 1; k < KS; ++k) v[p] += sums[k][p][t][c * 16 + m];
     }
     float x[4];
 #pragma unroll
@@ -634,40 +641,25 @@ __global__ __launch_bounds__(CG * KS * 64) void few_f8_kernel(GemmF8Args a) {
         x[i] = act_f8<ACT>(x[i]) * u;
       }
     }
-    if constexpr (OUT == F8_CODES) {
-      uint32_t top = 0;
+    if (row >= a.M) continue;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) top = max(top, i < left ? abs_bits(x[i]) : 0u);
-      const BlockF8 b = block_f8(max_of_32(top));  // of 32 threads, which share a row
-      uint32_t q[1];
-      codes_f8(x, b, q);
-      if (row >= a.M) continue;
-      if (c == 0) a.out_scale[(int64_t)row * a.os_row + (int64_t)blockIdx.x * a.os_block] = b.scale;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i < left) ((uint8_t*)a.out)[(int64_t)row * a.ldo + n + i] = (uint8_t)(q[0] >> (8 * i));
-    } else {
-      if (row >= a.M) continue;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i < left) {
-          if constexpr (OUT == F8_F32)
-            ((float*)a.out)[(int64_t)row * a.ldo + n + i] = x[i];
-          else
-            ((bf16*)a.out)[(int64_t)row * a.ldo + n + i] = (bf16)x[i];
-        }
-    }
+    for (int i = 0; i < 4; ++i)
+      if (i < left) {
+        if constexpr (OUT == F8_F32)
+          ((float*)a.out)[(int64_t)row * a.ldo + n + i] = x[i];
+        else
+          ((bf16*)a.out)[(int64_t)row * a.ldo + n + i] = (bf16)x[i];
+      }
   }
 }
 
 template <F8Out OUT, F8Act ACT>
 static void launch_few(const GemmF8Args& a, hipStream_t s) {
-  constexpr int CG = OUT == F8_CODES ? 8 : 1, KS = OUT == F8_CODES ? 2 : 4;
-  const dim3 grid((uint32_t)((a.N + CG * 16 - 1) / (CG * 16)));
+  const dim3 grid((uint32_t)((a.N + 15) / 16));
   if (a.M <= 16)
-    launch(few_f8_kernel<1, CG, KS, OUT, ACT>, grid, dim3(CG * KS * 64), 0, s, a);
+    launch(few_f8_kernel<1, 4, OUT, ACT>, grid, dim3(256), 0, s, a);
   else
-    launch(few_f8_kernel<2, CG, KS, OUT, ACT>, grid, dim3(CG * KS * 64), 0, s, a);
+    launch(few_f8_kernel<2, 4, OUT, ACT>, grid, dim3(256), 0, s, a);
 }
 
 // Tiles: BM x BN, wave grid, groups of it, LDS stages, wavefronts per SIMD.
@@ -689,7 +681,7 @@ static hipError_t launch_f8(const GemmF8Args& a, hipStream_t s) {
   F8Tile tile = choose_gemm_f8_tile(a.M, (long)a.N * (kGated ? 2 : 1), a.K, OUT == F8_CODES, OUT == F8_F32);
   switch (tile) {
     case kF8Few:
-      launch_few<OUT, ACT>(a, s);
+      if constexpr (f8_has_tile(kF8Few, OUT == F8_CODES, OUT != F8_BF16)) launch_few<OUT, ACT>(a, s);
       break;
 #define SF_F8_CASE(id, bm, bn, wm, wn, wk, st, mw)                                                              \
   case id: {                                                                                                  \

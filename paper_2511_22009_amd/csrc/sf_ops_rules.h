@@ -82,6 +82,7 @@ enum F8Tile {
 };
 constexpr bool f8_has_tile(F8Tile t, bool codes, bool exact) {
   return codes   ? t == kF8Codes32 || t == kF8Codes64
+         : t == kF8Few ? true
          : exact ? t == kF8Split32x4 || t == kF8Split64x4 || t == kF8Tile128
                  : t == kF8Split32 || t == kF8Split64 || t == kF8Deep128 || t == kF8Tile128 || t == kF8Tile128x256 ||
                        t == kF8Tile256x256;
@@ -122,7 +123,7 @@ inline F8Tile choose_gemm_f8_tile(long M, long N, long K, bool codes, bool exact
                                {kF8Split64x4, 64, 64, 1, 311, 4800, 311, 4800},
                                {kF8Tile128, 128, 128, 2, 1930, 4900, 1165, 5560}};
   constexpr F8Cost kCodes[] = {{kF8Codes32, 32, 256, 2, 1096, 6570, 776, 4510}, {kF8Codes64, 64, 256, 2, 1891, 7940, 1092, 6700}};
-  if (M <= 32 && (double)N * (double)K <= (M <= 16 ? 4e7 : 1.6e7)) return kF8Few;
+  if (!codes && M <= 32 && (double)N * (double)K <= (M <= 16 ? 4e7 : 1.6e7)) return kF8Few;
   const F8Cost* const from = codes ? kCodes : exact ? kExact : kTiles;
   const F8Cost* const to = codes ? kCodes + 2 : exact ? kExact + 3 : kTiles + 6;
   const int64_t slices = ((int64_t)K + 127) / 128;

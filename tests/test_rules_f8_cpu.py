@@ -15,7 +15,7 @@ int main() {
   int codes, exact;
   while (scanf("%ld %ld %ld %d %d", &M, &N, &K, &codes, &exact) == 5) {
     const sf::F8Tile t = sf::choose_gemm_f8_tile(M, N, K, codes, exact);
-    printf("%d %d\n", (int)t, (int)(t == sf::kF8Few || sf::f8_has_tile(t, codes, exact)));
+    printf("%d %d\n", (int)t, (int)sf::f8_has_tile(t, codes, exact));
   }
 }
 """
@@ -52,4 +52,4 @@ def test_f8_sizes_of_the_gpu_tests_reach_every_tile(tmp_path_factory):
     both = [(m, 2 * n, k) for m, n, k in gated]
     assert set(_f8_tiles(exe, [(*s, 0, 0) for s in both])[0]) == values
     assert set(_f8_tiles(exe, [(*s, 0, 1) for s in both])[0]) == {"few", "split32x4", "split64x4", "tile128"}
-    assert set(_f8_tiles(exe, [(*s, 1, 1) for s in both])[0]) == {"few", "codes32", "codes64"}
+    assert set(_f8_tiles(exe, [(*s, 1, 1) for s in both])[0]) == {"codes32", "codes64"}
