@@ -698,7 +698,7 @@ static hipError_t launch_f8(const GemmF8Args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_gemm_f8(F8Out kind, F8Act act, const GemmF8Args& a, hipStream_t s) {
+static hipError_t launch_part(F8Out kind, F8Act act, const GemmF8Args& a, hipStream_t s) {
   switch (act) {
     case F8_NONE: return kind == F8_BF16 ? launch_f8<F8_BF16, F8_NONE>(a, s) : launch_f8<F8_F32, F8_NONE>(a, s);
     case F8_SILU:
@@ -711,6 +711,39 @@ hipError_t launch_gemm_f8(F8Out kind, F8Act act, const GemmF8Args& a, hipStream_
                               : launch_f8<F8_CODES, F8_GELU>(a, s);
   }
   return hipErrorInvalidValue;
+}
+
+hipError_t launch_gemm_f8(F8Out kind, F8Act act, const GemmF8Args& a, hipStream_t s) {
+  const int sides = act == F8_NONE ? 1 : 2;
+  long rows, cols;
+  choose_gemm_f8_parts(a.M, (long)a.N * sides, a.K, kind == F8_CODES, kind == F8_F32, rows, cols);
+  cols /= sides;
+  GemmF8Args first = a, rest = a;
+  first.M = (int)rows;
+  first.N = (int)cols;
+  if (rows == a.M && cols == a.N) return launch_part(kind, act, first, s);
+  const int es = kind == F8_CODES ? 1 : kind == F8_BF16 ? 2 : 4;
+  if (rows < a.M) {
+    rest.M = a.M - first.M;
+    rest.a.q += rows * a.a.ld;
+    rest.a.scale += rows * a.a.s_row;
+    rest.out = (char*)a.out + rows * a.ldo * es;
+    if (a.out_scale) rest.out_scale += rows * a.os_row;
+  } else {  // a multiple of 128 columns
+    rest.N = a.N - first.N;
+    rest.b.q += cols * a.b.ld;
+    rest.b.scale += cols / kF8Block * a.b.s_row;
+    if (act != F8_NONE) {
+      rest.up.q += cols * a.up.ld;
+      rest.up.scale += cols / kF8Block * a.up.s_row;
+    }
+    if (a.bias) rest.bias += cols;
+    if (a.up_bias) rest.up_bias += cols;
+    rest.out = (char*)a.out + cols * es;
+    if (a.out_scale) rest.out_scale += cols / kF8Block * a.os_block;
+  }
+  const hipError_t e = launch_part(kind, act, first, s);
+  return e != hipSuccess ? e : launch_part(kind, act, rest, s);
 }
 
 }  // namespace sf

@@ -95,8 +95,25 @@ struct F8Cost {
   int bm, bn, per, slice, once, alone_slice, alone_once;
 };
 
-// Which tile: the one with the least work on its busiest CU. N counts columns of the weights (gated: both
-// projections). Costs from launches of one and of two rounds of each tile at K = 1024 and 4096. Some times (us):
+struct F8Choice {
+  F8Tile tile;
+  double cost;  // ns
+};
+// The tile among `from` to `to` with the least work on its busiest CU.
+inline F8Choice cheapest_f8_tile(const F8Cost* from, const F8Cost* to, int64_t M, int64_t N, int64_t K) {
+  const int64_t slices = (K + 127) / 128;
+  F8Choice best{from->tile, -1.0};
+  for (const F8Cost* t = from; t != to; ++t) {
+    const int64_t tiles = ((M + t->bm - 1) / t->bm) * ((N + t->bn - 1) / t->bn);
+    const int64_t k = (tiles + 255) / 256, rest = k % t->per;
+    const double cost = (double)(k / t->per) * ((double)t->slice * (double)slices + t->once) +
+                        (rest ? (double)t->alone_slice * (double)slices + t->alone_once : 0.0);
+    if (best.cost < 0.0 || cost < best.cost) best = F8Choice{t->tile, cost};
+  }
+  return best;
+}
+
+// The tiles of each kind of output. Costs from launches of one and of two rounds of each tile at K = 1024 and 4096. Some times (us):
 //   * 256 x 256, of large outputs: 16384 x 4608 x 1152 115, 128 x 256 129, 128 x 128 in pairs 136; 8192^3 492, 535
 //     and 585.
 //   * 128 x 128 in pairs where rounds of the large tiles are left half empty: 16384 x 1152 x 4608 123, 256 x 256 129.
@@ -112,34 +129,64 @@ struct F8Cost {
 //     two of them: 300 x 2 x 1152 x 1152 11.2, 64 x 256 14.6; 2048 x 2 x 2048 x 1024 28 and 23.
 // Up to 32 rows the weights' bytes count, which more and smaller workgroups fetch sooner: 32 x 3456 x 1152 4.4,
 // 64 x 64 6.1; but long weights that a tile's stages fetch faster: 32 x 8192 x 8192 25.8 and 17.7 (16 rows 18.2 and 17.0).
+struct F8Tiles {
+  const F8Cost *from, *to;
+};
+inline F8Tiles f8_tiles_of(bool codes, bool exact) {
+  static constexpr F8Cost kTiles[] = {{kF8Split32, 32, 64, 2, 279, 4540, 193, 3740},
+                                      {kF8Split64, 64, 64, 1, 242, 3700, 242, 3700},
+                                      {kF8Deep128, 128, 128, 1, 600, 4300, 600, 4300},
+                                      {kF8Tile128, 128, 128, 2, 1265, 2600, 834, 4000},
+                                      {kF8Tile128x256, 128, 256, 1, 1000, 5200, 1000, 5200},
+                                      {kF8Tile256x256, 256, 256, 1, 1900, 7300, 1900, 7300}};
+  static constexpr F8Cost kExact[] = {{kF8Split32x4, 32, 64, 1, 215, 4800, 215, 4800},
+                                      {kF8Split64x4, 64, 64, 1, 311, 4800, 311, 4800},
+                                      {kF8Tile128, 128, 128, 2, 1930, 4900, 1165, 5560}};
+  static constexpr F8Cost kCodes[] = {{kF8Codes32, 32, 256, 2, 1096, 6570, 776, 4510},
+                                      {kF8Codes64, 64, 256, 2, 1891, 7940, 1092, 6700}};
+  return codes ? F8Tiles{kCodes, kCodes + 2} : exact ? F8Tiles{kExact, kExact + 3} : F8Tiles{kTiles, kTiles + 6};
+}
+// N counts columns of the weights (gated: both projections).
 inline F8Tile choose_gemm_f8_tile(long M, long N, long K, bool codes, bool exact) {
-  constexpr F8Cost kTiles[] = {{kF8Split32, 32, 64, 2, 279, 4540, 193, 3740},
-                               {kF8Split64, 64, 64, 1, 242, 3700, 242, 3700},
-                               {kF8Deep128, 128, 128, 1, 600, 4300, 600, 4300},
-                               {kF8Tile128, 128, 128, 2, 1265, 2600, 834, 4000},
-                               {kF8Tile128x256, 128, 256, 1, 1000, 5200, 1000, 5200},
-                               {kF8Tile256x256, 256, 256, 1, 1900, 7300, 1900, 7300}};
-  constexpr F8Cost kExact[] = {{kF8Split32x4, 32, 64, 1, 215, 4800, 215, 4800},
-                               {kF8Split64x4, 64, 64, 1, 311, 4800, 311, 4800},
-                               {kF8Tile128, 128, 128, 2, 1930, 4900, 1165, 5560}};
-  constexpr F8Cost kCodes[] = {{kF8Codes32, 32, 256, 2, 1096, 6570, 776, 4510}, {kF8Codes64, 64, 256, 2, 1891, 7940, 1092, 6700}};
   if (!codes && M <= 32 && (double)N * (double)K <= (M <= 16 ? 4e7 : 1.6e7)) return kF8Few;
-  const F8Cost* const from = codes ? kCodes : exact ? kExact : kTiles;
-  const F8Cost* const to = codes ? kCodes + 2 : exact ? kExact + 3 : kTiles + 6;
-  const int64_t slices = ((int64_t)K + 127) / 128;
-  double least = -1.0;
-  F8Tile best = from->tile;
-  for (const F8Cost* t = from; t != to; ++t) {
-    const int64_t tiles = (((int64_t)M + t->bm - 1) / t->bm) * (((int64_t)N + t->bn - 1) / t->bn);
-    const int64_t k = (tiles + 255) / 256, rest = k % t->per;
-    const double cost = (double)(k / t->per) * ((double)t->slice * (double)slices + t->once) +
-                        (rest ? (double)t->alone_slice * (double)slices + t->alone_once : 0.0);
-    if (least < 0.0 || cost < least) {
-      best = t->tile;
-      least = cost;
+  const F8Tiles t = f8_tiles_of(codes, exact);
+  return cheapest_f8_tile(t.from, t.to, M, N, K).tile;
+}
+
+// A product whose last round of tiles leaves most CUs idle is cheaper as two, one after the other: the rows, or the columns
+// (multiples of 256), that a tile takes in whole rounds or without its last partial column, and the others, each with a tile of its
+// own. 16384 x 1152 x 4608: 1024 columns in one round of 256 x 256 tiles 84 us, 128 columns in 128 x 128 tiles 22, all of them
+// in 2.25 rounds of 128 x 128 in pairs 123. rows, cols: the first part's; M and N where the whole is not to be parted. Products
+// below 40 us stay whole (a second launch and its fixed part count there), and those that would gain less than a twelfth.
+inline void choose_gemm_f8_parts(long M, long N, long K, bool codes, bool exact, long& rows, long& cols) {
+  rows = M;
+  cols = N;
+  const F8Tiles t = f8_tiles_of(codes, exact);
+  const double whole = cheapest_f8_tile(t.from, t.to, M, N, K).cost;
+  if (M <= 32 || whole < 40e3) return;
+  double least = whole * (11.0 / 12.0);
+  for (const F8Cost* c = t.from; c != t.to; ++c) {
+    const int64_t tm = ((int64_t)M + c->bm - 1) / c->bm, tn = ((int64_t)N + c->bn - 1) / c->bn, round = 256 * (int64_t)c->per;
+    const int64_t full = tm * tn / round * round;
+    const int64_t r = full / tn * c->bm, n[2] = {full / tm * c->bn / 256 * 256, (int64_t)N / c->bn * c->bn / 256 * 256};
+    if (r > 0 && r < M) {
+      const double two = cheapest_f8_tile(t.from, t.to, r, N, K).cost + cheapest_f8_tile(t.from, t.to, M - r, N, K).cost + 2e3;
+      if (two < least) {
+        least = two;
+        rows = (long)r;
+        cols = N;
+      }
     }
+    for (const int64_t first : n)
+      if (first > 0 && first < N) {
+        const double two = cheapest_f8_tile(t.from, t.to, M, first, K).cost + cheapest_f8_tile(t.from, t.to, M, N - first, K).cost + 2e3;
+        if (two < least) {
+          least = two;
+          rows = M;
+          cols = (long)first;
+        }
+      }
   }
-  return best;
 }
 
 }  // namespace sf

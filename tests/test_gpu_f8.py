@@ -253,6 +253,23 @@ def test_gated(M, N, K, name, dtype):
     check_gated(M, N, K, dtype, name, bias=(M + N) % 2 == 0, narrow=True)
 
 
+# Rows, outputs, K, what the outputs are, and whether rows or columns are parted: products in two launches.
+PARTS = [(4150, 2048, 3001, "bf16", False, "rows"), (4160, 4200, 1601, "bf16", False, "cols"), (4100, 2050, 1500, "fp32", False, "rows"),
+         (2100, 4160, 1500, "fp32", False, "cols"), (4150, 1024, 3000, "bf16", True, "rows"), (4160, 2100, 1601, "bf16", True, "cols"),
+         (2060, 2150, 1500, "fp32", True, "rows"), (2100, 2080, 1500, "fp32", True, "cols"), (2100, 2048, 2301, "f8", True, "rows"),
+         (256, 16500, 2300, "f8", True, "cols")]
+
+
+@pytest.mark.parametrize("M,N,K,kind,gated,part", PARTS)
+def test_products_in_two_parts(M, N, K, kind, gated, part):
+    dtype = {"bf16": BF16, "fp32": FP32, "f8": F8}[kind]
+    for narrow in (False, True):
+        if gated:
+            check_gated(M, N, K, dtype, "silu", bias=True, narrow=narrow)
+        else:
+            check_matmul(M, N, K, dtype, bias=True, narrow=narrow)
+
+
 def test_gated_outputs_that_are_given():
     from paper_2511_22009_amd import gated_matmul_f8
     g = gen(8)
