@@ -118,7 +118,7 @@ inline F8Choice cheapest_f8_tile(const F8Cost* from, const F8Cost* to, int64_t M
 //     and 585.
 //   * 128 x 128 in pairs where rounds of the large tiles are left half empty: 16384 x 1152 x 4608 123, 256 x 256 129.
 //   * 128 x 128 with four stages, eight wavefronts, one per CU, for single rounds of it: 2048 x 2048 x 4096 23, in pairs
-//     31, 128 x 256 37.
+//     31, 128 x 256 37; half a round of 16384 x 128 x 4608 22, 64 x 64 25 (its cost is between what a whole and half a round take).
 //   * 64 x 64 with K split over two groups of wavefronts for small grids: 1024 x 1024 x 4096 11.5, over four 13.3, 32 x 64
 //     13.5; not split 13.9 at 512 x 1024 x 4352, 128 x 128 there 30; in fp32 517 x 1001 x 4321 over four 16.3, not split 25.
 //   * 32 x 64 with one wavefront to a group, two groups (fp32: four) for the smallest: 512 x 1024 x 4352 10.2, 64 x 64 11.8;
@@ -135,7 +135,7 @@ struct F8Tiles {
 inline F8Tiles f8_tiles_of(bool codes, bool exact) {
   static constexpr F8Cost kTiles[] = {{kF8Split32, 32, 64, 2, 279, 4540, 193, 3740},
                                       {kF8Split64, 64, 64, 1, 242, 3700, 242, 3700},
-                                      {kF8Deep128, 128, 128, 1, 600, 4300, 600, 4300},
+                                      {kF8Deep128, 128, 128, 1, 540, 4200, 540, 4200},
                                       {kF8Tile128, 128, 128, 2, 1265, 2600, 834, 4000},
                                       {kF8Tile128x256, 128, 256, 1, 1000, 5200, 1000, 5200},
                                       {kF8Tile256x256, 256, 256, 1, 1900, 7300, 1900, 7300}};
