@@ -653,13 +653,20 @@ __global__ __launch_bounds__(KS * 64) void few_f8_kernel(GemmF8Args a) {
   }
 }
 
-template <F8Out OUT, F8Act ACT>
-static void launch_few(const GemmF8Args& a, hipStream_t s) {
+// K over four wavefronts, from 4096 on over eight (8 x 8192 x 4096 11.4 us and 9.3, 32 x 2 x 1152 x 4608 12.9 and 11.7, 8 x 1152
+// x 4608 level; 16 x 1152 x 2048 4.0 and 4.2, 16 x 4608 x 1152 5.0 and 5.8).
+template <F8Out OUT, F8Act ACT, int KS>
+static void launch_few_of(const GemmF8Args& a, hipStream_t s) {
   const dim3 grid((uint32_t)((a.N + 15) / 16));
   if (a.M <= 16)
-    launch(few_f8_kernel<1, 4, OUT, ACT>, grid, dim3(256), 0, s, a);
+    launch(few_f8_kernel<1, KS, OUT, ACT>, grid, dim3(KS * 64), 0, s, a);
   else
-    launch(few_f8_kernel<2, 4, OUT, ACT>, grid, dim3(256), 0, s, a);
+    launch(few_f8_kernel<2, KS, OUT, ACT>, grid, dim3(KS * 64), 0, s, a);
+}
+template <F8Out OUT, F8Act ACT>
+static void launch_few(const GemmF8Args& a, hipStream_t s) {
+  if (a.K < 4096) launch_few_of<OUT, ACT, 4>(a, s);
+  else launch_few_of<OUT, ACT, 8>(a, s);
 }
 
 // Tiles: BM x BN, wave grid, groups of it, LDS stages, wavefronts per SIMD.

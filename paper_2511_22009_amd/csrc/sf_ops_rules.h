@@ -116,7 +116,8 @@ inline F8Choice cheapest_f8_tile(const F8Cost* from, const F8Cost* to, int64_t M
 // The tiles of each kind of output. Costs from launches of one and of two rounds of each tile at K = 1024 and 4096. Some times (us):
 //   * 256 x 256, of large outputs: 16384 x 4608 x 1152 115, 128 x 256 129, 128 x 128 in pairs 136; 8192^3 492, 535
 //     and 585.
-//   * 128 x 128 in pairs where rounds of the large tiles are left half empty: 16384 x 1152 x 4608 123, 256 x 256 129.
+//   * 128 x 128 in pairs where rounds of the large tiles are left half empty: 16384 x 1152 x 4608 whole 123, 256 x 256
+//     129.
 //   * 128 x 128 with four stages, eight wavefronts, one per CU, for single rounds of it: 2048 x 2048 x 4096 23, in pairs
 //     31, 128 x 256 37; half a round of 16384 x 128 x 4608 22, 64 x 64 25 (its cost is between what a whole and half a round take).
 //   * 64 x 64 with K split over two groups of wavefronts for small grids: 1024 x 1024 x 4096 11.5, over four 13.3, 32 x 64

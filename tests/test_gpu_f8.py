@@ -134,7 +134,7 @@ SIZES = [(1, 1, 1), (1, 3456, 1152), (2, 17, 15), (16, 16, 16), (17, 100, 127), 
          (65, 64, 128), (65, 65, 17), (100, 1001, 300), (517, 1001, 777), (128, 128, 130), (300, 260, 8333), (129, 770, 1),
          (2048, 1100, 256), (1000, 4100, 127), (4096, 2304, 768), (2500, 4000, 1153), (32, 4096, 4100),
          (2100, 2000, 520), (4699, 786, 1300), (1412, 5554, 520), (1610, 606, 520), (600, 5500, 260),
-         (500, 2000, 70), (600, 1536, 1300), (257, 1700, 4300)]
+         (500, 2000, 70), (600, 1536, 1300), (257, 1700, 4300), (20, 500, 4100), (9, 333, 4096), (16, 1500, 4200)]
 
 
 @pytest.mark.parametrize("narrow", [False, True], ids=["wide", "narrow"])
@@ -247,7 +247,7 @@ def check_gated(M, N, K, dtype, name, bias, narrow=False):
 @pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 2048, 768), (16, 17, 33), (20, 130, 129), (64, 300, 128), (65, 33, 300), (200, 129, 144),
                                    (300, 700, 1000), (513, 64, 8320), (1025, 2100, 260), (2304, 2176, 768), (32, 1000, 1152), (800, 600, 140),
                                    (4699, 393, 1300), (646, 2750, 260), (1610, 303, 520), (2048, 550, 256), (500, 1000, 70),
-                                   (590, 700, 2309)])
+                                   (590, 700, 2309), (8, 300, 4222), (30, 260, 4100)])
 def test_gated(M, N, K, name, dtype):
     check_gated(M, N, K, dtype, name, bias=(M + N) % 2 == 1)
     check_gated(M, N, K, dtype, name, bias=(M + N) % 2 == 0, narrow=True)
