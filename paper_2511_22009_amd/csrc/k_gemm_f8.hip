@@ -685,7 +685,7 @@ static void launch_few(const GemmF8Args& a, hipStream_t s) {
 template <F8Out OUT, F8Act ACT>
 static hipError_t launch_f8(const GemmF8Args& a, hipStream_t s) {
   constexpr bool kGated = ACT != F8_NONE;
-  F8Tile tile = choose_gemm_f8_tile(a.M, (long)a.N * (kGated ? 2 : 1), a.K, OUT == F8_CODES, OUT == F8_F32);
+  F8Tile tile = choose_gemm_f8_tile(a.M, (long)a.N * (kGated ? 2 : 1), a.K, OUT == F8_CODES, OUT == F8_F32, kGated);
   switch (tile) {
     case kF8Few:
       if constexpr (f8_has_tile(kF8Few, OUT == F8_CODES, OUT != F8_BF16)) launch_few<OUT, ACT>(a, s);

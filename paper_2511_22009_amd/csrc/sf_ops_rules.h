@@ -129,7 +129,10 @@ inline F8Choice cheapest_f8_tile(const F8Cost* from, const F8Cost* to, int64_t M
 //     eight wavefronts, one a CU, 398 and 43; 64 x 256 of that kind 489 and 42. 32 x 256 while a CU gets one or
 //     two of them: 300 x 2 x 1152 x 1152 11.2, 64 x 256 14.6; 2048 x 2 x 2048 x 1024 28 and 23.
 // Up to 32 rows the weights' bytes count, which more and smaller workgroups fetch sooner: 32 x 3456 x 1152 4.4,
-// 64 x 64 6.1; but long weights that a tile's stages fetch faster: 32 x 8192 x 8192 25.8 and 17.7 (16 rows 18.2 and 17.0).
+// 64 x 64 6.1; but long weights that a tile's stages fetch faster: 32 x 8192 x 8192 25.8 and 17.7 (16 rows 18.2 and 17.0). Of
+// 17 rows on each of those workgroups reads as many rows as columns, and a second round of them (fp32: a third) takes longer than
+// 32 x 64: 32 x 3456 x 1152 4.6 and 5.4, 32 x 4608 x 1152 6.5 and 5.5, 32 x 9216 x 1152 8.7 and 5.6 (fp32 4.7 and 7.0, 6.6 and 7.0,
+// 8.8 and 7.3).
 struct F8Tiles {
   const F8Cost *from, *to;
 };
@@ -148,8 +151,10 @@ inline F8Tiles f8_tiles_of(bool codes, bool exact) {
   return codes ? F8Tiles{kCodes, kCodes + 2} : exact ? F8Tiles{kExact, kExact + 3} : F8Tiles{kTiles, kTiles + 6};
 }
 // N counts columns of the weights (gated: both projections).
-inline F8Tile choose_gemm_f8_tile(long M, long N, long K, bool codes, bool exact) {
-  if (!codes && M <= 32 && (double)N * (double)K <= (M <= 16 ? 4e7 : 1.6e7)) return kF8Few;
+inline F8Tile choose_gemm_f8_tile(long M, long N, long K, bool codes, bool exact, bool gated) {
+  const bool few = M <= 16 ? (double)N * (double)K <= 4e7
+                           : M <= 32 && (double)N * (double)K <= 1.6e7 && N / (gated ? 32 : 16) <= (exact ? 512 : 256);
+  if (few && !codes) return kF8Few;
   const F8Tiles t = f8_tiles_of(codes, exact);
   return cheapest_f8_tile(t.from, t.to, M, N, K).tile;
 }

@@ -134,7 +134,7 @@ SIZES = [(1, 1, 1), (1, 3456, 1152), (2, 17, 15), (16, 16, 16), (17, 100, 127), 
          (65, 64, 128), (65, 65, 17), (100, 1001, 300), (517, 1001, 777), (128, 128, 130), (300, 260, 8333), (129, 770, 1),
          (2048, 1100, 256), (1000, 4100, 127), (4096, 2304, 768), (2500, 4000, 1153), (32, 4096, 4100),
          (2100, 2000, 520), (4699, 786, 1300), (1412, 5554, 520), (1610, 606, 520), (600, 5500, 260),
-         (500, 2000, 70), (600, 1536, 1300), (257, 1700, 4300), (20, 500, 4100), (9, 333, 4096), (16, 1500, 4200)]
+         (500, 2000, 70), (600, 1536, 1300), (257, 1700, 4300), (20, 500, 4100), (9, 333, 4096), (16, 1500, 4200), (25, 4500, 260)]
 
 
 @pytest.mark.parametrize("narrow", [False, True], ids=["wide", "narrow"])
