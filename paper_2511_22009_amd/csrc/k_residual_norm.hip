@@ -7,6 +7,7 @@
 #include <algorithm>
 
 #include "sf_f8_device.h"
+#include "sf_ops_rules.h"
 
 namespace sf {
 
@@ -271,19 +272,18 @@ static void launch_rows(ResidualNormArgs a, hipStream_t s) {
   const int span = turns * ROWS;
   const uint32_t spans = (uint32_t)((a.tokens + (int64_t)span - 1) / span);
   const FastDiv div = make_fastdiv(spans);
-  const int most = std::max((int)((1 << 21) / spans), 1);  // a grid holds less than 2^32 threads
-  const int samples = a.samples;
-  for (int from = 0; from < samples; from += most) {
-    launch(residual_norm_kernel<TH, TY, OUT, NV, WAVES, WHOLE>, dim3((uint32_t)std::min(most, samples - from) * spans), dim3(threads_of(WAVES)), 0, s, a, div, span);
-    a.h += (int64_t)most * a.h_sample * (int64_t)sizeof(TH);
-    a.y += (int64_t)most * a.y_sample * (int64_t)sizeof(TY);
-    a.h_out += (int64_t)most * a.ho_sample * (int64_t)sizeof(TH);
-    if (a.out) a.out += (int64_t)most * a.out_sample * (OUT == NORM_CODES ? 1 : OUT == NORM_F32 ? 4 : 2);
-    if (a.out_scale) a.out_scale += (int64_t)most * a.os_sample;
-    if (a.gate) a.gate += (int64_t)most * a.gate_sample;
-    if (a.scale) a.scale += (int64_t)most * a.scale_sample;
-    if (a.shift) a.shift += (int64_t)most * a.shift_sample;
-  }
+  const int64_t most = std::max<int64_t>((1 << 21) / spans, 1);  // a grid holds less than 2^32 threads
+  in_parts(a.samples, most, [&](int64_t, int64_t n) {
+    launch(residual_norm_kernel<TH, TY, OUT, NV, WAVES, WHOLE>, dim3((uint32_t)n * spans), dim3(threads_of(WAVES)), 0, s, a, div, span);
+    a.h += n * a.h_sample * (int64_t)sizeof(TH);
+    a.y += n * a.y_sample * (int64_t)sizeof(TY);
+    a.h_out += n * a.ho_sample * (int64_t)sizeof(TH);
+    if (a.out) a.out += n * a.out_sample * (OUT == NORM_CODES ? 1 : OUT == NORM_F32 ? 4 : 2);
+    if (a.out_scale) a.out_scale += n * a.os_sample;
+    if (a.gate) a.gate += n * a.gate_sample;
+    if (a.scale) a.scale += n * a.scale_sample;
+    if (a.shift) a.shift += n * a.shift_sample;
+  });
 }
 
 // A wavefront per row where there are many, else a workgroup, whose lanes each wait for less.

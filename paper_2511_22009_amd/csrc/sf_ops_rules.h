@@ -1,4 +1,5 @@
-// Which tile a product of 8-bit codes takes. Plain C++, as CPU tests run it too.
+// Which tile a product of 8-bit codes takes, and how the rows around a block are shared out. Plain C++, as CPU
+// tests run it too.
 #pragma once
 
 #include <cstdint>
@@ -193,6 +194,15 @@ inline void choose_gemm_f8_parts(long M, long N, long K, bool codes, bool exact,
         }
       }
   }
+}
+
+// ---- rows around a block ---------------------------------------------------------------
+
+// A count in parts of at most `most`: call(first, n) for each. In 64 bits, since counts go up to 2^31 - 1 and the
+// first one past the last part does not fit 32.
+template <typename F>
+inline void in_parts(int64_t count, int64_t most, F call) {
+  for (int64_t first = 0; first < count; first += most) call(first, count - first < most ? count - first : most);
 }
 
 }  // namespace sf
