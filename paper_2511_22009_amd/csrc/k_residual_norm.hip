@@ -4,8 +4,6 @@
 // bounds it: h and y are read once, h' and a written once, and a row stays in registers between its
 // two norms. 4 x 4096 rows of 1152 dims, h fp32, y bf16, a as codes: 50 us, 4.2 TB/s (a as bf16 47, 4.8 TB/s; the rate
 // of a large copy 41); 2760 rows of 771 dims in fp32 9.8; one row of 1152 4.3 in the kernel.
-#include <algorithm>
-
 #include "sf_f8_device.h"
 #include "sf_ops_rules.h"
 
@@ -164,9 +162,9 @@ __global__ __launch_bounds__(threads_of(WAVES)) void residual_norm_kernel(Residu
   constexpr int STEP = WAVES * 256, ROWS = threads_of(WAVES) / 64 / WAVES;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t sample = fdiv(blockIdx.x, div_spans);
-  const int start = (int)(blockIdx.x - sample * div_spans.d) * span, end = min(start + span, a.tokens);
+  const int start = (int)(blockIdx.x - sample * div_spans.d) * span, end = span_end(start, span, a.tokens);
+  if (wave / WAVES >= end - start) return;  // whole wavefronts, and with several to a row whole workgroups
   int token = start + wave / WAVES;
-  if (token >= end) return;  // whole wavefronts, and with several to a row whole workgroups
   const int first = 4 * ((wave % WAVES) * 64 + (threadIdx.x & 63));
   const TH* const h = (const TH*)a.h + sample * a.h_sample;
   const TY* const y = (const TY*)a.y + sample * a.y_sample;
@@ -209,8 +207,8 @@ __global__ __launch_bounds__(threads_of(WAVES)) void residual_norm_kernel(Residu
     float x[NV][4];
 #pragma unroll
     for (int i = 0; i < NV; ++i) take_piece<WHOLE>(x[i], yp[i], first + i * STEP, a.D);
-    const int next = token + ROWS, ahead = min(next, end - 1);
-    fetch_y(ahead);
+    const bool more = ROWS < end - token;
+    fetch_y(row_ahead(token, ROWS, end));
     if (a.post != NORM_NONE) normalise<NV, WAVES>(x, a.post, a, first, lds);
     TH* const h_out = (TH*)a.h_out + sample * a.ho_sample + (int64_t)token * a.ho_token + first;
 #pragma unroll
@@ -221,7 +219,7 @@ __global__ __launch_bounds__(threads_of(WAVES)) void residual_norm_kernel(Residu
       for (int e = 0; e < 4; ++e) x[i][e] = __builtin_fmaf(a.r, hv[e], x[i][e] * vg[i][e]);
     }
     // before this row's h' leaves: over h itself, the last row is read again
-    if (next < end) fetch_h(next);
+    if (more) fetch_h(token + ROWS);
 #pragma unroll
     for (int i = 0; i < NV; ++i) Out4<TH>::run(h_out + i * STEP, x[i], a.D - first - i * STEP);
     if (a.out) {
@@ -256,8 +254,8 @@ __global__ __launch_bounds__(threads_of(WAVES)) void residual_norm_kernel(Residu
         }
       }
     }
-    token = next;
-    if (token >= end) break;
+    if (!more) break;
+    token += ROWS;
   }
 }
 
@@ -267,14 +265,10 @@ static void launch_rows(ResidualNormArgs a, hipStream_t s) {
   // as many workgroups as a CU holds at once, each as many rows of its sample as that takes (4096 x 1152 to codes: two
   // 17.9 us, four, which take turns, 21.3; 16384 x 768: three 32.6, four 27.9)
   constexpr int64_t kGroups = NV > 4 ? 512 : NV > 3 && WAVES == 1 ? 768 : 1024;
-  const int64_t rows = (int64_t)a.samples * a.tokens;
-  const int turns = (int)std::min<int64_t>((rows + kGroups * ROWS - 1) / (kGroups * ROWS), (a.tokens + ROWS - 1) / ROWS);
-  const int span = turns * ROWS;
-  const uint32_t spans = (uint32_t)((a.tokens + (int64_t)span - 1) / span);
-  const FastDiv div = make_fastdiv(spans);
-  const int64_t most = std::max<int64_t>((1 << 21) / spans, 1);  // a grid holds less than 2^32 threads
-  in_parts(a.samples, most, [&](int64_t, int64_t n) {
-    launch(residual_norm_kernel<TH, TY, OUT, NV, WAVES, WHOLE>, dim3((uint32_t)n * spans), dim3(threads_of(WAVES)), 0, s, a, div, span);
+  const NormSpans p = norm_spans(a.samples, a.tokens, ROWS, kGroups);
+  const FastDiv div = make_fastdiv(p.spans);
+  in_parts(a.samples, p.most, [&](int64_t, int64_t n) {
+    launch(residual_norm_kernel<TH, TY, OUT, NV, WAVES, WHOLE>, dim3((uint32_t)n * p.spans), dim3(threads_of(WAVES)), 0, s, a, div, p.span);
     a.h += n * a.h_sample * (int64_t)sizeof(TH);
     a.y += n * a.y_sample * (int64_t)sizeof(TY);
     a.h_out += n * a.ho_sample * (int64_t)sizeof(TH);

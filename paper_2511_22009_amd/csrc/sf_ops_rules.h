@@ -205,4 +205,22 @@ inline void in_parts(int64_t count, int64_t most, F call) {
   for (int64_t first = 0; first < count; first += most) call(first, count - first < most ? count - first : most);
 }
 
+// Workgroups that take `step` rows at once, about `groups` of them: `span` rows of one sample each, `spans` to a
+// sample, and `most` samples in a launch, since a grid holds less than 2^32 threads.
+struct NormSpans {
+  int span;
+  uint32_t spans;
+  int64_t most;
+};
+inline NormSpans norm_spans(int64_t samples, int64_t tokens, int step, int64_t groups) {
+  const int64_t all = (samples * tokens + groups * step - 1) / (groups * step), one = (tokens + step - 1) / step;
+  const int64_t span = (all < one ? all : one) * step, spans = (tokens + span - 1) / span;
+  return NormSpans{(int)span, (uint32_t)spans, spans < (1 << 21) ? (1 << 21) / spans : 1};
+}
+
+// Rows of a sample from `start` on go to one workgroup, `span` of them or what is left: the first row past them. And
+// the row that is read ahead: `step` rows further, or the last one again. Neither leaves 32 bits, whatever tokens is.
+constexpr int span_end(int start, int span, int tokens) { return span < tokens - start ? start + span : tokens; }
+constexpr int row_ahead(int token, int step, int end) { return step < end - token ? token + step : end - 1; }
+
 }  // namespace sf

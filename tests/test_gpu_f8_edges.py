@@ -24,3 +24,9 @@ def test_residual_norm_of_as_many_samples_as_it_takes():
     """1024 launches; the first sample past the last one is 2^31."""
     rows = (1 << 31) - 1
     add_one_in_place(rows, (rows, 1, 1))
+
+
+def test_residual_norm_of_as_many_tokens_as_it_takes():
+    """One sample, its last workgroup's rows up to the last; the first row past them is 2^31."""
+    rows = (1 << 31) - 1
+    add_one_in_place(rows, (1, rows, 1))

@@ -36,3 +36,54 @@ def test_parts_of_a_count_cover_it_once(tmp_path_factory):
                        text=True, timeout=60)
     assert r.returncode == 0, r.stdout
     assert [int(v) for v in r.stdout.split()] == [-(-c // m) for c, m in calls]
+
+
+SPANS = r"""
+#include <cstdio>
+#include "sf_ops_rules.h"
+// Reads samples tokens step groups, walks the workgroups of a sample as the kernel does and fails where rows are missed, taken
+// twice or read past the sample. A wavefront's rows are walked at its first and its last three.
+int main() {
+  long long samples, tokens, groups;
+  int step;
+  while (scanf("%lld %lld %d %lld", &samples, &tokens, &step, &groups) == 4) {
+    const sf::NormSpans p = sf::norm_spans(samples, tokens, step, groups);
+    bool ok = p.span >= 1 && p.span % step == 0 && p.spans >= 1 && p.most >= 1 && (p.spans == 1 || p.spans * p.most <= 1 << 21);
+    ok = ok && (long long)(p.spans - 1) * p.span < tokens && (long long)p.spans * p.span >= tokens;
+    for (uint32_t b = 0; ok && b < p.spans; ++b) {
+      const int start = (int)b * p.span, end = sf::span_end(start, p.span, (int)tokens);
+      const long long want = (long long)(b + 1) * p.span;
+      ok = end == (want < tokens ? want : tokens);
+      for (int w = 0; ok && w < step && w < end - start; ++w) {
+        const long long last = start + w + ((long long)end - 1 - start - w) / step * step;
+        int token = start + w;
+        ok = sf::row_ahead(token, step, end) == (token + (long long)step < end ? token + (long long)step : end - 1);
+        if (last - 3ll * step > token) token = (int)(last - 3ll * step);
+        for (;; token += step) {
+          const int ahead = sf::row_ahead(token, step, end);
+          ok = ok && token <= last && ahead >= start && ahead < end;
+          if (!(ok && step < end - token)) break;
+          ok = ahead == token + step;
+        }
+        ok = ok && token == last;
+      }
+    }
+    if (!ok) {
+      printf("%lld x %lld, %d rows at once, %lld groups: span %d, %u spans\n", samples, tokens, step, groups, p.span, p.spans);
+      return 1;
+    }
+  }
+}
+"""
+
+
+def test_workgroups_cover_a_samples_rows(tmp_path_factory):
+    """Up to the largest count of tokens that a call takes, where the first row past the last workgroup's is 2^31."""
+    top = (1 << 31) - 1
+    counts = (1, 2, 3, 4, 5, 1001, 2048, 16384, 1 << 21, (1 << 21) + 1, (1 << 30) + 5, top - (1 << 21), top - (1 << 21) + 1, top - 4, top - 3,
+              top - 1, top)
+    calls = [(s, t, step, g) for t in counts for s in sorted({1, 2, 3, 1000, top // t}) if s * t <= top for step in (1, 4)
+             for g in (512, 768, 1024)]
+    r = subprocess.run([_compiled(tmp_path_factory, "spans", SPANS)], input="".join("%d %d %d %d\n" % c for c in calls),
+                       capture_output=True, text=True, timeout=60)
+    assert r.returncode == 0, r.stdout
