@@ -101,7 +101,8 @@ __device__ __forceinline__ void normalise(float (&x)[NV][4], int kind, const Res
         for (int i = 0; i < NV; ++i)
 #pragma unroll
           for (int c = 0; c < 4; ++c) x[i][c] = __builtin_amdgcn_ldexpf(x[i][c], by);
-        eps = __builtin_amdgcn_ldexpf(__builtin_amdgcn_ldexpf(eps, by), by);
+        // of large rows it would become 0, and a deviation of 0 times 1 / sqrt(0) NaN; next to another one this is nothing
+        if (eps > 0.0f) eps = fmaxf(__builtin_amdgcn_ldexpf(__builtin_amdgcn_ldexpf(eps, by), by), 0x1p-126f);
         continue;
       }
     }
