@@ -468,7 +468,8 @@ int sf_gated_matmul_f8(const sf_codes* a, const sf_codes* gate, const sf_codes* 
  * A norm is SF_NORM_RMS, x / sqrt(mean x^2 + eps), SF_NORM_LAYER, (x - mean) / sqrt(variance + eps)
  * (biased variance), or SF_NORM_NONE. pre reads h' before its rounding to h's type. Everything in
  * fp32, one rounding to each output's type; a row whose squares fp32 does not hold is scaled by a power of
- * two first, so finite rows of every size are normalised.
+ * two first, so finite rows of every size are normalised. SF_NORM_LAYER of a row of one value is 0 (eps > 0; NaN for
+ * eps 0, as SF_NORM_RMS of a row of zeros), also where its mean is rounded.
  * h, h_out: element type h_type; h_out may be h itself with the same strides. y: y_type. out: out_type (NULL:
  * h' alone; the fields of a are not read then), SF_TYPE_F8 for codes with a scale per row and block of
  * 128 dims in out_scale as sf_quantize_f8 makes them (strides of out multiples of 16 then, at an

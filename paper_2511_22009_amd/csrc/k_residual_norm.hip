@@ -64,7 +64,9 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, float* lds) {
 
 // x of a row (pieces of four, zeros past D, also afterwards) becomes its norm without a gain. Where the squares or the sum leave
 // what fp32 holds to full precision, the row is scaled by a power of two first, so finite rows of
-// every size are normalised.
+// every size are normalised. A mean that is rounded stays in every deviation; where it is over 16 deviations large, what it
+// left (of nearly one value, small multiples of one step, exactly) is normalised in the row's place, so a
+// row of one value becomes 0. With that done always, 2760 x 771 rows took 10.9 us instead of 9.8.
 template <int NV, int WAVES>
 __device__ __forceinline__ void normalise(float (&x)[NV][4], int kind, const ResidualNormArgs& a, int first, float* lds) {
   constexpr int STEP = WAVES * 256;
@@ -75,18 +77,18 @@ __device__ __forceinline__ void normalise(float (&x)[NV][4], int kind, const Res
 #pragma unroll
       for (int i = 0; i < NV; ++i) sum += (x[i][0] + x[i][1]) + (x[i][2] + x[i][3]);
       sum = row_sum<WAVES>(sum, lds);
-      mean = sum / (float)a.D;
+      if (again > 0 || fabsf(sum) < 1e30f) mean = sum / (float)a.D;  // fp32's largest numbers stay so without it
     }
     float q = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float c = first + i * STEP + e < a.D ? x[i][e] - mean : 0.0f;
-        q = __builtin_fmaf(c, c, q);
+        x[i][e] = first + i * STEP + e < a.D ? x[i][e] - mean : 0.0f;
+        q = __builtin_fmaf(x[i][e], x[i][e], q);
       }
     q = row_sum<WAVES>(q, lds);
-    if (again == 0 && !(q < 1e37f && q > 1e-28f && fabsf(sum) < 1e37f)) {
+    if (again == 0 && !(q < 1e37f && q > 1e-28f && fabsf(sum) < 1e30f)) {
       uint32_t top = 0;
 #pragma unroll
       for (int i = 0; i < NV; ++i)
@@ -105,12 +107,15 @@ __device__ __forceinline__ void normalise(float (&x)[NV][4], int kind, const Res
         if (eps > 0.0f) eps = fmaxf(__builtin_amdgcn_ldexpf(__builtin_amdgcn_ldexpf(eps, by), by), 0x1p-126f);
         continue;
       }
+      if (kind == NORM_LAYER && top >= 0x7f800000u) q = __uint_as_float(0x7fc00000u);  // as a mean that is not finite leaves it
     }
-    const float by = 1.0f / sqrtf(q / (float)a.D + eps);
+    q /= (float)a.D;
+    if (again < 3 && q < 0x1p-8f * mean * mean) continue;
+    const float by = 1.0f / sqrtf(q + eps);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[i][e] = first + i * STEP + e < a.D ? (x[i][e] - mean) * by : 0.0f;
+      for (int e = 0; e < 4; ++e) x[i][e] *= by;
     return;
   }
 }

@@ -4,7 +4,7 @@ import pytest
 pytestmark = pytest.mark.gpu
 
 from gpu_util import torch  # noqa: E402
-from f8_util import BF16, F8, FP32  # noqa: E402
+from f8_util import BF16, F8, FP32, U, gen, worst  # noqa: E402
 
 ids = lambda v: str(v).replace("torch.", "")  # noqa: E731
 
@@ -61,3 +61,53 @@ def constant_rows(D, dtype, eps=1e-6):
 def test_layer_norm_of_constant_rows(D, dtype, eps):
     """No deviation and an eps above 0: the norm is 0, whatever the size. Sums of powers of two of one value are exact."""
     constant_rows(D, dtype, eps)
+
+
+@pytest.mark.parametrize("eps", [1e-6, 1e-30])
+@pytest.mark.parametrize("dtype", [BF16, FP32, F8], ids=ids)
+@pytest.mark.parametrize("D", [3, 5, 100, 129, 257, 770, 771, 1000, 1152, 1276, 1800, 3000, 5000, 8191, 16384])
+def test_layer_norm_of_constant_rows_whose_mean_is_rounded(D, dtype, eps):
+    """A mean that is some steps off leaves a deviation of that in every value, and their mean takes it off."""
+    constant_rows(D, dtype, eps)
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+@pytest.mark.parametrize("D", [2, 5, 128, 257, 770, 1000, 1152, 2044, 5000, 16384])
+def test_layer_norm_of_rows_of_nearly_one_value(D, eps):
+    """Values a few steps of fp32 apart: their deviations are whole steps, which the mean's rounding must not hide.
+
+    What the first mean leaves are whole steps, exactly; of these the mean is off by U of it, each deviation by U of itself, and
+    so is what their own mean takes off: under 4 U of the row's largest deviation. The root of the mean square has as many
+    roundings of a partial sum as in f8_util.norm, and six more."""
+    from paper_2511_22009_amd import residual_norm
+    g = gen(D)
+    for n in (1, 200):
+        base = torch.tensor([1e-30, 1e-10, 1.0, 1000.1, 1e10, 1e15, 1e20, 1e30, 3e38], device="cuda") * (1 - 0.3 * torch.rand(9, generator=g, device="cuda"))
+        base = torch.cat([base, -base])
+        steps = torch.randint(-3, 4, (18, D), generator=g, device="cuda", dtype=torch.int32)
+        steps[::3] *= torch.rand((6, D), generator=g, device="cuda") < 0.1
+        steps[1::3] = 0
+        steps[:, 0] = 1                                    # at least one value is another
+        steps[:, -1] = 0
+        x = (base.view(torch.int32)[:, None] + steps).view(FP32)
+        off = x.double() - base.double()[:, None]
+        off = off - off.mean(-1, keepdim=True)
+        want = off / (off.square().mean(-1, keepdim=True) + eps).sqrt()
+        allowed = (want.abs() + want.abs().amax(-1, keepdim=True)) * (D / 64 + 12 + 10) * U
+        x, y = x.repeat(n, 1), torch.zeros((18 * n, D), device="cuda")
+        pre = residual_norm(x, y, pre="layer", dtype=FP32, eps=eps)[1]
+        post = residual_norm(y, x, post="layer", eps=eps)[0]
+        assert worst(pre, want.repeat(n, 1), allowed.repeat(n, 1)) <= 1.0
+        assert worst(post, want.repeat(n, 1), allowed.repeat(n, 1)) <= 1.0
+
+
+def test_layer_norm_next_to_the_largest_number():
+    """Rows whose values lose fp32's range when their mean is taken off, but for a scale."""
+    from paper_2511_22009_amd import residual_norm
+    top = torch.finfo(FP32).max
+    x = torch.tensor([[top, -top * (1 - 2.0 ** -5)], [top, -top], [top, 0.0], [-top, -top * (1 - 2.0 ** -20)]], device="cuda")
+    for D in (2, 1152):
+        h = x.repeat(1, D // 2)
+        out = residual_norm(h, torch.zeros_like(h), pre="layer", dtype=FP32)[1]
+        assert worst(out, torch.tensor([1.0, -1.0], device="cuda", dtype=torch.float64).repeat(4, D // 2) * torch.tensor([[1], [1], [1], [-1.0]], device="cuda"),
+                     torch.full((4, D), (D / 64 + 32) * U, device="cuda", dtype=torch.float64)) <= 1.0
