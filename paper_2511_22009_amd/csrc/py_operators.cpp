@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/core/GradMode.h>
 #include <torch/csrc/Exceptions.h>
@@ -63,6 +64,8 @@ const at::Tensor& tensor(PyObject* o, const char* what, std::initializer_list<at
   const at::Tensor& t = THPVariable_Unpack(o);
   if (t.requires_grad() && c10::GradMode::is_enabled())
     bad_type(what, ": requires grad, and nothing here is differentiated; call under torch.no_grad() or detach it");
+  if (c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(0).defined())
+    bad_type(what, ": carries a forward-mode tangent, and nothing here is differentiated; call with the primal that unpack_dual() gives");
   if (t.is_neg()) bad_type(what, ": a lazily negated view, whose memory holds the opposite values; call resolve_neg()");
   for (const at::ScalarType s : types)
     if (t.scalar_type() == s) return t;

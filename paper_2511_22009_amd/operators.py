@@ -10,7 +10,8 @@ its tensors, on `stream` or torch's current stream there. Outputs that are not g
 allocated for that stream. With a `stream` other than the current one, ordering it after
 the work that fills the inputs is the caller's, as in torch; the inputs' memory is kept
 until the stream is done with it. Nothing is differentiated: a tensor that requires grad is
-a TypeError unless gradients are off (torch.no_grad, torch.inference_mode).
+a TypeError unless gradients are off (torch.no_grad, torch.inference_mode), and so is one
+that carries a forward-mode tangent.
 """
 import ctypes
 
