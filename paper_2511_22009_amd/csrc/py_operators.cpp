@@ -131,8 +131,14 @@ PyObject* pair(PyObject* a, PyObject* b) {
   Py_XDECREF(b);
   return r;
 }
+// A call's result: the tensor that was given for it, which has new values now (a backward pass that had kept the
+// old ones has to see that, as after torch's own calls), or the one made here.
 PyObject* given_or(PyObject* given, const at::Tensor& made) {
-  if (given != Py_None) return Py_NewRef(given);
+  if (given != Py_None) {
+    const at::Tensor& t = THPVariable_Unpack(given);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    return Py_NewRef(given);
+  }
   return THPVariable_Wrap(made);
 }
 

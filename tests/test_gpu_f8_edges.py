@@ -4,7 +4,7 @@ import pytest
 pytestmark = pytest.mark.gpu
 
 from gpu_util import torch  # noqa: E402
-from f8_util import BF16, F8, FP32, U, gen, worst  # noqa: E402
+from f8_util import BF16, F8, FP32, U, gen, randn, worst  # noqa: E402
 
 ids = lambda v: str(v).replace("torch.", "")  # noqa: E731
 
@@ -111,3 +111,64 @@ def test_layer_norm_next_to_the_largest_number():
         out = residual_norm(h, torch.zeros_like(h), pre="layer", dtype=FP32)[1]
         assert worst(out, torch.tensor([1.0, -1.0], device="cuda", dtype=torch.float64).repeat(4, D // 2) * torch.tensor([[1], [1], [1], [-1.0]], device="cuda"),
                      torch.full((4, D), (D / 64 + 32) * U, device="cuda", dtype=torch.float64)) <= 1.0
+
+
+def given_results():
+    """(results that are given, call that writes them) for every operator."""
+    from paper_2511_22009_amd import (Rotary, gated_matmul_f8, matmul_f8, matmul_i8, qk_norm_rotate, quantize_f8, quantize_rows,
+                                      residual_norm, rotate)
+    g = gen(11)
+    x, h, pos, y = randn(g, 40, 64), randn(g, 2, 5, 3, 64), randn(g, 5, 2), randn(g, 40, 64)
+    r, f8 = Rotary([32, 32]), lambda t: torch.zeros_like(t).to(F8)
+    i8, si8 = quantize_rows(x)
+    a, sa = quantize_f8(x)
+    w, sw = quantize_f8(x, 128)
+    e = lambda *s: torch.zeros(s, device="cuda")  # noqa: E731
+    for call, outs in (
+            (lambda o, s: quantize_rows(x, o, s), (torch.zeros_like(i8), e(40))), (lambda o: matmul_i8(i8, si8, i8, si8, out=o), (e(40, 40),)),
+            (lambda o: rotate(o, pos, r, out=o), (h.clone(),)),
+            (lambda q, k: qk_norm_rotate(q, k, positions=pos, rotary=r, out=(q, k)), (h.clone(), h.clone())),
+            (lambda o, s: quantize_f8(x, 1, o, s), (f8(x), e(40, 1))), (lambda o: matmul_f8(a, sa, w, sw, out=o), (e(40, 40),)),
+            (lambda o, s: gated_matmul_f8(a, sa, w, sw, w, sw, out=o, out_scale=s), (f8(e(40, 48))[:, :40], e(40, 1))),
+            (lambda o, n, s: residual_norm(o, y, pre="rms", h_out=o, out=n, out_scale=s), (x.clone(), f8(x), e(40, 1)))):
+        yield outs, call
+
+
+def test_results_that_are_given_count_as_changed():
+    """A backward pass that kept the old values ends with an error, as after torch's own writes."""
+    for outs, call in given_results():
+        before = [t._version for t in outs]
+        call(*outs)
+        assert [t._version for t in outs] == [v + 1 for v in before]
+    from paper_2511_22009_amd import residual_norm
+    h = torch.ones((4, 64), device="cuda")
+    w = torch.ones((4, 64), device="cuda", requires_grad=True)
+    loss = (w * h).sum()
+    residual_norm(h, h.clone(), h_out=h)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+
+
+def test_results_that_are_given_in_inference_mode():
+    with torch.inference_mode():
+        for outs, call in given_results():
+            call(*outs)
+        room = torch.zeros((4, 64), device="cuda")
+    from paper_2511_22009_amd import residual_norm
+    with torch.no_grad():
+        assert residual_norm(room, torch.ones((4, 64), device="cuda"), h_out=room)[0] is room and bool((room == 1).all())
+
+
+def test_tensors_with_a_forward_mode_tangent_are_refused():
+    import torch.autograd.forward_ad as fw
+    from paper_2511_22009_amd import quantize_f8, quantize_rows, residual_norm
+    x = randn(gen(12), 4, 64)
+    for call in (quantize_rows, quantize_f8, lambda t: residual_norm(t, x, pre="rms"), lambda t: residual_norm(x, x, pre="rms", pre_gain=t[0])):
+        want = call(x)
+        with torch.no_grad(), fw.dual_level():
+            d = fw.make_dual(x, torch.ones_like(x))
+            with pytest.raises(TypeError, match="tangent"):
+                call(d)
+            got = call(fw.unpack_dual(d).primal)
+        for p, q in zip(got, want):
+            assert torch.equal(p.float(), q.float())
