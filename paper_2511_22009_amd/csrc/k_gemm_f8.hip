@@ -685,24 +685,28 @@ static void launch_few(const GemmF8Args& a, hipStream_t s) {
 template <F8Out OUT, F8Act ACT>
 static hipError_t launch_f8(const GemmF8Args& a, hipStream_t s) {
   constexpr bool kGated = ACT != F8_NONE;
-  F8Tile tile = choose_gemm_f8_tile(a.M, (long)a.N * (kGated ? 2 : 1), a.K, OUT == F8_CODES, OUT == F8_F32, kGated);
-  switch (tile) {
+  const F8Tile tile = choose_gemm_f8_tile(a.M, (long)a.N * (kGated ? 2 : 1), a.K, OUT == F8_CODES, OUT == F8_F32, kGated);
+  switch (tile) {  // a tile without a kernel of this kind, which the rule does not give, is no answer
     case kF8Few:
-      if constexpr (f8_has_tile(kF8Few, OUT == F8_CODES, OUT != F8_BF16)) launch_few<OUT, ACT>(a, s);
+      if constexpr (f8_has_tile(kF8Few, OUT == F8_CODES, OUT != F8_BF16)) {
+        launch_few<OUT, ACT>(a, s);
+        return hipGetLastError();
+      }
       break;
-#define SF_F8_CASE(id, bm, bn, wm, wn, wk, st, mw)                                                              \
-  case id: {                                                                                                  \
-    constexpr int on = kGated ? bn / 2 : bn;                                                                  \
-    const int64_t tiles = (((int64_t)a.M + bm - 1) / bm) * (((int64_t)a.N + on - 1) / on);                    \
-    if (tiles > 0x7fffffff) return hipErrorInvalidValue;                                                      \
-    if constexpr (f8_has_tile(id, OUT == F8_CODES, OUT != F8_BF16))                              \
-      launch(gemm_f8_kernel<bm, bn, wm, wn, wk, st, mw, OUT, ACT>, dim3((uint32_t)tiles), dim3(wm * wn * wk * 64), 0, s, a); \
-    break;                                                                                                    \
-  }
+#define SF_F8_CASE(id, bm, bn, wm, wn, wk, st, mw)                                                                               \
+  case id:                                                                                                                       \
+    if constexpr (f8_has_tile(id, OUT == F8_CODES, OUT != F8_BF16)) {                                                            \
+      constexpr int on = kGated ? bn / 2 : bn;                                                                                   \
+      const int64_t tiles = (((int64_t)a.M + bm - 1) / bm) * (((int64_t)a.N + on - 1) / on);                                     \
+      if (tiles > 0x7fffffff) break;                                                                                             \
+      launch(gemm_f8_kernel<bm, bn, wm, wn, wk, st, mw, OUT, ACT>, dim3((uint32_t)tiles), dim3(wm * wn * wk * 64), 0, s, a);     \
+      return hipGetLastError();                                                                                                  \
+    }                                                                                                                            \
+    break;
     SF_F8_TILES(SF_F8_CASE)
 #undef SF_F8_CASE
   }
-  return hipGetLastError();
+  return hipErrorInvalidValue;
 }
 
 static hipError_t launch_part(F8Out kind, F8Act act, const GemmF8Args& a, hipStream_t s) {
