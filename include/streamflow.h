@@ -442,9 +442,14 @@ int sf_quantize_f8(const void* x, int type, long long rows, int cols, long long 
  * a: M rows, a scale per row and block; b: N rows of weights, a scale per 128 rows and block. Sums over
  * a block on the matrix cores: for fp32 outputs (and outputs that are codes) in fp32; for bf16 eight products of
  * adjacent k are added to each other first, each cut off below 2^-13 of the largest one's power of two, which is
- * twice as fast and some 1.5e-5 of a result, and the eights then in fp32. sa sb rounded to fp32 (so beyond its range
+ * twice as fast, and the eights then in fp32. On codes of a bell that is some 1.5e-5 of a result, a hundredth of what its
+ * rounding to bf16 costs (one output in fifty to a hundred is the neighbour of the exact sum's bf16); where products cancel, it
+ * is measured by the products and not by what is left of them. sa sb rounded to fp32 (so beyond its range
  * it is lost); its product with the block's sum added to the sum over blocks with one rounding to fp32; the
- * output's type last. bias: fp32 [N] or NULL. out: [M][N], row length ldo >= N, element type out_type
+ * output's type last. The order in which blocks are added goes by M, N, K and the output's type (K is shared out where
+ * there are few rows or few tiles, and a product may be two launches with an order each): the same call gives the
+ * same bits every time, but a row of a call with other rows, or with more of them, may differ in the last bits of its fp32
+ * sums. (Outputs that are codes, below, have one order, block after block, whatever the call's size.) bias: fp32 [N] or NULL. out: [M][N], row length ldo >= N, element type out_type
  * (SF_PREC_*), any alignment of its elements. K 1..1048576, M and N from 0 on. */
 int sf_matmul_f8(const sf_codes* a, const sf_codes* b, const float* bias, int M, int N, int K, void* out, long long ldo,
                  int out_type, void* hip_stream);
@@ -468,7 +473,8 @@ int sf_gated_matmul_f8(const sf_codes* a, const sf_codes* gate, const sf_codes* 
  * A norm is SF_NORM_RMS, x / sqrt(mean x^2 + eps), SF_NORM_LAYER, (x - mean) / sqrt(variance + eps)
  * (biased variance), or SF_NORM_NONE. pre reads h' before its rounding to h's type. Everything in
  * fp32, one rounding to each output's type; a row whose squares fp32 does not hold is scaled by a power of
- * two first, so finite rows of every size are normalised. SF_NORM_LAYER of a row of one value is 0 (eps > 0; NaN for
+ * two first, so finite rows of every size are normalised. gate post_gain and pre_gain (1 + scale) are multiplied with each
+ * other first (beyond fp32's range such a factor is lost). SF_NORM_LAYER of a row of one value is 0 (eps > 0; NaN for
  * eps 0, as SF_NORM_RMS of a row of zeros), also where its mean is rounded.
  * h, h_out: element type h_type; h_out may be h itself with the same strides. y: y_type. out: out_type (NULL:
  * h' alone; the fields of a are not read then), SF_TYPE_F8 for codes with a scale per row and block of

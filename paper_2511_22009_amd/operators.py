@@ -164,7 +164,11 @@ def quantize_f8(x, block_rows=1, out=None, scale=None, stream=None):
 def matmul_f8(a, a_scale, b, b_scale, bias=None, dtype=torch.bfloat16, out=None, stream=None):
     """a [M, K] (codes of `quantize_f8`, a scale per row and block) times b [N, K] transposed
     (a scale per 128 rows and block), plus bias [N] (fp32): [M, N] in `dtype` (bfloat16 or
-    float32), or in `out`, whose columns are adjacent and whose type then holds."""
+    float32), or in `out`, whose columns are adjacent and whose type then holds. Sums are fp32's
+    for float32; for bfloat16 each eight adjacent products are added with those below 2^-13 of
+    the largest cut off there, at twice the rate: some 1.5e-5 of a result, more of one whose
+    products cancel. The order in which blocks of K are added goes by the sizes, so the last bits
+    of a row's sums may differ from those in a call with more or fewer rows."""
     kind = _of(_TYPES, dtype, "dtype")
     if stream is not None:
         return _aside(stream, (a, a_scale, b, b_scale, bias), _ext.matmul_f8, a, a_scale, b, b_scale, bias, kind, out)
@@ -176,8 +180,9 @@ def gated_matmul_f8(a, a_scale, gate, gate_scale, up, up_scale, gate_bias=None, 
     """act(a gate^T + gate_bias) * (a up^T + up_bias), the first half of a gated feed-forward,
     operands as in `matmul_f8`; activation "silu" or "gelu_tanh". [M, N] in `dtype`
     (bfloat16 or float32) or, for float8_e4m3fn, (codes, scale) as `quantize_f8` makes them
-    of the fp32 values, for the projection that follows. `out` and `out_scale` take the
-    results where they are given; out's type then holds."""
+    of the fp32 values, for the projection that follows. Sums as in `matmul_f8`: those of
+    bfloat16 outputs at twice the rate, those of float32 outputs and of codes in fp32. `out` and
+    `out_scale` take the results where they are given; out's type then holds."""
     kind, act = _of(_TYPES_OR_CODES, dtype, "dtype"), _of(_ACTS, activation, "activation")
     if stream is not None:
         return _aside(stream, (a, a_scale, gate, gate_scale, up, up_scale, gate_bias, up_bias), _ext.gated_matmul_f8, a, a_scale, gate,

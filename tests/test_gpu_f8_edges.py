@@ -4,6 +4,7 @@ import pytest
 pytestmark = pytest.mark.gpu
 
 from gpu_util import torch  # noqa: E402
+import f8_util as P  # noqa: E402
 from f8_util import BF16, F8, FP32, U, gen, randn, worst  # noqa: E402
 
 ids = lambda v: str(v).replace("torch.", "")  # noqa: E731
@@ -172,3 +173,40 @@ def test_tensors_with_a_forward_mode_tangent_are_refused():
             got = call(fw.unpack_dual(d).primal)
         for p, q in zip(got, want):
             assert torch.equal(p.float(), q.float())
+
+
+@pytest.mark.parametrize("N,K", [(1152, 1152), (300, 4400), (4200, 1601)])
+def test_rows_do_not_see_each_other_but_for_the_order_of_sums(N, K):
+    """Codes whose products are multiples of 2^-6 and scales of 1: every sum is below 14.1 K < 2^17 and a multiple of 2^-6, so exact
+    in fp32 in every order. Then a row has the same bits in calls of every size, tile and number of launches."""
+    from paper_2511_22009_amd import gated_matmul_f8, matmul_f8
+    g = gen(N + K)
+    M = 4160
+    (a, sa), (w, sw), (u, su) = (P.codes(g, n, K, b) for n, b in ((M, 1), (N, 128), (N, 128)))
+    for q in (a, w, u):
+        P.narrow(q)
+    sa, sw, su = sa.sign(), sw.sign(), su.sign()
+    small = 2.0 ** -12
+    for call in (lambda m: matmul_f8(a[m], sa[m], w, sw), lambda m: matmul_f8(a[m], sa[m], w, sw, dtype=FP32),
+                 lambda m: gated_matmul_f8(a[m], sa[m], w, sw * small, u, su, dtype=BF16),
+                 lambda m: gated_matmul_f8(a[m], sa[m], w, sw * small, u, su, dtype=FP32),
+                 lambda m: gated_matmul_f8(a[m], sa[m], w, sw * small, u, su, dtype=F8)):
+        whole = call(slice(0, M))
+        for m in (slice(0, 1), slice(7, 23), slice(1, 33), slice(100, 165), slice(1000, 1300), slice(3000, 4100), slice(4100, M)):
+            part = call(m)
+            for p, q in zip(*((v if isinstance(v, tuple) else (v,)) for v in (part, whole))):
+                p, q = (t.view(torch.uint8) if t.dtype == F8 else t for t in (p, q[m]))
+                assert torch.equal(p, q)
+
+
+def test_rows_that_become_codes_do_not_see_each_other():
+    """Their blocks are added in one order in every tile and part: the same bits, whatever else is in the call."""
+    from paper_2511_22009_amd import gated_matmul_f8
+    for M, N, K in ((2100, 2048, 2301), (1300, 300, 1152)):
+        g = gen(M)
+        (a, sa), (w, sw), (u, su) = (P.codes(g, n, K, b) for n, b in ((M, 1), (N, 128), (N, 128)))
+        call = lambda m: gated_matmul_f8(a[m], sa[m], w, sw, u, su, activation="gelu_tanh", dtype=F8)  # noqa: E731
+        q, s = call(slice(0, M))
+        for m in (slice(0, 1), slice(5, 38), slice(600, 900), slice(200, M - 1)):
+            p, t = call(m)
+            assert torch.equal(p.view(torch.uint8), q[m].view(torch.uint8)) and torch.equal(t, s[m])
