@@ -286,28 +286,24 @@ static void launch_rows(ResidualNormArgs a, hipStream_t s) {
   });
 }
 
-// A wavefront per row where there are many, else a workgroup, whose lanes each wait for less.
+#define SF_NORM_TILES(X) X(1, 1) X(3, 1) X(4, 1) X(5, 1) X(1, 4) X(2, 4) X(4, 4) X(2, 16) X(4, 16)
+
 template <typename TH, typename TY, NormOut OUT>
 static hipError_t launch_t(const ResidualNormArgs& a, hipStream_t s) {
-  const bool many = (int64_t)a.samples * a.tokens >= 2048;
-  if (a.D % 4 == 0) {
-    if (a.D <= 256) launch_rows<TH, TY, OUT, 1, 1, true>(a, s);
-    else if (a.D <= 768 && many) launch_rows<TH, TY, OUT, 3, 1, true>(a, s);
-    else if (a.D <= 1024 && many) launch_rows<TH, TY, OUT, 4, 1, true>(a, s);
-    else if (a.D <= 1280 && many) launch_rows<TH, TY, OUT, 5, 1, true>(a, s);
-    else if (a.D <= 1024) launch_rows<TH, TY, OUT, 1, 4, true>(a, s);
-    else if (a.D <= 2048) launch_rows<TH, TY, OUT, 2, 4, true>(a, s);
-    else if (a.D <= 4096) launch_rows<TH, TY, OUT, 4, 4, true>(a, s);
-    else if (a.D <= 8192) launch_rows<TH, TY, OUT, 2, 16, true>(a, s);
-    else launch_rows<TH, TY, OUT, 4, 16, true>(a, s);
-  } else {
-    if (a.D <= 256) launch_rows<TH, TY, OUT, 1, 1, false>(a, s);
-    else if (a.D <= 1024) launch_rows<TH, TY, OUT, 1, 4, false>(a, s);
-    else if (a.D <= 2048) launch_rows<TH, TY, OUT, 2, 4, false>(a, s);
-    else if (a.D <= 8192) launch_rows<TH, TY, OUT, 2, 16, false>(a, s);
-    else launch_rows<TH, TY, OUT, 4, 16, false>(a, s);
+  const NormTile t = choose_norm_tile((int64_t)a.samples * a.tokens, a.D);
+#define SF_NORM_CASE(nv, w)                                                                            \
+  if (t.pieces == nv && t.waves == w) {                                                                \
+    if (a.D % 4 == 0)                                                                                  \
+      launch_rows<TH, TY, OUT, nv, w, true>(a, s);                                                     \
+    else if constexpr (norm_has_tile(NormTile{nv, w}, false))                                          \
+      launch_rows<TH, TY, OUT, nv, w, false>(a, s);                                                    \
+    else                                                                                               \
+      return hipErrorInvalidValue;                                                                     \
+    return hipGetLastError();                                                                          \
   }
-  return hipGetLastError();
+  SF_NORM_TILES(SF_NORM_CASE)
+#undef SF_NORM_CASE
+  return hipErrorInvalidValue;
 }
 
 template <typename TH, typename TY>

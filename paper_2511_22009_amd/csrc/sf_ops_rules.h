@@ -205,6 +205,25 @@ inline void in_parts(int64_t count, int64_t most, F call) {
   for (int64_t first = 0; first < count; first += most) call(first, count - first < most ? count - first : most);
 }
 
+// Pieces of four dims that a lane holds of a row, and wavefronts that share it. A wavefront takes a row where there are many,
+// else a workgroup does, whose lanes each wait for less. `whole`: D is a multiple of four.
+struct NormTile {
+  int pieces, waves;
+};
+constexpr NormTile choose_norm_tile(int64_t rows, int D) {
+  const bool whole = D % 4 == 0, many = whole && rows >= 2048;
+  return D <= 256            ? NormTile{1, 1}
+         : many && D <= 768  ? NormTile{3, 1}
+         : many && D <= 1024 ? NormTile{4, 1}
+         : many && D <= 1280 ? NormTile{5, 1}
+         : D <= 1024         ? NormTile{1, 4}
+         : D <= 2048         ? NormTile{2, 4}
+         : whole && D <= 4096 ? NormTile{4, 4}
+         : D <= 8192         ? NormTile{2, 16}
+                             : NormTile{4, 16};
+}
+constexpr bool norm_has_tile(NormTile t, bool whole) { return whole || !(t.pieces > 2 && t.waves < 16); }
+
 // Workgroups that take `step` rows at once, about `groups` of them: `span` rows of one sample each, `spans` to a
 // sample, and `most` samples in a launch, since a grid holds less than 2^32 threads.
 struct NormSpans {

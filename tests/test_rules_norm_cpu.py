@@ -1,8 +1,11 @@
 """How the rows around a block are shared out over launches and workgroups, compiled for the host from the header that the
 kernels include."""
+import ast
+import os
+import re
 import subprocess
 
-from test_rules_cpu import _compiled
+from test_rules_cpu import CSRC, ROOT, _compiled
 
 PARTS = r"""
 #include <cstdio>
@@ -87,3 +90,45 @@ def test_workgroups_cover_a_samples_rows(tmp_path_factory):
     r = subprocess.run([_compiled(tmp_path_factory, "spans", SPANS)], input="".join("%d %d %d %d\n" % c for c in calls),
                        capture_output=True, text=True, timeout=60)
     assert r.returncode == 0, r.stdout
+
+
+TILES = r"""
+#include <cstdio>
+#include "sf_ops_rules.h"
+// Reads rows D, prints the pieces and wavefronts of a row, and whether that holds it and has a kernel.
+int main() {
+  long long rows;
+  int D;
+  while (scanf("%lld %d", &rows, &D) == 2) {
+    const sf::NormTile t = sf::choose_norm_tile(rows, D);
+    printf("%d %d %d\n", t.pieces, t.waves, (int)(256 * t.pieces * t.waves >= D && sf::norm_has_tile(t, D % 4 == 0)));
+  }
+}
+"""
+
+
+def _tiles(tmp_path_factory, calls):
+    out = subprocess.run([_compiled(tmp_path_factory, "tiles", TILES)], input="".join("%d %d\n" % c for c in calls), capture_output=True,
+                         text=True, check=True, timeout=60).stdout.split()
+    out = [int(v) for v in out]
+    return list(zip(out[::3], out[1::3], (d % 4 == 0 for _, d in calls))), out[2::3]
+
+
+def test_a_row_fits_what_takes_it(tmp_path_factory):
+    calls = [(rows, d) for d in range(1, 16385) for rows in (1, 2047, 2048, 1 << 20)]
+    tiles, fit = _tiles(tmp_path_factory, calls)
+    assert len(fit) == len(calls) and all(fit)
+    kernels = open(os.path.join(CSRC, "k_residual_norm.hip")).read()
+    named = {(int(p), int(w)) for p, w in re.findall(r"X\((\d+), (\d+)\)", kernels)}
+    assert named == {t[:2] for t in tiles}
+
+
+def test_the_gpu_tests_reach_every_kernel_of_the_norms(tmp_path_factory):
+    tree = ast.parse(open(os.path.join(ROOT, "tests", "test_gpu_norm_tiles.py")).read())
+    few, many = (next(ast.literal_eval(n.value) for n in tree.body if isinstance(n, ast.Assign) and n.targets[0].id == name)
+                 for name in ("FEW", "MANY"))
+    every = set(_tiles(tmp_path_factory, [(rows, d) for d in range(1, 16385) for rows in (1, 2048)])[0])
+    assert all(s * t < 2048 for s, t, _ in few) and all(s * t >= 2048 for s, t, _ in many)
+    assert set(_tiles(tmp_path_factory, [(s * t, d) for s, t, d in few + many])[0]) == every
+    only_many = every - set(_tiles(tmp_path_factory, [(1, d) for d in range(1, 16385)])[0])
+    assert only_many == {(3, 1, True), (4, 1, True), (5, 1, True)}
