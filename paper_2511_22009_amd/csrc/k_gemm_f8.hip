@@ -725,6 +725,7 @@ static hipError_t launch_part(F8Out kind, F8Act act, const GemmF8Args& a, hipStr
   return hipErrorInvalidValue;
 }
 
+// Events for a launch's own times (t_launch_events) go to the first part alone; nothing times these calls by them.
 hipError_t launch_gemm_f8(F8Out kind, F8Act act, const GemmF8Args& a, hipStream_t s) {
   const int sides = act == F8_NONE ? 1 : 2;
   long rows, cols;

@@ -9,6 +9,7 @@
 #include <initializer_list>
 
 #include "sf_ops.h"
+#include "sf_ops_rules.h"
 
 namespace sf {
 
@@ -135,16 +136,15 @@ int f8_call(const sf_codes* a, const sf_codes* b, const sf_codes* up, const floa
   if (codes && (!out_scale || !aligned16(out) || ldo % 16 || !own_scales(M, (N - 1) / SF_F8_BLOCK + 1, scale_row, scale_block)))
     return SF_E_INVAL;
   const int64_t size = codes ? 1 : out_type == SF_PREC_BF16 ? 2 : 4;
-  // grids this large have tiles of at least 32 outputs to a thread: 2^36 outputs are 2^31 threads at most
-  const int64_t most = std::min<int64_t>(kMostRows, (1ll << 36) / std::min<int64_t>(N, kMostRows) / 256 * 256);
+  const int64_t most = sf::f8_most_rows(N);
   for (int64_t m = 0; m < M; m += most)
-    for (int64_t n = 0; n < N; n += kMostRows) {  // a multiple of 128
+    for (int64_t n = 0; n < N; n += sf::kF8MostColumns) {
       sf::GemmF8Args g{};
       g.a = take_codes(a, m, 1);
       g.b = take_codes(b, n, SF_F8_BLOCK);
       if (up) g.up = take_codes(up, n, SF_F8_BLOCK);
       g.M = (int)std::min<int64_t>(most, M - m);
-      g.N = (int)std::min<int64_t>(kMostRows, N - n);
+      g.N = (int)std::min<int64_t>(sf::kF8MostColumns, N - n);
       g.K = K;
       g.bias = bias ? bias + n : nullptr;
       g.up_bias = up_bias ? up_bias + n : nullptr;

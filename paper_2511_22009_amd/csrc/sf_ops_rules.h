@@ -196,6 +196,14 @@ inline void choose_gemm_f8_parts(long M, long N, long K, bool codes, bool exact,
   }
 }
 
+// Columns (outputs) and rows of one launch of a product, whose grid holds less than 2^32 threads: longer calls are several.
+// Grids this large have tiles of at least 32 outputs to a thread, so 2^36 outputs are 2^31 threads at most.
+constexpr int64_t kF8MostColumns = 1 << 23;  // a multiple of 128
+inline int64_t f8_most_rows(int64_t N) {
+  const int64_t n = N < kF8MostColumns ? N : kF8MostColumns, most = (int64_t{1} << 36) / n / 256 * 256;
+  return most < (1 << 23) ? most : 1 << 23;
+}
+
 // ---- rows around a block ---------------------------------------------------------------
 
 // A count in parts of at most `most`: call(first, n) for each. In 64 bits, since counts go up to 2^31 - 1 and the

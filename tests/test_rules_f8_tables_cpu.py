@@ -5,7 +5,7 @@ import re
 import subprocess
 
 from test_rules_cpu import CSRC, ROOT, _compiled
-from test_rules_f8_cpu import F8_TILES, _f8_parts, _f8_tiles
+from test_rules_f8_cpu import F8_NAMES, F8_TILES, _f8_parts, _f8_tiles
 
 TABLES = r"""
 #include <cstdio>
@@ -54,3 +54,53 @@ def test_sizes_of_the_tests_of_sums_take_every_tile(tmp_path_factory):
     calls = [(m, 2 * n, k, 0, 1) for m, n, k in whole]
     assert set(_f8_tiles(tiles, [(*c, 1) for c in calls])[0]) == {"tile128"}
     assert all((rows, cols) == c[:2] for c, (rows, cols, _, _) in zip(calls, _f8_parts(tmp_path_factory, calls)))
+
+
+GRIDS = r"""
+#include <cstdio>
+#include "sf_ops_rules.h"
+// Reads M N, prints the rows and columns of a call's launches.
+int main() {
+  long long M, N;
+  while (scanf("%lld %lld", &M, &N) == 2)
+    printf("%lld %lld\n", (long long)sf::f8_most_rows(N), (long long)sf::kF8MostColumns);
+}
+"""
+
+
+def test_grids_at_the_ends_of_the_ranges_hold_less_than_2_to_the_32_threads(tmp_path_factory):
+    """Whole launches and what is left of them, up to the largest sizes that a call takes, in parts and tiles as the rule has them."""
+    top = (1 << 31) - 1
+    sizes = (1, 15, 16, 17, 32, 33, 64, 257, 1152, 8191, 8192, 8193, (1 << 23) - 1, 1 << 23, (1 << 23) + 1, (1 << 30) + 3, top)
+    calls = [(m, n) for m in sizes for n in sizes]
+    out = [int(v) for v in subprocess.run([_compiled(tmp_path_factory, "grids", GRIDS)], input="".join("%d %d\n" % c for c in calls),
+                                          capture_output=True, text=True, check=True).stdout.split()]
+    launches = set()
+    for (m, n), rows, cols in zip(calls, out[::2], out[1::2]):
+        assert rows >= 8192 and rows <= 1 << 23 and rows % 256 == 0 and cols % 128 == 0
+        launches |= {(r, c) for r in {min(m, rows), m % rows} for c in {min(n, cols), n % cols} if r and c}
+    kernels = open(os.path.join(CSRC, "k_gemm_f8.hip")).read()
+    tile = {m[0]: [int(v) for v in m[1].split(",")] for m in re.findall(r"X\((kF8\w+), ([\d, ]+)\)", kernels)}
+    names = re.findall(r"kF8\w+", re.search(r"enum F8Tile \{(.*?)\}", open(os.path.join(CSRC, "sf_ops_rules.h")).read(), re.S).group(1))
+    tiles = _compiled(tmp_path_factory, "grid_tiles", F8_TILES)
+    kinds = ((0, 0, 0), (0, 1, 0), (0, 0, 1), (0, 1, 1), (1, 1, 1))
+    whole = [(r, c, k, *kind) for r, c in sorted(launches) for k in (1, 128, 1152, 4096, 1 << 20) for kind in kinds]
+    parts = _f8_parts(tmp_path_factory, [(r, c * (1 + g), k, codes, exact) for r, c, k, codes, exact, g in whole])
+    grids = set()
+    for (r, c, k, codes, exact, g), (rows, cols, _, _) in zip(whole, parts):
+        cols //= 1 + g
+        grids |= {(rows, cols, k, codes, exact, g)}
+        if rows < r:
+            grids.add((r - rows, c, k, codes, exact, g))
+        elif cols < c:
+            grids.add((r, c - cols, k, codes, exact, g))
+    grids = sorted(grids)
+    taken = _f8_tiles(tiles, [(r, c * (1 + g), k, codes, exact, g) for r, c, k, codes, exact, g in grids])[0]
+    index = {n: names[i] for i, n in enumerate(F8_NAMES)}
+    for (r, c, k, codes, exact, g), name in zip(grids, taken):
+        if name == "few":
+            groups, threads = -(-c // 16), 64 * (8 if k >= 4096 else 4)
+        else:
+            bm, bn, wm, wn, wk = tile[index[name]][:5]
+            groups, threads = -(-r // bm) * -(-c // (bn // 2 if g else bn)), wm * wn * wk * 64
+        assert groups * threads < 1 << 32, (r, c, k, name)
