@@ -461,7 +461,7 @@ int sf_matmul_f8(const sf_codes* a, const sf_codes* b, const float* bias, int M,
  * scale per row and 128 outputs in out_scale (strides in elements, not 0 over more than one entry);
  * ldo a multiple of 16 then, at an address that is one. out_scale is not used otherwise. Codes come of
  * sums in fp32, at half the matrix rate: where a rounding to bf16 before them does no harm, bf16 outputs and then
- * sf_quantize_f8 take less time (16384 x 2 x 4608 x 1152 216 us, codes at once 340; 300 x 2 x 1152 x 1152 9 and 11). */
+ * sf_quantize_f8 take less time (16384 x 2 x 4608 x 1152 some 220 us, codes at once some 350; 300 x 2 x 1152 x 1152 9.6 and 11). */
 enum { SF_ACT_SILU = 0, SF_ACT_GELU_TANH = 1 };
 int sf_gated_matmul_f8(const sf_codes* a, const sf_codes* gate, const sf_codes* up, const float* gate_bias, const float* up_bias,
                        int act, int M, int N, int K, void* out, long long ldo, int out_type, float* out_scale,

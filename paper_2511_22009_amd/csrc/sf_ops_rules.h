@@ -114,26 +114,27 @@ inline F8Choice cheapest_f8_tile(const F8Cost* from, const F8Cost* to, int64_t M
   return best;
 }
 
-// The tiles of each kind of output. Costs from launches of one and of two rounds of each tile at K = 1024 and 4096. Some times (us):
-//   * 256 x 256, of large outputs: 16384 x 4608 x 1152 115, 128 x 256 129, 128 x 128 in pairs 136; 8192^3 492, 535
-//     and 585.
-//   * 128 x 128 in pairs where rounds of the large tiles are left half empty: 16384 x 1152 x 4608 whole 123, 256 x 256
-//     129.
+// The tiles of each kind of output. Costs from launches of one and of two rounds of each tile at K = 1024 and 4096. Some times (us,
+// all of one run: launches of one tile in a row on three sets of operands, codes of a bell as wide as e4m3 goes; codes with
+// smaller magnitudes cost less power, and large products up to a tenth less time):
+//   * 256 x 256, of large outputs: 16384 x 4608 x 1152 122, 128 x 256 134, 128 x 128 in pairs 136; 8192^3 508, 551
+//     and 617.
+//   * 128 x 128 in pairs where rounds of the large tiles are left half empty: 4100 x 2048 x 2048 in fp32.
 //   * 128 x 128 with four stages, eight wavefronts, one per CU, for single rounds of it: 2048 x 2048 x 4096 23, in pairs
-//     31, 128 x 256 37; half a round of 16384 x 128 x 4608 22, 64 x 64 25 (its cost is between what a whole and half a round take).
-//   * 64 x 64 with K split over two groups of wavefronts for small grids: 1024 x 1024 x 4096 11.5, over four 13.3, 32 x 64
-//     13.5; not split 13.9 at 512 x 1024 x 4352, 128 x 128 there 30; in fp32 517 x 1001 x 4321 over four 16.3, not split 25.
-//   * 32 x 64 with one wavefront to a group, two groups (fp32: four) for the smallest: 512 x 1024 x 4352 10.2, 64 x 64 11.8;
-//     300 x 1152 x 1152 5.6 and 6.3; in fp32 100 x 1152 x 4608 11.7 and 14.3, 300 x 1152 x 1152 7.3 and 8.2. With the
-//     groups of the other type, bf16 9.8 to 10.7, 6.3, fp32 512 x 1024 x 4096 14.7 and not 11.7.
-//   * codes: 64 x 256, two workgroups a CU: gated 16384 x 2 x 4608 x 1152 388, 1024 x 2 x 4608 x 1152 33; 128 x 256 with
-//     eight wavefronts, one a CU, 398 and 43; 64 x 256 of that kind 489 and 42. 32 x 256 while a CU gets one or
-//     two of them: 300 x 2 x 1152 x 1152 11.2, 64 x 256 14.6; 2048 x 2 x 2048 x 1024 28 and 23.
-// Up to 32 rows the weights' bytes count, which more and smaller workgroups fetch sooner: 32 x 3456 x 1152 4.4,
-// 64 x 64 6.1; but long weights that a tile's stages fetch faster: 32 x 8192 x 8192 25.8 and 17.7 (16 rows 18.2 and 17.0). Of
+//     31, 128 x 256 31; half a round of 16384 x 128 x 4608 24, 64 x 64 25 (its cost is between what a whole and half a round take).
+//   * 64 x 64 with K split over two groups of wavefronts for small grids: 1024 x 1024 x 4096 11.8, over four 12.7, 32 x 64
+//     13.8; in fp32 517 x 1001 x 4321 over four 16.2, 32 x 64 23.
+//   * 32 x 64 with one wavefront to a group, two groups (fp32: four) for the smallest: 512 x 1024 x 4352 10.6, 64 x 64 11.8,
+//     128 x 128 19; 300 x 1152 x 1152 5.5 and 6.2; in fp32 100 x 1152 x 4608 11.7 and 14.1, 300 x 1152 x 1152 7.2 and 8.0. With four
+//     groups bf16 10.8 and 6.2.
+//   * codes: 64 x 256, two workgroups a CU: gated 16384 x 2 x 4608 x 1152 382, 1024 x 2 x 4608 x 1152 34; 128 x 256 with
+//     eight wavefronts, one a CU, 400 and 42; 32 x 256 491 and 37. 32 x 256 while a CU gets one or
+//     two of them: 300 x 2 x 1152 x 1152 11.1, 64 x 256 14.2; 2048 x 2 x 2048 x 1024 28 and 23.
+// Up to 32 rows the weights' bytes count, which more and smaller workgroups fetch sooner: 32 x 3456 x 1152 4.5, 32 x 64 5.4,
+// 64 x 64 6.1; but long weights that a tile's stages fetch faster: 32 x 8192 x 8192 26.2 and 15.7 (16 rows 17.7 and 15.4). Of
 // 17 rows on each of those workgroups reads as many rows as columns, and a second round of them (fp32: a third) takes longer than
-// 32 x 64: 32 x 3456 x 1152 4.6 and 5.4, 32 x 4608 x 1152 6.5 and 5.5, 32 x 9216 x 1152 8.7 and 5.6 (fp32 4.7 and 7.0, 6.6 and 7.0,
-// 8.8 and 7.3).
+// 32 x 64: 32 x 4608 x 1152 6.4 and 5.4, 32 x 9216 x 1152 8.6 and 5.5 (fp32 3456 columns 4.7 and 6.9, 4608 6.6 and 7.1,
+// 9216 8.7 and 7.2).
 struct F8Tiles {
   const F8Cost *from, *to;
 };
@@ -162,8 +163,8 @@ inline F8Tile choose_gemm_f8_tile(long M, long N, long K, bool codes, bool exact
 
 // A product whose last round of tiles leaves most CUs idle is cheaper as two, one after the other: the rows, or the columns
 // (multiples of 256), that a tile takes in whole rounds or without its last partial column, and the others, each with a tile of its
-// own. 16384 x 1152 x 4608: 1024 columns in one round of 256 x 256 tiles 84 us, 128 columns in 128 x 128 tiles 22, all of them
-// in 2.25 rounds of 128 x 128 in pairs 123. rows, cols: the first part's; M and N where the whole is not to be parted. Products
+// own. 16384 x 1152 x 4608, in the run above: 1024 columns in one round of 256 x 256 tiles 83 us, 128 columns in 128 x 128 tiles 24,
+// both 103, all of them in 2.25 rounds of 128 x 128 in pairs 123; 4224 x 4096 x 4096 81 and 104. rows, cols: the first part's; M and N where the whole is not to be parted. Products
 // below 40 us stay whole (a second launch and its fixed part count there), and those that would gain less than a twelfth.
 inline void choose_gemm_f8_parts(long M, long N, long K, bool codes, bool exact, long& rows, long& cols) {
   rows = M;
