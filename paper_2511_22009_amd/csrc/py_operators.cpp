@@ -150,7 +150,7 @@ int64_t pitch_of(const at::Tensor& t, const char* what, int64_t need) {
   const int64_t ld = t.size(0) > 1 ? t.stride(0) : need;
   if (ld % 16 || ld < need || (uintptr_t)t.data_ptr() % 16)
     bad_value(what, ": rows have to start at multiples of 16 bytes, at least ", need, " apart (strides ", t.strides(),
-              "); quantize_rows leaves them so");
+              "), as quantize_rows and quantize_f8 leave them");
   return ld;
 }
 

@@ -210,3 +210,40 @@ def test_rows_that_become_codes_do_not_see_each_other():
         for m in (slice(0, 1), slice(5, 38), slice(600, 900), slice(200, M - 1)):
             p, t = call(m)
             assert torch.equal(p.view(torch.uint8), q[m].view(torch.uint8)) and torch.equal(t, s[m])
+
+
+def test_offsets_past_32_bits():
+    """Tensors of over 2^32 entries: what lies on both sides of 2^31, 2^32 and at the end is what smaller calls give there."""
+    from paper_2511_22009_amd import gated_matmul_f8, matmul_f8, quantize_f8, residual_norm
+    g = gen(70)
+    M, W = 70001, 65536
+    rows = [*range(5), *range(32766, 32770), *range(65534, 65538), *range(M - 5, M)]
+    x = torch.zeros((M, W), device="cuda", dtype=BF16)
+    x[rows] = randn(g, len(rows), W, dtype=BF16)
+    a, sa = quantize_f8(x)
+    want = quantize_f8(x[rows])
+    assert torch.equal(a.view(torch.uint8)[rows], want[0].view(torch.uint8)) and torch.equal(sa[rows], want[1])
+    assert int(torch.count_nonzero(sa.any(1))) == len(rows)
+    # a product that reads them, and one that writes as many
+    b, sb = P.codes(g, 40, W, 128)
+    out = matmul_f8(a, sa, b, sb, dtype=FP32)
+    P.check(out[rows], *P.product(a[rows], sa[rows], b, sb, exact=True), FP32)
+    del x, a, sa, out
+    (a, sa), (b, sb), (u, su) = (P.codes(g, n, 48, r) for n, r in ((M, 1), (W, 128), (W, 128)))
+    out = matmul_f8(a, sa, b, sb)
+    P.check(out[rows], *P.product(a[rows], sa[rows], b, sb, exact=False), BF16)
+    del out
+    q, s = gated_matmul_f8(a, sa, b, sb, u, su, dtype=F8)
+    want = gated_matmul_f8(a[rows], sa[rows], b, sb, u, su, dtype=F8)   # codes have one order of sums
+    assert torch.equal(q.view(torch.uint8)[rows], want[0].view(torch.uint8)) and torch.equal(s[rows], want[1])
+    del q, s, a, b, u
+    T, D = 131100, 16384
+    tokens = [0, 1, *range(65534, 65538), T - 2, T - 1]
+    h = torch.ones((2, T, D), device="cuda", dtype=BF16)
+    part = randn(g, 2, len(tokens), D, dtype=BF16)
+    h[:, tokens] = part
+    y = randn(g, 1, 1, D, dtype=BF16)
+    want, (wq, ws) = residual_norm(part, y.expand(2, len(tokens), -1).contiguous(), post="rms", pre="layer", dtype=F8)
+    got, (q, s) = residual_norm(h, y.expand(2, T, -1), post="rms", pre="layer", dtype=F8, h_out=h)
+    assert torch.equal(got[:, tokens], want) and torch.equal(s[:, tokens], ws)
+    assert torch.equal(q.view(torch.uint8)[:, tokens], wq.view(torch.uint8))
