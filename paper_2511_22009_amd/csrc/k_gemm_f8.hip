@@ -15,10 +15,10 @@
 // are codes, are for what comes after to see more than that: the operands' codes are converted to fp16, which holds
 // every one, and multiplied by v_mfma_f32_16x16x32_f16 at half the rate (1e-8 on the same codes).
 //
-// What bounds it. Large products in bf16: the matrix cores at the clock that their power leaves, 8192^3 492 us, 2235
-// TFLOP/s (a library's product with one scale per operand, without the fmas, 409). Outputs that are exact: the vector
+// What bounds it. Large products in bf16: the matrix cores at the clock that their power leaves, 8192^3 482 to 503 us by
+// the codes' magnitudes, 2280 to 2190 TFLOP/s (a library's product with one scale per operand, without the fmas, 409). Outputs that are exact: the vector
 // unit, which converts 128 pairs of codes and runs 64 fmas of a wavefront's 64 x 64 outputs a slice beside 1024 cycles of
-// matrix work: gated 16384 x 2 x 4608 x 1152 to codes 333 us, to fp32 335, to bf16 177. Single rounds of tiles:
+// matrix work: gated 16384 x 2 x 4608 x 1152 to codes 333 to 359 us, to fp32 335, to bf16 176. Single rounds of tiles:
 // the first slices and the outputs of all at once (gated 4096 x 2 x 2048 x 768 17 us). Few tiles: a turn's latencies and the
 // L2's rate to one CU (517 x 1001 x 4321 fp32 15). Few rows: the weights' bytes and one chain of latencies (8 x 2 x 2048 x 768
 // 4.7, the host's part of a call among them).

@@ -2,8 +2,8 @@
 //   u = post(y) post_gain,  h' = r h + gate u,  a = pre(h') pre_gain (1 + scale) + shift,
 // each norm the division by the root mean square, or that of what the mean leaves, or none. Bandwidth
 // bounds it: h and y are read once, h' and a written once, and a row stays in registers between its
-// two norms. 4 x 4096 rows of 1152 dims, h fp32, y bf16, a as codes: 50 us, 4.2 TB/s (a as bf16 47, 4.8 TB/s; the rate
-// of a large copy 41); 2760 rows of 771 dims in fp32 9.8; one row of 1152 4.3 in the kernel.
+// two norms. 4 x 4096 rows of 1152 dims, h fp32, y bf16, a as codes: 49 us, 4.2 TB/s (a as bf16 46, 4.9 TB/s; the rate
+// of a large copy 41); 2760 rows of 771 dims in fp32 9.9; eight rows of 1152 4.5 in the kernel.
 #include "sf_f8_device.h"
 #include "sf_ops_rules.h"
 
