@@ -59,6 +59,10 @@ const auto kFloats = {at::kFloat};
 const auto kCodes = {at::kChar};
 const auto kF8Codes = {at::kFloat8_e4m3fn};
 
+// A tensor of the call under way whose class dispatches to Python: a fake of torch's tracing, whose address is no memory, or
+// one that keeps its values elsewhere. stream_of() refuses it, after every other check, which CPU tests run on fakes.
+thread_local const char* t_elsewhere = nullptr;
+
 const at::Tensor& tensor(PyObject* o, const char* what, std::initializer_list<at::ScalarType> types) {
   if (!THPVariable_Check(o) || !THPVariable_Unpack(o).is_cuda()) bad_type(what, ": expected a CUDA tensor");
   const at::Tensor& t = THPVariable_Unpack(o);
@@ -67,6 +71,8 @@ const at::Tensor& tensor(PyObject* o, const char* what, std::initializer_list<at
   if (c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(0).defined())
     bad_type(what, ": carries a forward-mode tangent, and nothing here is differentiated; call with the primal that unpack_dual() gives");
   if (t.is_neg()) bad_type(what, ": a lazily negated view, whose memory holds the opposite values; call resolve_neg()");
+  if (t._is_zerotensor()) bad_type(what, ": zeros without memory; clone it");
+  if (!t_elsewhere && t.unsafeGetTensorImpl()->is_python_dispatch()) t_elsewhere = what;
   for (const at::ScalarType s : types)
     if (t.scalar_type() == s) return t;
   bad_type(what, ": expected ", types.size() > 1 ? "BFloat16 or Float" : c10::toString(*types.begin()), ", got ",
@@ -85,7 +91,9 @@ const float* vector(PyObject* o, const char* what, int64_t n, int device, bool n
   return (const float*)t.data_ptr();
 }
 
+// The stream of a call whose tensors have passed their checks.
 void* stream_of(int device) {
+  if (t_elsewhere) bad_type(t_elsewhere, ": a fake tensor, or one of a class with a dispatch of its own, has no values at its address");
   PyObject* const index = PyLong_FromLong(device);
   PyObject* const raw = index ? PyObject_CallOneArg(g_raw_stream, index) : nullptr;
   Py_XDECREF(index);
@@ -171,8 +179,8 @@ PyObject* quantize_rows(PyObject* const* args) {
     ldc = pitch_of(codes, "out", need);
   }
   float* to = const_cast<float*>(vector(args[2], "scale", rows, device, true));
-  const c10::DeviceGuard guard(x.device());
   void* const stream = stream_of(device);
+  const c10::DeviceGuard guard(x.device());
   const int rc = unlocked([&] {
     if (!codes.defined()) {
       codes = at::empty_strided({rows, ldc}, {ldc, 1}, x.options().dtype(at::kChar));
@@ -224,8 +232,8 @@ PyObject* matmul_i8(PyObject* const* args) {
                 out.strides(), " on ", out.device());
     if (M > 1) ldo = out.stride(0);
   }
-  const c10::DeviceGuard guard(a.device());
   void* const stream = stream_of(device);
+  const c10::DeviceGuard guard(a.device());
   const int rc = unlocked([&] {
     if (!out.defined()) out = at::empty_strided({M, N}, {N, 1}, a.options().dtype(type == SF_PREC_BF16 ? at::kBFloat16 : at::kFloat));
     return g_matmul_i8((const signed char*)a.data_ptr(), lda, sa, (const signed char*)b.data_ptr(), ldb, sb, bias, m, n, k,
@@ -295,8 +303,8 @@ PyObject* rotate(PyObject* const* args) {
   if (inverse < 0) throw Raised{};
   at::Tensor out = heads_out(x, "x", args[4]);
   const int rows = as_int(x.size(0), "x"), tokens = as_int(x.size(1), "x"), heads = as_int(x.size(2), "x"), dims = as_int(x.size(3), "x");
-  const c10::DeviceGuard guard(x.device());
   void* const stream = stream_of(x.get_device());
+  const c10::DeviceGuard guard(x.device());
   const int rc = unlocked([&] {
     const sf_heads h = heads_of(x, heads, out);
     return g_rotate(&h, type_of(x), rows, tokens, dims, rope, pos.at, pos.row, inverse, stream);
@@ -334,8 +342,8 @@ PyObject* qk_norm_rotate(PyObject* const* args) {
   if (k) k_out = heads_out(*k, "k", args[8]);
   const int rows = as_int(q.size(0), "q"), tokens = as_int(q.size(1), "q"), dh = as_int(dims, "q");
   const int q_heads = as_int(q.size(2), "q"), k_heads = k ? as_int(k->size(2), "k") : 0;
-  const c10::DeviceGuard guard(q.device());
   void* const stream = stream_of(device);
+  const c10::DeviceGuard guard(q.device());
   const int rc = unlocked([&] {
     const sf_heads hq = heads_of(q, q_heads, q_out), hk = k ? heads_of(*k, k_heads, k_out) : sf_heads{};
     return g_qk_norm_rotate(&hq, k ? &hk : nullptr, q_gain, k_gain, (float)eps, type_of(q), rows, tokens, dh, rope, pos.at,
@@ -396,8 +404,8 @@ PyObject* quantize_f8(PyObject* const* args) {
     ldc = pitch_of(codes, "out", need);
   }
   if (args[3] != Py_None) scale = scales_given(args[3], "scale", scale_rows, blocks, x);
-  const c10::DeviceGuard guard(x.device());
   void* const stream = stream_of(x.get_device());
+  const c10::DeviceGuard guard(x.device());
   const int rc = unlocked([&] {
     if (!codes.defined()) {
       codes = at::empty_strided({rows, ldc}, {ldc, 1}, x.options().dtype(at::kFloat8_e4m3fn));
@@ -448,8 +456,8 @@ PyObject* matmul_f8(PyObject* const* args) {
   const long type = long_of(args[5]);
   int64_t ldo = N;
   at::Tensor out = product_out(args[6], M, N, a, false, &ldo);
-  const c10::DeviceGuard guard(a.device());
   void* const stream = stream_of(a.get_device());
+  const c10::DeviceGuard guard(a.device());
   const int rc = unlocked([&] {
     if (!out.defined()) out = at::empty_strided({M, N}, {N, 1}, a.options().dtype(scalar_of(type)));
     return g_matmul_f8(&ca, &cb, bias, m, n, k, out.data_ptr(), ldo, type_of(out), stream);
@@ -478,8 +486,8 @@ PyObject* gated_matmul_f8(PyObject* const* args) {
     if (!codes) bad_value("out_scale: only with outputs that are codes");
     scale = scales_given(args[11], "out_scale", M, blocks_of(N), a);
   }
-  const c10::DeviceGuard guard(a.device());
   void* const stream = stream_of(a.get_device());
+  const c10::DeviceGuard guard(a.device());
   const int rc = unlocked([&] {
     if (!out.defined()) {
       if (codes) ldo = codes_pitch(N);
@@ -584,8 +592,8 @@ PyObject* residual_norm(PyObject* const* args) {
         scale.size(dim - 1) != blocks_of(dims))
       bad_value("out_scale: expected one value per row and ", SF_F8_BLOCK, " dims on ", h.device(), ", got ", scale.sizes(), " on ", scale.device());
   }
-  const c10::DeviceGuard guard(h.device());
   void* const stream = stream_of(device);
+  const c10::DeviceGuard guard(h.device());
   const int rc = unlocked([&] {
     if (!h_out.defined()) h_out = at::empty(h.sizes(), h.options());
     const Rows ho = rows_of(h_out, "h_out");
@@ -668,6 +676,7 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
     PyErr_Format(PyExc_TypeError, n != N ? "expected %d arguments" : "not bound", N);
     return nullptr;
   }
+  t_elsewhere = nullptr;
   try {
     return F(args);
   } catch (const Refused& e) {

@@ -11,7 +11,8 @@ allocated for that stream. With a `stream` other than the current one, ordering 
 the work that fills the inputs is the caller's, as in torch; the inputs' memory is kept
 until the stream is done with it. Nothing is differentiated: a tensor that requires grad is
 a TypeError unless gradients are off (torch.no_grad, torch.inference_mode), and so is one
-that carries a forward-mode tangent.
+that carries a forward-mode tangent. So is a tensor whose values are not at its address: a fake
+of torch's tracing, or one of a class with a dispatch of its own.
 """
 import ctypes
 

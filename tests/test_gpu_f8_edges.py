@@ -247,3 +247,25 @@ def test_offsets_past_32_bits():
     got, (q, s) = residual_norm(h, y.expand(2, T, -1), post="rms", pre="layer", dtype=F8, h_out=h)
     assert torch.equal(got[:, tokens], want) and torch.equal(s[:, tokens], ws)
     assert torch.equal(q.view(torch.uint8)[:, tokens], wq.view(torch.uint8))
+
+
+def test_tensors_without_values_at_their_address_are_refused():
+    """Zeros that autograd keeps without memory, fakes of tracing; parameters and plain subclasses have theirs."""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    from paper_2511_22009_amd import quantize_f8, quantize_rows, residual_norm
+    x = randn(gen(13), 4, 64)
+
+    class Rows(torch.Tensor):
+        pass
+    for call in (quantize_rows, quantize_f8, lambda t: residual_norm(t, x, pre="rms"), lambda t: residual_norm(x, x, gate=t[0])):
+        with pytest.raises(TypeError, match="zeros"):
+            call(torch._efficientzerotensor((4, 64), device="cuda"))
+        with FakeTensorMode() as mode:
+            fake = mode.from_tensor(x)
+        with pytest.raises(TypeError, match="fake"):
+            call(fake)
+        want = call(x)
+        with torch.no_grad():
+            for t in (torch.nn.Parameter(x), x.as_subclass(Rows)):
+                for p, q in zip(call(t), want):
+                    assert (p is None and q is None) or torch.equal(p.float(), q.float())
