@@ -456,7 +456,8 @@ int sf_matmul_f8(const sf_codes* a, const sf_codes* b, const float* bias, int M,
 
 /* The first half of a gated feed-forward in one pass over its rows:
  *   out[m][n] = act(G[m][n]) U[m][n],  G = A . gate^T + gate_bias, U = A . up^T + up_bias
- * both as sf_matmul_f8 has them, N rows of weights each, act SF_ACT_SILU (x / (1 + e^-x)) or SF_ACT_GELU_TANH.
+ * both as sf_matmul_f8 has them, N rows of weights each, act SF_ACT_SILU (x / (1 + e^-x)) or SF_ACT_GELU_TANH
+ * (of either, what is below 1e-35 in magnitude may be 0).
  * out_type SF_PREC_*: values. SF_TYPE_F8: codes as sf_quantize_f8 makes them of the fp32 values, one
  * scale per row and 128 outputs in out_scale (strides in elements, not 0 over more than one entry);
  * ldo a multiple of 16 then, at an address that is one. out_scale is not used otherwise. Codes come of
